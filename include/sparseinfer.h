@@ -404,6 +404,149 @@ si_status si_predict_sparse_mlp_i8(const uint32_t* signs, const int8_t* w_gate, 
                                    void* workspace, size_t workspace_bytes, uint32_t flags, int32_t* counters,
                                    void* stream);
 
+/*
+ * MXFP4 weights: 4-bit floating point with a scale for every 32 values.  A row
+ * of n values is stored as np = 128 ceil(n / 128) of them (zeros behind the
+ * n-th):
+ *   codes  : [rows][np / 2] uint8, two 4-bit codes a byte, value 2 j in the low
+ *            half of byte j.  A code is a sign bit (8) and one of
+ *            0, 0.5, 1, 1.5, 2, 3, 4, 6 (0 .. 7).
+ *   scales : [rows][np / 32] uint8, X + 127 for a scale of 2^X; 255 is NaN.
+ * A value is its code times the scale of its 32.
+ */
+
+/* Element types of the calls that take more than one. */
+typedef enum { SI_F16 = 0, SI_BF16 = 1, SI_F32 = 2 } si_dtype;
+
+/* Bytes of the codes and of the scales of `rows` rows of n values (0 for
+ * rows outside [0, 2^24] or n outside [1, 2^24]).  Host-only. */
+size_t si_mxfp4_codes_bytes(int rows, int n);
+size_t si_mxfp4_scales_bytes(int rows, int n);
+
+/*
+ * Rows to MXFP4: weights once at load, activations in front of a product with
+ * _a4.  For each 32 values v of a row (the last ones padded with zeros), with m
+ * the largest |v|:
+ *   X = floor(log2 m) - 2, at least -127; the code of v is the nearest to
+ *   v / 2^X, ties to the even code, 6 where |v| / 2^X > 6, with v's sign (that
+ *   of zeros too).
+ * m = 0 gives the scale byte 0; a block with an infinity or a NaN the byte 255
+ * and codes of signs alone, so that it reads back as NaN.
+ *   w     : rows of n values of type w_dtype, ldw elements from row to row
+ *           (ldw >= n where rows > 1), at any address that fits an element.
+ *   q, scale : written, si_mxfp4_codes_bytes / si_mxfp4_scales_bytes.
+ *   rows  : 0 to 2^24 (0 does nothing); n: 1 to 2^24, any length.
+ */
+si_status si_quantize_rows_mxfp4(const void* w, int w_dtype, size_t ldw, int rows, int n, uint8_t* q, uint8_t* scale,
+                                 void* stream);
+
+/* MXFP4 rows as values: w [rows][n] of type w_dtype (rounded to nearest even
+ * where the type cannot hold a value; exact in bf16 and float32 down to
+ * 2^-126, and in fp16 for rows quantized from fp16). */
+si_status si_dequantize_rows_mxfp4(const uint8_t* q, const uint8_t* scale, int rows, int n, void* w, int w_dtype,
+                                   void* stream);
+
+/*
+ * Packed signs of MXFP4 W_gate (or W_fc1) codes [k][d / 2], once at load, in
+ * the layout of si_pack_signs: si_predict accepts them as they are.  They are
+ * the signs of the values that were quantized.
+ */
+si_status si_pack_signs_mxfp4(const uint8_t* q_gate, int k, int d, uint32_t* signs, void* stream);
+
+/*
+ * Products with MXFP4 weights, for prompts and for tokens whose rows are not
+ * predicted, float32 accumulation on the matrix cores:
+ *   si_linear_mxfp4       : y[t][i] = sum_j x[t][j] W[i][j]
+ *   si_gated_linear_mxfp4 : h[t][i] = max(sum_j x[t][j] W_gate[i][j], 0) *
+ *                           (sum_j x[t][j] W_up[i][j]), Eq. (1) steps 1-3 over
+ *                           every row; q_up = s_up = NULL: the non-gated
+ *                           max(sum_j x[t][j] W_fc1[i][j], 0).
+ *   x  : m rows of n values, fp16 or bf16 (x_dtype), ldx elements from row to
+ *        row (ldx >= n where m > 1), at any address that fits an element.
+ *        With fp16 activations the weights take part as their fp16 values (the
+ *        values themselves for weights quantized from fp16; beyond fp16's range
+ *        infinities, and multiples of 2^-24 below its normal numbers); with bf16
+ *        as they are.
+ *   q, scale : W's [rows] rows of n values in MXFP4.
+ *   y (h)    : [m][rows] of type y_dtype, written.
+ *   m 0 to 2^24 (0 does nothing), rows 1 to 2^24, n 1 to 2^20; SI_ERR_SHAPE too
+ *   where a launch would exceed 2^32 threads.
+ *   workspace: si_linear_mxfp4_workspace_bytes() bytes of scratch (may be NULL
+ *        where that is 0); nothing is kept in it from one call to the next, and
+ *        two calls that can run at the same time need one each.
+ * The _a4 forms take the activations in MXFP4 as well (xq, x_scale from
+ * si_quantize_rows_mxfp4): products of 4-bit values with both scales, on the
+ * matrix cores' own 4-bit instructions.
+ * The sums' order depends on the shapes alone: the same call gives the same bits.
+ */
+si_status si_linear_mxfp4(const void* x, int x_dtype, size_t ldx, int m, int n, const uint8_t* q, const uint8_t* scale,
+                          int rows, void* y, int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
+si_status si_gated_linear_mxfp4(const void* x, int x_dtype, size_t ldx, int m, int n, const uint8_t* q_gate,
+                                const uint8_t* s_gate, const uint8_t* q_up, const uint8_t* s_up, int rows, void* h,
+                                int h_dtype, void* workspace, size_t workspace_bytes, void* stream);
+si_status si_linear_mxfp4_a4(const uint8_t* xq, const uint8_t* x_scale, int m, int n, const uint8_t* q,
+                             const uint8_t* scale, int rows, void* y, int y_dtype, void* workspace,
+                             size_t workspace_bytes, void* stream);
+si_status si_gated_linear_mxfp4_a4(const uint8_t* xq, const uint8_t* x_scale, int m, int n, const uint8_t* q_gate,
+                                   const uint8_t* s_gate, const uint8_t* q_up, const uint8_t* s_up, int rows, void* h,
+                                   int h_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of the four products (`gated` nonzero: with W_up; x NULL:
+ * the _a4 forms).  Of x only the alignment counts, with ldx: activations that
+ * cannot be read in 16-byte pieces are copied into the workspace.  0 for
+ * unsupported shapes and where none is needed.  Host-only. */
+size_t si_linear_mxfp4_workspace_bytes(const void* x, size_t ldx, int m, int rows, int n, int gated);
+
+/* Bytes of the workspace of the two calls below (0 for unsupported shapes): a
+ * si_workspace_bytes() workspace with more behind it, under the same rules
+ * (zero-filled before its first use, one call at a time); si_read_h3 and
+ * si_workspace_check accept it. */
+size_t si_mxfp4_workspace_bytes(int k, int d, int b);
+
+/*
+ * The MXFP4 forms of si_sparse_mlp (mask mode) and si_predict_sparse_mlp, with
+ * their arguments, flags, counters and outputs, for every supported shape:
+ *   q_gate, s_gate, q_up, s_up : W_gate, W_up [k] rows of d values in MXFP4
+ *        (q_up = s_up = NULL: the non-gated ReLU MLP);
+ *   q_down_t, s_down_t : W_down^T, [k] rows of d values in MXFP4 (transposed
+ *        first, then quantized: a scale covers 32 columns of y).
+ * Two launches, which do not need the device to themselves; y is the same bits
+ * in every run.  x and y must not overlap.  A kept row whose gate value is NaN
+ * makes y NaN.
+ */
+si_status si_sparse_mlp_mxfp4(const uint8_t* q_gate, const uint8_t* s_gate, const uint8_t* q_up, const uint8_t* s_up,
+                              const uint8_t* q_down_t, const uint8_t* s_down_t, int k, int d, const uint16_t* x, int b,
+                              const uint8_t* mask, float* y, void* workspace, size_t workspace_bytes, uint32_t flags,
+                              int32_t* counters, void* stream);
+si_status si_predict_sparse_mlp_mxfp4(const uint32_t* signs, const uint8_t* q_gate, const uint8_t* s_gate,
+                                      const uint8_t* q_up, const uint8_t* s_up, const uint8_t* q_down_t,
+                                      const uint8_t* s_down_t, int k, int d, const uint16_t* x, int b, float alpha,
+                                      uint8_t* mask, int32_t* active_idx, int32_t* n_active, float* y, void* workspace,
+                                      size_t workspace_bytes, uint32_t flags, int32_t* counters, void* stream);
+
+/*
+ * What stands between the products of two blocks, in one pass over each token:
+ *   P  = RMSNorm(branch) * post_w, or branch itself where post_w is NULL
+ *   h' = h + scale * gate * P       (gate NULL: 1; branch NULL: h' = h)
+ *   x  = RMSNorm(h') * pre_w        (of h' before it is rounded to h_out's type)
+ * with RMSNorm(v) = v / sqrt(mean(v^2) + eps), in float32.
+ *   h, h_out : tokens rows of d values of type h_dtype, ldh and ldo elements
+ *        from row to row; h_out is written and may be h itself, or NULL.
+ *   branch   : rows of type branch_dtype, ldb; NULL (with post_w, gate and h_out
+ *        NULL): only x is formed.
+ *   post_w, pre_w : [d] float32; pre_w and x both given or both NULL.
+ *   gate     : [ceil(tokens / rows_per_gate)][d] float32: token t is multiplied
+ *        with row t / rows_per_gate (rows_per_gate = tokens: one gate for all).
+ *   x        : rows of type x_dtype, ldx, written.
+ *   tokens 0 to 2^23 - 1 (0 does nothing), d 1 to 16384, strides >= d where
+ *   tokens > 1, addresses that fit an element.  At least one of h_out and x.
+ *   Outputs must not overlap anything else (columns of one matrix do not).
+ */
+si_status si_norm_residual(const void* h, int h_dtype, size_t ldh, const void* branch, int branch_dtype, size_t ldb,
+                           const float* post_w, const float* gate, int rows_per_gate, float scale, void* h_out,
+                           size_t ldo, const float* pre_w, void* x, int x_dtype, size_t ldx, int tokens, int d,
+                           float eps, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

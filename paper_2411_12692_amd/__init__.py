@@ -4,7 +4,9 @@ Thin PyTorch-facing binding of ``libsparseinfer.so`` (see
 ``include/sparseinfer.h``).  PyTorch only provides device memory and the
 current stream; every step of the path runs in the library's HIP kernels.
 The functions take contiguous CUDA tensors: fp16 weights/inputs (``float16``
-or ``int16`` bit patterns), and return new tensors.
+or ``int16`` bit patterns), and return new tensors.  The MXFP4 products and
+``norm_residual`` also take bf16 and float32 and rows with a stride, and run on
+the device of their tensors.
 """
 
 from __future__ import annotations
@@ -20,6 +22,9 @@ __all__ = [
     "sparse_mlp", "predict_sparse_mlp", "mlp_block", "MLPLayer",
     "quantize_rows_i8", "pack_signs_i8", "transpose_down_i8", "sparse_mlp_i8", "predict_sparse_mlp_i8",
     "Int8MLPLayer",
+    "quantize_rows_mxfp4", "dequantize_rows_mxfp4", "pack_signs_mxfp4", "linear_mxfp4", "gated_linear_mxfp4",
+    "linear_mxfp4_a4", "gated_linear_mxfp4_a4", "mxfp4_workspace_bytes", "new_workspace_mxfp4", "sparse_mlp_mxfp4",
+    "predict_sparse_mlp_mxfp4", "MXFP4MLPLayer", "norm_residual",
 ]
 
 
@@ -254,8 +259,13 @@ class MLPLayer:
                                   flags=flags, outputs=outputs, y=y)
 
     def block(self, h, norm_w, eps: float, alpha: float, flags: int = 0, outputs: bool = False,
-              y: torch.Tensor = None):
-        """``h + MLP(RMSNorm(h) * norm_w)`` in one launch (see ``mlp_block``)."""
+              y: torch.Tensor = None, post_norm_w=None, gate=None, scale: float = 1.0):
+        """``h + MLP(RMSNorm(h) * norm_w)`` in one launch (see ``mlp_block``).
+        With a norm behind the MLP, a gate or a residual scale
+        (``h + scale * gate * RMSNorm(MLP(..)) * post_norm_w``) the call is
+        ``norm_residual`` in front of and behind the MLP."""
+        if post_norm_w is not None or gate is not None or scale != 1.0:
+            return _block(self, h, norm_w, eps, alpha, flags, outputs, y, post_norm_w, gate, scale)
         return mlp_block(h, norm_w, eps, self.signs, self.w_gate, self.w_up, self.w_down_t, alpha, self.workspace,
                          flags=flags, outputs=outputs, y=y)
 
@@ -381,6 +391,380 @@ class Int8MLPLayer:
         return predict_sparse_mlp_i8(self.signs, self.q_gate, self.s_gate, self.q_up, self.s_up, self.q_down_t,
                                      self.s_down, x, alpha, self.workspace, flags=flags, outputs=outputs, y=y)
 
+    def block(self, h, norm_w, eps: float, alpha: float, flags: int = 0, outputs: bool = False,
+              y: torch.Tensor = None, post_norm_w=None, gate=None, scale: float = 1.0):
+        """``h + scale * gate * [RMSNorm](MLP(RMSNorm(h) * norm_w))`` (see
+        ``MLPLayer.block``): ``norm_residual`` in front of and behind the MLP."""
+        return _block(self, h, norm_w, eps, alpha, flags, outputs, y, post_norm_w, gate, scale)
+
     def sparse_mlp(self, x, mask, flags: int = 0, counters: bool = False):
         return sparse_mlp_i8(self.q_gate, self.s_gate, self.q_up, self.s_up, self.q_down_t, self.s_down, x,
                              self.workspace, mask, flags, counters)
+
+
+# ---- MXFP4 weights and the norms around a block -----------------------------
+
+_DTYPE = {torch.float16: _lib.SI_F16, torch.int16: _lib.SI_F16, torch.bfloat16: _lib.SI_BF16,
+          torch.float32: _lib.SI_F32}
+_HALF = (torch.float16, torch.int16, torch.bfloat16)
+_ANY = (*_HALF, torch.float32)
+
+
+def _call_on(device: torch.device, name: str, *args) -> None:
+    """``name(*args, stream)`` on ``device``'s current stream; ``device`` need
+    not be the current one."""
+    if device.index == torch.cuda.current_device():
+        _lib.call(name, *args, _stream())
+    else:
+        with torch.cuda.device(device):
+            _lib.call(name, *args, _stream())
+
+
+def _same_device(*tensors):
+    device = tensors[0].device
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors on {device} and {t.device}")
+    return device
+
+
+def _rows(t, name: str, dtypes):
+    """A ``[rows][n]`` tensor (or one row ``[n]``) whose rows are contiguous, with
+    any stride between them: returns it with two dims and the stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor (got {t.device})")
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+    if t.dim() == 1:
+        t = t.unsqueeze(0)
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be [rows][n], got {tuple(t.shape)}")
+    rows, n = t.shape
+    if n > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    ld = t.stride(0) if rows > 1 else n
+    if ld < n:
+        raise ValueError(f"{name}'s rows overlap")
+    return t, ld
+
+
+def _mx(q, scale, name: str, n: int = None):
+    """Checks MXFP4 rows; ``n`` values long when given."""
+    _dev(q, name, (torch.uint8,), 2)
+    _dev(scale, f"{name}'s scales", (torch.uint8,), 2)
+    rows, width = q.shape
+    if width % 64 or tuple(scale.shape) != (rows, width // 16):
+        raise ValueError(f"{name} {tuple(q.shape)} and its scales {tuple(scale.shape)} are not MXFP4 rows")
+    if n is not None and width != (n + 127) // 128 * 64:
+        raise ValueError(f"{name} has rows of {2 * width} stored values, {n} do not take that many")
+    return rows
+
+
+def quantize_rows_mxfp4(w: torch.Tensor):
+    """Rows ``w [rows][n]`` (fp16, bf16 or float32, any row stride) to MXFP4
+    (``si_quantize_rows_mxfp4``): returns the codes, uint8 ``[rows][np / 2]``, and
+    scales, uint8 ``[rows][np / 32]``, with ``np`` = ``n`` rounded up to 128."""
+    w, ld = _rows(w, "w", _ANY)
+    rows, n = w.shape
+    np_ = (n + 127) // 128 * 128
+    q = torch.empty(rows, np_ // 2, dtype=torch.uint8, device=w.device)
+    scale = torch.empty(rows, np_ // 32, dtype=torch.uint8, device=w.device)
+    _call_on(w.device, "si_quantize_rows_mxfp4", _vp(w), _DTYPE[w.dtype], ld, rows, n, _vp(q), _vp(scale))
+    return q, scale
+
+
+def dequantize_rows_mxfp4(q: torch.Tensor, scale: torch.Tensor, n: int, dtype=torch.float16) -> torch.Tensor:
+    """MXFP4 rows of ``n`` values as ``[rows][n]`` of ``dtype``
+    (``si_dequantize_rows_mxfp4``)."""
+    rows = _mx(q, scale, "q", n)
+    if dtype not in _ANY:
+        raise TypeError(f"dtype {dtype}, expected one of {_ANY}")
+    device = _same_device(q, scale)
+    w = torch.empty(rows, n, dtype=dtype, device=device)
+    _call_on(device, "si_dequantize_rows_mxfp4", _vp(q), _vp(scale), rows, n, _vp(w), _DTYPE[dtype])
+    return w
+
+
+def pack_signs_mxfp4(q_gate: torch.Tensor) -> torch.Tensor:
+    """Packed signs of MXFP4 ``W_gate`` codes (the layout of ``pack_signs``)."""
+    _dev(q_gate, "q_gate", (torch.uint8,), 2)
+    k, d = q_gate.shape[0], 2 * q_gate.shape[1]
+    nbytes = signs_bytes(k, d)
+    if nbytes == 0:
+        raise ValueError(f"unsupported shape k={k} d={d}")
+    out = torch.empty(nbytes // 4, dtype=torch.int32, device=q_gate.device)
+    _call_on(q_gate.device, "si_pack_signs_mxfp4", _vp(q_gate), k, d, _vp(out))
+    return out
+
+
+def _product(name, x_args, x_ptr, ldx, m, n, weights, out_dtype, device):
+    """One of the four products; ``weights`` is ``q, scale`` or ``q_gate,
+    s_gate, q_up, s_up``.  Scratch comes from torch's allocator, in the stream's
+    order like any tensor."""
+    gated = len(weights) == 4
+    rows = _mx(weights[0], weights[1], "q" if not gated else "q_gate", n)
+    if gated and weights[2] is not None and _mx(weights[2], weights[3], "q_up", n) != rows:
+        raise ValueError("q_up does not match q_gate")
+    if out_dtype not in _ANY:
+        raise TypeError(f"out_dtype {out_dtype}, expected one of {_ANY}")
+    _same_device(*(t for t in weights if t is not None))
+    if weights[0].device != device:
+        raise ValueError(f"activations on {device}, weights on {weights[0].device}")
+    y = torch.empty(m, rows, dtype=out_dtype, device=device)
+    nbytes = _lib.load().si_linear_mxfp4_workspace_bytes(x_ptr, ldx, m, rows, n,
+                                                         1 if gated and weights[2] is not None else 0)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    _call_on(device, name, *x_args, m, n, *(_vp(t) for t in weights), rows, _vp(y), _DTYPE[out_dtype], _vp(ws), nbytes)
+    return y
+
+
+def linear_mxfp4(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, out_dtype=None) -> torch.Tensor:
+    """``x W^T`` with MXFP4 weights ``q, scale`` of ``[rows][n]``
+    (``si_linear_mxfp4``); ``x [m][n]`` fp16 or bf16, any row stride.  Returns
+    ``[m][rows]`` in ``out_dtype`` (``x``'s type)."""
+    x, ld = _rows(x, "x", _HALF)
+    m, n = x.shape
+    return _product("si_linear_mxfp4", (_vp(x), _DTYPE[x.dtype], ld), _vp(x), ld, m, n, (q, scale),
+                    out_dtype or x.dtype, x.device)
+
+
+def gated_linear_mxfp4(x: torch.Tensor, q_gate, s_gate, q_up=None, s_up=None, out_dtype=None) -> torch.Tensor:
+    """``ReLU(x W_gate^T) * (x W_up^T)`` over every row, Eq. (1) steps 1-3 of a
+    prompt (``si_gated_linear_mxfp4``); ``q_up=None``: ``ReLU(x W_fc1^T)``."""
+    x, ld = _rows(x, "x", _HALF)
+    m, n = x.shape
+    return _product("si_gated_linear_mxfp4", (_vp(x), _DTYPE[x.dtype], ld), _vp(x), ld, m, n,
+                    (q_gate, s_gate, q_up, s_up), out_dtype or x.dtype, x.device)
+
+
+def linear_mxfp4_a4(xq: torch.Tensor, x_scale: torch.Tensor, q: torch.Tensor, scale: torch.Tensor,
+                    out_dtype=torch.float16) -> torch.Tensor:
+    """``linear_mxfp4`` with the activations in MXFP4 too
+    (``quantize_rows_mxfp4``), on the 4-bit matrix instructions."""
+    m = _mx(xq, x_scale, "xq")
+    n = 2 * xq.shape[1]
+    return _product("si_linear_mxfp4_a4", (_vp(xq), _vp(x_scale)), None, 0, m, n, (q, scale), out_dtype,
+                    _same_device(xq, x_scale))
+
+
+def gated_linear_mxfp4_a4(xq: torch.Tensor, x_scale: torch.Tensor, q_gate, s_gate, q_up=None, s_up=None,
+                          out_dtype=torch.float16) -> torch.Tensor:
+    """``gated_linear_mxfp4`` with the activations in MXFP4 too."""
+    m = _mx(xq, x_scale, "xq")
+    n = 2 * xq.shape[1]
+    return _product("si_gated_linear_mxfp4_a4", (_vp(xq), _vp(x_scale)), None, 0, m, n,
+                    (q_gate, s_gate, q_up, s_up), out_dtype, _same_device(xq, x_scale))
+
+
+def mxfp4_workspace_bytes(k: int, d: int, b: int = 1) -> int:
+    return int(_lib.load().si_mxfp4_workspace_bytes(k, d, b))
+
+
+def new_workspace_mxfp4(k: int, d: int, b: int = 1, device=None) -> torch.Tensor:
+    """Zero-filled workspace for MXFP4 sparse MLP calls with up to ``b`` tokens."""
+    n = mxfp4_workspace_bytes(k, d, b)
+    if n == 0:
+        raise ValueError(f"unsupported shape k={k} d={d} b={b}")
+    return torch.zeros(n, dtype=torch.uint8, device=device or "cuda")
+
+
+def _mx_mlp_weights(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x):
+    k = _mx(q_gate, s_gate, "q_gate")
+    d = 2 * q_gate.shape[1]
+    if q_up is not None and _mx(q_up, s_up, "q_up", d) != k:
+        raise ValueError("q_up does not match q_gate")
+    if _mx(q_down_t, s_down_t, "q_down_t", d) != k:
+        raise ValueError("q_down_t does not match q_gate")
+    x = _x2(x, d)
+    _same_device(x, q_gate, s_gate, q_up, s_up, q_down_t, s_down_t)
+    return k, d, x, x.shape[0]
+
+
+def _out_y(y, b, d, x):
+    if y is None:
+        return torch.empty(b, d, dtype=torch.float32, device=x.device)
+    _dev(y, "y", (torch.float32,))
+    if y.numel() != b * d:
+        raise ValueError(f"y must hold [{b}][{d}] floats")
+    return y
+
+
+def sparse_mlp_mxfp4(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, workspace, mask, flags: int = 0,
+                     counters: bool = False, y: torch.Tensor = None):
+    """Eq. (1) over the rows kept by ``mask`` with MXFP4 weights
+    (``si_sparse_mlp_mxfp4``); ``q_up=None``: the non-gated ReLU MLP.  Returns
+    ``y [b][d]`` float32 (and the ``[3]`` work counters with ``counters``)."""
+    k, d, x, b = _mx_mlp_weights(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x)
+    _dev(mask, "mask", (torch.uint8,), 1)
+    if mask.numel() != k:
+        raise ValueError(f"mask must hold {k} rows")
+    device = _same_device(x, mask, workspace, y)
+    y = _out_y(y, b, d, x)
+    cnt = torch.empty(3, dtype=torch.int32, device=device) if counters else None
+    _call_on(device, "si_sparse_mlp_mxfp4", _vp(q_gate), _vp(s_gate), _vp(q_up), _vp(s_up), _vp(q_down_t),
+             _vp(s_down_t), k, d, _vp(x), b, _vp(mask), _vp(y), _vp(workspace), workspace.numel(), flags, _vp(cnt))
+    return (y, cnt) if counters else y
+
+
+def predict_sparse_mlp_mxfp4(signs, q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, alpha, workspace,
+                             flags: int = 0, outputs: bool = False, y: torch.Tensor = None):
+    """The whole per-token path with MXFP4 weights
+    (``si_predict_sparse_mlp_mxfp4``); ``signs`` from ``pack_signs_mxfp4``.
+    Returns ``y`` (and ``(mask, active_idx, n_active, counters)`` with
+    ``outputs``)."""
+    k, d, x, b = _mx_mlp_weights(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x)
+    _dev(signs, "signs", (torch.int32,))
+    if signs.numel() * 4 != signs_bytes(k, d):
+        raise ValueError(f"signs do not belong to [{k}][{d}]")
+    device = _same_device(x, signs, workspace, y)
+    y = _out_y(y, b, d, x)
+    if outputs:
+        mask = torch.empty(k, dtype=torch.uint8, device=device)
+        idx = torch.empty(k, dtype=torch.int32, device=device)
+        n = torch.empty(1, dtype=torch.int32, device=device)
+        cnt = torch.empty(3, dtype=torch.int32, device=device)
+    else:
+        mask = idx = n = cnt = None
+    _call_on(device, "si_predict_sparse_mlp_mxfp4", _vp(signs), _vp(q_gate), _vp(s_gate), _vp(q_up), _vp(s_up),
+             _vp(q_down_t), _vp(s_down_t), k, d, _vp(x), b, float(alpha), _vp(mask), _vp(idx), _vp(n), _vp(y),
+             _vp(workspace), workspace.numel(), flags, _vp(cnt))
+    return (y, (mask, idx, n, cnt)) if outputs else y
+
+
+def norm_residual(h: torch.Tensor, branch: torch.Tensor = None, post_w: torch.Tensor = None,
+                  gate: torch.Tensor = None, scale: float = 1.0, pre_w: torch.Tensor = None, eps: float = 1e-5,
+                  x_dtype=torch.float16, out: torch.Tensor = None):
+    """What stands between the products of two blocks, in one launch
+    (``si_norm_residual``)::
+
+        h' = h + scale * gate * (RMSNorm(branch) * post_w)   # post_w None: branch itself
+        x  = RMSNorm(h') * pre_w
+
+    ``h`` and ``branch`` are ``[tokens][d]`` (or ``[d]``) in fp16, bf16 or
+    float32, with any row stride; ``gate`` float32 ``[d]`` or ``[g][d]``, each row
+    for ``tokens / g`` consecutive tokens; ``post_w`` and ``pre_w`` float32
+    ``[d]``.  Returns ``(h', x)``: ``h'`` in ``h``'s type (in ``out`` when given,
+    which may be ``h``; None without a branch), ``x`` in ``x_dtype`` (None without
+    ``pre_w``)."""
+    shape = h.shape if isinstance(h, torch.Tensor) else None
+    h2, ldh = _rows(h, "h", _ANY)
+    tokens, d = h2.shape
+    if x_dtype not in _ANY:
+        raise TypeError(f"x_dtype {x_dtype}, expected one of {_ANY}")
+    b2, ldb = h2, 0
+    if branch is not None:
+        b2, ldb = _rows(branch, "branch", _ANY)
+        if b2.shape != h2.shape:
+            raise ValueError(f"branch {tuple(b2.shape)} does not match h {tuple(h2.shape)}")
+    elif post_w is not None or gate is not None or out is not None:
+        raise ValueError("post_w, gate and out need a branch")
+    elif pre_w is None:
+        raise ValueError("nothing to compute: neither branch nor pre_w")
+    for t, name in ((post_w, "post_w"), (pre_w, "pre_w")):
+        if t is not None:
+            _dev(t, name, (torch.float32,), 1)
+            if t.numel() != d:
+                raise ValueError(f"{name} must hold {d} values")
+    per = 1
+    if gate is not None:
+        _dev(gate, "gate", (torch.float32,))
+        g2 = gate.view(1, -1) if gate.dim() == 1 else gate
+        if g2.dim() != 2 or g2.shape[1] != d or g2.shape[0] < 1 or tokens % g2.shape[0]:
+            raise ValueError(f"gate must be [{d}] or [g][{d}] with g dividing {tokens} tokens, got {tuple(gate.shape)}")
+        per = max(tokens // g2.shape[0], 1)
+    h_out = x = None
+    ldo = 0
+    if branch is not None:
+        if out is None:
+            out = torch.empty(shape, dtype=h.dtype, device=h.device)
+        h_out, ldo = _rows(out, "out", (h.dtype,))
+        if h_out.shape != h2.shape:
+            raise ValueError(f"out {tuple(out.shape)} does not match h {tuple(h.shape)}")
+    if pre_w is not None:
+        x = torch.empty(shape, dtype=x_dtype, device=h.device)
+    device = _same_device(h2, b2, post_w, gate, pre_w, h_out)
+    _call_on(device, "si_norm_residual", _vp(h2), _DTYPE[h2.dtype], ldh, _vp(b2) if branch is not None else None,
+             _DTYPE[b2.dtype], ldb, _vp(post_w), _vp(gate), per, float(scale), _vp(h_out), ldo, _vp(pre_w), _vp(x),
+             _DTYPE[x_dtype], d, tokens, d, float(eps))
+    return out if branch is not None else None, x
+
+
+def _block(layer, h, norm_w, eps, alpha, flags, outputs, y, post_norm_w, gate, scale):
+    """The MLP half of a decoder layer around ``layer``'s call: ``h`` float32
+    ``[b][d]``; the result in ``y`` when given."""
+    _dev(h, "h", (torch.float32,))
+    h2 = h.view(-1, layer.d)
+    _, x = norm_residual(h2, pre_w=norm_w, eps=eps)
+    res = layer(x, alpha, flags=flags, outputs=outputs)
+    branch = res[0] if outputs else res
+    if y is not None:
+        _dev(y, "y", (torch.float32,))
+        if y.numel() != h2.numel():
+            raise ValueError(f"y must hold [{h2.shape[0]}][{layer.d}] floats")
+        y = y.view(h2.shape)
+    out, _ = norm_residual(h2, branch, post_w=post_norm_w, gate=gate, scale=scale, eps=eps, out=y)
+    return (out, res[1]) if outputs else out
+
+
+class MXFP4MLPLayer:
+    """One layer with MXFP4 weights, made on the device at load from fp16, bf16
+    or float32 weights ``W_gate``, ``W_up`` (``[k][d]``) and ``W_down``
+    (``[d][k]``): the quantized ``W_gate``, ``W_up`` and ``W_down^T``, and the
+    packed signs.  ``prompt=True`` keeps ``W_down`` quantized along ``k`` as
+    well, for ``prompt`` (its scales cover other values than ``W_down^T``'s).
+    ``w_up=None``: a non-gated ReLU MLP."""
+
+    def __init__(self, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, max_batch: int = 1,
+                 prompt: bool = False):
+        self.k, self.d = w_gate.shape
+        self.q_gate, self.s_gate = quantize_rows_mxfp4(w_gate)
+        self.q_up, self.s_up = quantize_rows_mxfp4(w_up) if w_up is not None else (None, None)
+        if w_down.dtype == torch.float32:
+            w_down_t = w_down.t().contiguous()
+        else:
+            w_down_t = transpose_down(w_down.view(torch.int16)).view(w_down.dtype)
+        self.q_down_t, self.s_down_t = quantize_rows_mxfp4(w_down_t)
+        self.q_down, self.s_down = quantize_rows_mxfp4(w_down) if prompt else (None, None)
+        self.signs = pack_signs_mxfp4(self.q_gate)
+        self.workspace = new_workspace_mxfp4(self.k, self.d, max_batch, w_gate.device)
+
+    def __call__(self, x, alpha: float, flags: int = 0, outputs: bool = False, y: torch.Tensor = None):
+        return predict_sparse_mlp_mxfp4(self.signs, self.q_gate, self.s_gate, self.q_up, self.s_up, self.q_down_t,
+                                        self.s_down_t, x, alpha, self.workspace, flags=flags, outputs=outputs, y=y)
+
+    def sparse_mlp(self, x, mask, flags: int = 0, counters: bool = False):
+        return sparse_mlp_mxfp4(self.q_gate, self.s_gate, self.q_up, self.s_up, self.q_down_t, self.s_down_t, x,
+                                self.workspace, mask, flags, counters)
+
+    def block(self, h, norm_w, eps: float, alpha: float, flags: int = 0, outputs: bool = False,
+              y: torch.Tensor = None, post_norm_w=None, gate=None, scale: float = 1.0):
+        """``h + scale * gate * [RMSNorm](MLP(RMSNorm(h) * norm_w))`` of 1 to 8
+        tokens (see ``MLPLayer.block``)."""
+        return _block(self, h, norm_w, eps, alpha, flags, outputs, y, post_norm_w, gate, scale)
+
+    def prompt(self, x, out_dtype=None, a4: bool = False):
+        """The dense MLP of a prompt, ``x [m][d]`` fp16 or bf16: ``ReLU(x
+        W_gate^T) * (x W_up^T)`` in ``x``'s type, then the product with
+        ``W_down^T``; returns ``[m][d]`` in ``out_dtype`` (``x``'s type).
+        ``a4``: both products take their activations in MXFP4."""
+        if self.q_down is None:
+            raise ValueError("the layer was made without prompt=True")
+        out_dtype = out_dtype or x.dtype
+        if a4:
+            h = gated_linear_mxfp4_a4(*quantize_rows_mxfp4(x), self.q_gate, self.s_gate, self.q_up, self.s_up,
+                                      out_dtype=x.dtype)
+            return linear_mxfp4_a4(*quantize_rows_mxfp4(h), self.q_down, self.s_down, out_dtype)
+        h = gated_linear_mxfp4(x, self.q_gate, self.s_gate, self.q_up, self.s_up)
+        return linear_mxfp4(h, self.q_down, self.s_down, out_dtype)
+
+    def prompt_block(self, h, norm_w, eps: float, x_dtype=torch.bfloat16, a4: bool = False, post_norm_w=None, gate=None,
+                     scale: float = 1.0, next_norm_w=None, out: torch.Tensor = None):
+        """The MLP half of a decoder layer of a prompt: ``norm_residual``,
+        ``prompt``, ``norm_residual``.  Returns ``(h', x')`` with ``x' =
+        RMSNorm(h') * next_norm_w`` for what follows (None without it)."""
+        _, x = norm_residual(h, pre_w=norm_w, eps=eps, x_dtype=x_dtype)
+        branch = self.prompt(x, a4=a4)
+        return norm_residual(h, branch.view(h.shape), post_w=post_norm_w, gate=gate, scale=scale, pre_w=next_norm_w,
+                             eps=eps, x_dtype=x_dtype, out=out)

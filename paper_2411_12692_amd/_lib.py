@@ -25,6 +25,9 @@ SI_ERR_TIMEOUT = 9
 SI_ERR_LIST = 10
 SI_NO_AS = 1
 SI_NO_SPECULATION = 2
+SI_F16 = 0
+SI_BF16 = 1
+SI_F32 = 2
 
 _p = ctypes.c_void_p
 _i = ctypes.c_int
@@ -63,6 +66,21 @@ SIGNATURES = {
                                       _u32, _p, _p]),
     "si_rmsnorm_predict_sparse_mlp": (_i, [_p, _p, _f, _p, _p, _p, _p, _i, _i, _i, _f, _p, _p, _p, _p, _p, _sz,
                                            _u32, _p, _p]),
+    "si_mxfp4_codes_bytes": (_sz, [_i, _i]),
+    "si_mxfp4_scales_bytes": (_sz, [_i, _i]),
+    "si_quantize_rows_mxfp4": (_i, [_p, _i, _sz, _i, _i, _p, _p, _p]),
+    "si_dequantize_rows_mxfp4": (_i, [_p, _p, _i, _i, _p, _i, _p]),
+    "si_pack_signs_mxfp4": (_i, [_p, _i, _i, _p, _p]),
+    "si_linear_mxfp4": (_i, [_p, _i, _sz, _i, _i, _p, _p, _i, _p, _i, _p, _sz, _p]),
+    "si_gated_linear_mxfp4": (_i, [_p, _i, _sz, _i, _i, _p, _p, _p, _p, _i, _p, _i, _p, _sz, _p]),
+    "si_linear_mxfp4_a4": (_i, [_p, _p, _i, _i, _p, _p, _i, _p, _i, _p, _sz, _p]),
+    "si_gated_linear_mxfp4_a4": (_i, [_p, _p, _i, _i, _p, _p, _p, _p, _i, _p, _i, _p, _sz, _p]),
+    "si_linear_mxfp4_workspace_bytes": (_sz, [_p, _sz, _i, _i, _i, _i]),
+    "si_mxfp4_workspace_bytes": (_sz, [_i, _i, _i]),
+    "si_sparse_mlp_mxfp4": (_i, [_p, _p, _p, _p, _p, _p, _i, _i, _p, _i, _p, _p, _p, _sz, _u32, _p, _p]),
+    "si_predict_sparse_mlp_mxfp4": (_i, [_p, _p, _p, _p, _p, _p, _p, _i, _i, _p, _i, _f, _p, _p, _p, _p, _p, _sz,
+                                         _u32, _p, _p]),
+    "si_norm_residual": (_i, [_p, _i, _sz, _p, _i, _sz, _p, _p, _i, _f, _p, _sz, _p, _p, _i, _sz, _i, _i, _f, _p]),
 }
 
 _lib = None

@@ -1,68 +1,11 @@
 // C ABI of libsparseinfer: argument validation, Eq. (2) threshold, launches.
 #include <atomic>
-#include <cmath>
-#include <cstdarg>
-#include <cstdint>
-#include <cstdio>
 
-#include "../../include/sparseinfer.h"
-#include "si_device.h"
-#include "si_launch.h"
+#include "api_common.h"
 
 namespace {
 
-thread_local char g_err[512] = "";
-
-int32_t threshold(float alpha, int d);
-
-// Rows with N_neg < T - margin count as surely active: their W_up and
-// W_down^T requests go out with the W_gate row, before the gate result.
-// Products of the signs are symmetric (Section IV-A), so a row whose signs
-// agree with the token's on at least half of the elements (the rows Eq. (2)
-// keeps at alpha = 1: N_neg < T(1)) is more likely positive than not, and a
-// row kept only because alpha > 1 is more likely zero: those wait for their
-// gate value, so a larger alpha never adds speculative reads.  With 2-4
-// tokens the kept rows of one token are confident only d/16 below that (a
-// row kept by a fresh token sits near N_neg = d/2); with 5-8 tokens the union
-// of the tokens' kept sets is nearly every row and nearly every one is active
-// for some token, so every kept row is treated as confident.
-int confident_margin(int d, int b, int T) {
-  if (b > 4) return 0;
-  const int T1 = threshold(1.0f, d);
-  return (T > T1 ? T - T1 : 0) + (b == 1 ? 0 : d / 16);
-}
-
-si_status fail(si_status s, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof g_err, fmt, ap);
-  va_end(ap);
-  return s;
-}
-
-si_status hip_status(hipError_t e, const char* what) {
-  if (e == hipSuccess) return SI_OK;
-  return fail(SI_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-#define REQUIRE_PTR(p) \
-  if (!(p)) return fail(SI_ERR_NULL, "%s is NULL", #p)
-#define REQUIRE_ALIGNED(p) \
-  if ((p) && !aligned16(p)) return fail(SI_ERR_ALIGN, "%s is not 16-byte aligned", #p)
-
-si_status check_kd(int k, int d) {
-  if (k < 1 || k > (1 << 24)) return fail(SI_ERR_SHAPE, "k=%d outside [1, 2^24]", k);
-  if (d < 128 || d > si::kMaxD || d % 128 != 0)
-    return fail(SI_ERR_SHAPE, "d=%d must be a multiple of 128 in [128, %d]", d, si::kMaxD);
-  return SI_OK;
-}
-
-si_status check_b(int b) {
-  if (b < 1 || b > si::kMaxB) return fail(SI_ERR_SHAPE, "b=%d outside [1, %d]", b, si::kMaxB);
-  return SI_OK;
-}
+using namespace si;
 
 si_status check_ws(const void* ws, size_t bytes, int k, int b) {
   REQUIRE_PTR(ws);
@@ -88,6 +31,23 @@ int32_t threshold(float alpha, int d) {
 }
 
 }  // namespace
+
+// Rows with N_neg < T - margin count as surely active: their W_up and
+// W_down^T requests go out with the W_gate row, before the gate result.
+// Products of the signs are symmetric (Section IV-A), so a row whose signs
+// agree with the token's on at least half of the elements (the rows Eq. (2)
+// keeps at alpha = 1: N_neg < T(1)) is more likely positive than not, and a
+// row kept only because alpha > 1 is more likely zero: those wait for their
+// gate value, so a larger alpha never adds speculative reads.  With 2-4
+// tokens the kept rows of one token are confident only d/16 below that (a
+// row kept by a fresh token sits near N_neg = d/2); with 5-8 tokens the union
+// of the tokens' kept sets is nearly every row and nearly every one is active
+// for some token, so every kept row is treated as confident.
+int si::confident_margin(int d, int b, int T) {
+  if (b > 4) return 0;
+  const int T1 = threshold(1.0f, d);
+  return (T > T1 ? T - T1 : 0) + (b == 1 ? 0 : d / 16);
+}
 
 extern "C" {
 
