@@ -2,6 +2,7 @@
 // validation and launches.
 #include "api_common.h"
 #include "mx.h"
+#include "mx_launch.h"
 
 namespace {
 

@@ -20,6 +20,7 @@
 //    n is split over blocks as well and k_mx_join adds the parts in order.
 #include "layer_common.h"
 #include "mx.h"
+#include "mx_launch.h"
 
 namespace si {
 

@@ -16,7 +16,7 @@
 // takes kUnits such pieces, a block's width apart, so that all its requests are
 // in flight together.
 #include "mx.h"
-#include "si_launch.h"
+#include "mx_launch.h"
 
 namespace si {
 

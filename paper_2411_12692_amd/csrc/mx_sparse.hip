@@ -18,15 +18,19 @@
 //
 // Bound at one token by two launches' latency chains (signs, gate/up; h3, down,
 // fold, sum), not by the bytes.
-#include "mx.h"
 #include "layer_common.h"
+#include "mx.h"
+#include "mx_launch.h"
 
 namespace si {
 
 constexpr int kMG = 32;      // rows of a block of k_mx_rows
 constexpr int kMW = 8;       // waves of a block
 constexpr int kMT = kMW * kWave;
-static_assert(H_MX_DONE + kMaxD / kTile <= H_WORDS, "a counter for each tile");
+// header words of the workspace that no other call uses: chunks of each tile of y
+// that are done (zero between calls)
+constexpr int kHdrDone = 16;
+static_assert(kHdrDone > H_H3_FORM && kHdrDone + kMaxD / kTile <= H_WORDS, "a counter for each tile");
 constexpr int kDownTarget = 512;  // blocks that k_mx_down aims at
 
 inline __host__ __device__ int mx_groups(int k) { return (k + kMG - 1) / kMG; }
@@ -480,7 +484,7 @@ hipError_t launch_mx_mlp(const MxMlpCall& c, hipStream_t s) {
   a.hdr = reinterpret_cast<uint32_t*>(base);
   a.kmask = reinterpret_cast<uint32_t*>(base + M.kmask);
   a.counts = reinterpret_cast<int32_t*>(base + M.counts);
-  a.done = a.hdr + H_MX_DONE;
+  a.done = a.hdr + kHdrDone;
   a.part = reinterpret_cast<float*>(base + M.part);
   a.h3 = reinterpret_cast<float*>(base + L.h3);
   a.y = c.y;

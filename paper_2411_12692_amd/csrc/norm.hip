@@ -9,7 +9,7 @@
 // h'.  GT threads take a row, U pieces of 8 values each, so a row's requests are
 // all in flight before the first sum.
 #include "mx.h"
-#include "si_launch.h"
+#include "mx_launch.h"
 
 namespace si {
 

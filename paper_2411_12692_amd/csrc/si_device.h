@@ -21,7 +21,6 @@ enum : int {
   H_ERR = 1,          // sticky device-side error bits (read together with H_EPOCH as one 64-bit word)
   H_N_INTERNAL = 2,   // kept-row count when the list lives in the workspace
   H_H3_FORM = 3,      // where the last MLP call left its per-row h3 values (kH3*)
-  H_MX_DONE = 16,     // [16] MXFP4 MLP: chunks of a tile of y that are done (zero between calls)
   H_WORDS = 64
 };
 
