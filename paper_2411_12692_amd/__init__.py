@@ -406,72 +406,97 @@ class Int8MLPLayer:
 
 _DTYPE = {torch.float16: _lib.SI_F16, torch.int16: _lib.SI_F16, torch.bfloat16: _lib.SI_BF16,
           torch.float32: _lib.SI_F32}
-_HALF = (torch.float16, torch.int16, torch.bfloat16)
-_ANY = (*_HALF, torch.float32)
+_HALF = frozenset((torch.float16, torch.int16, torch.bfloat16))
+_ANY = _HALF | {torch.float32}
+_current_device = torch.cuda.current_device
 
 
-def _call_on(device: torch.device, name: str, *args) -> None:
-    """``name(*args, stream)`` on ``device``'s current stream; ``device`` need
-    not be the current one."""
-    if device.index == torch.cuda.current_device():
+# These calls take a few microseconds each, so what is checked on every call is
+# checked in few steps, and what is wrong is named afterwards.
+
+def _call_on(index: int, name: str, *args) -> None:
+    """``name(*args, stream)`` on the current stream of device ``index``, which
+    need not be the current one."""
+    if index == _current_device():
         _lib.call(name, *args, _stream())
     else:
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             _lib.call(name, *args, _stream())
 
 
-def _same_device(*tensors):
-    device = tensors[0].device
+def _same_device(*tensors) -> int:
+    """The index of the device that all of the tensors (None: none) are on."""
+    index = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors on {device} and {t.device}")
-    return device
+        if t is not None and t.get_device() != index:
+            raise ValueError(f"tensors on {tensors[0].device} and {t.device}")
+    return index
 
 
 def _rows(t, name: str, dtypes):
     """A ``[rows][n]`` tensor (or one row ``[n]``) whose rows are contiguous, with
-    any stride between them: returns it with two dims and the stride."""
+    any stride between them: returns ``(rows, n, stride)``."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor (got {t.device})")
     if t.dtype not in dtypes:
-        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
-    if t.dim() == 1:
-        t = t.unsqueeze(0)
-    if t.dim() != 2:
-        raise ValueError(f"{name} must be [rows][n], got {tuple(t.shape)}")
-    rows, n = t.shape
-    if n > 1 and t.stride(1) != 1:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {sorted(map(str, dtypes))}")
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        rows, n = shape
+        ld = stride[0] if rows > 1 else n
+    elif len(shape) == 1:
+        rows, n = 1, shape[0]
+        ld = n
+    else:
+        raise ValueError(f"{name} must be [rows][n], got {tuple(shape)}")
+    if stride[-1] != 1 and n > 1:
         raise ValueError(f"{name} must have contiguous rows")
-    ld = t.stride(0) if rows > 1 else n
     if ld < n:
         raise ValueError(f"{name}'s rows overlap")
-    return t, ld
+    return rows, n, ld
 
 
-def _mx(q, scale, name: str, n: int = None):
-    """Checks MXFP4 rows; ``n`` values long when given."""
+def _mx(q, scale, name: str, n: int = None) -> int:
+    """The number of the MXFP4 rows ``q, scale``; of ``n`` values each when
+    given."""
+    try:
+        rows, width = q.shape
+        if (q.is_cuda and scale.is_cuda and q.dtype is torch.uint8 and scale.dtype is torch.uint8
+                and q.is_contiguous() and scale.is_contiguous() and width & 63 == 0
+                and scale.shape == (rows, width >> 4) and (n is None or width == (n + 127) // 128 * 64)):
+            return rows
+    except (AttributeError, ValueError):
+        pass
     _dev(q, name, (torch.uint8,), 2)
     _dev(scale, f"{name}'s scales", (torch.uint8,), 2)
-    rows, width = q.shape
-    if width % 64 or tuple(scale.shape) != (rows, width // 16):
+    if width & 63 or tuple(scale.shape) != (rows, width // 16):
         raise ValueError(f"{name} {tuple(q.shape)} and its scales {tuple(scale.shape)} are not MXFP4 rows")
-    if n is not None and width != (n + 127) // 128 * 64:
-        raise ValueError(f"{name} has rows of {2 * width} stored values, {n} do not take that many")
-    return rows
+    raise ValueError(f"{name} has rows of {2 * width} stored values, {n} do not take that many")
+
+
+def _floats(t, shape, name: str) -> int:
+    """The address of a contiguous float32 tensor of that shape, or None."""
+    if t is None:
+        return None
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.float32 and t.is_contiguous()
+            and t.shape == shape):
+        return t.data_ptr()
+    _dev(t, name, (torch.float32,))
+    raise ValueError(f"{name} must be {list(shape)}, got {tuple(t.shape)}")
 
 
 def quantize_rows_mxfp4(w: torch.Tensor):
     """Rows ``w [rows][n]`` (fp16, bf16 or float32, any row stride) to MXFP4
     (``si_quantize_rows_mxfp4``): returns the codes, uint8 ``[rows][np / 2]``, and
     scales, uint8 ``[rows][np / 32]``, with ``np`` = ``n`` rounded up to 128."""
-    w, ld = _rows(w, "w", _ANY)
-    rows, n = w.shape
-    np_ = (n + 127) // 128 * 128
-    q = torch.empty(rows, np_ // 2, dtype=torch.uint8, device=w.device)
-    scale = torch.empty(rows, np_ // 32, dtype=torch.uint8, device=w.device)
-    _call_on(w.device, "si_quantize_rows_mxfp4", _vp(w), _DTYPE[w.dtype], ld, rows, n, _vp(q), _vp(scale))
+    rows, n, ld = _rows(w, "w", _ANY)
+    pieces = (n + 127) // 128
+    q = w.new_empty((rows, pieces * 64), dtype=torch.uint8)
+    scale = w.new_empty((rows, pieces * 4), dtype=torch.uint8)
+    _call_on(w.get_device(), "si_quantize_rows_mxfp4", w.data_ptr(), _DTYPE[w.dtype], ld, rows, n, q.data_ptr(),
+             scale.data_ptr())
     return q, scale
 
 
@@ -480,10 +505,10 @@ def dequantize_rows_mxfp4(q: torch.Tensor, scale: torch.Tensor, n: int, dtype=to
     (``si_dequantize_rows_mxfp4``)."""
     rows = _mx(q, scale, "q", n)
     if dtype not in _ANY:
-        raise TypeError(f"dtype {dtype}, expected one of {_ANY}")
-    device = _same_device(q, scale)
-    w = torch.empty(rows, n, dtype=dtype, device=device)
-    _call_on(device, "si_dequantize_rows_mxfp4", _vp(q), _vp(scale), rows, n, _vp(w), _DTYPE[dtype])
+        raise TypeError(f"dtype {dtype}, expected one of {sorted(map(str, _ANY))}")
+    w = q.new_empty((rows, n), dtype=dtype)
+    _call_on(_same_device(q, scale), "si_dequantize_rows_mxfp4", q.data_ptr(), scale.data_ptr(), rows, n, w.data_ptr(),
+             _DTYPE[dtype])
     return w
 
 
@@ -495,28 +520,29 @@ def pack_signs_mxfp4(q_gate: torch.Tensor) -> torch.Tensor:
     if nbytes == 0:
         raise ValueError(f"unsupported shape k={k} d={d}")
     out = torch.empty(nbytes // 4, dtype=torch.int32, device=q_gate.device)
-    _call_on(q_gate.device, "si_pack_signs_mxfp4", _vp(q_gate), k, d, _vp(out))
+    _call_on(q_gate.get_device(), "si_pack_signs_mxfp4", _vp(q_gate), k, d, _vp(out))
     return out
 
 
-def _product(name, x_args, x_ptr, ldx, m, n, weights, out_dtype, device):
+def _product(name, x, x_args, ldx, m, n, weights, out_dtype, *more):
     """One of the four products; ``weights`` is ``q, scale`` or ``q_gate,
-    s_gate, q_up, s_up``.  Scratch comes from torch's allocator, in the stream's
-    order like any tensor."""
+    s_gate, q_up, s_up``, ``more`` further tensors that have to be on ``x``'s
+    device.  Scratch comes from torch's allocator, in the stream's order like any
+    tensor."""
     gated = len(weights) == 4
-    rows = _mx(weights[0], weights[1], "q" if not gated else "q_gate", n)
-    if gated and weights[2] is not None and _mx(weights[2], weights[3], "q_up", n) != rows:
+    rows = _mx(weights[0], weights[1], "q_gate" if gated else "q", n)
+    up = gated and weights[2] is not None
+    if up and _mx(weights[2], weights[3], "q_up", n) != rows:
         raise ValueError("q_up does not match q_gate")
     if out_dtype not in _ANY:
-        raise TypeError(f"out_dtype {out_dtype}, expected one of {_ANY}")
-    _same_device(*(t for t in weights if t is not None))
-    if weights[0].device != device:
-        raise ValueError(f"activations on {device}, weights on {weights[0].device}")
-    y = torch.empty(m, rows, dtype=out_dtype, device=device)
-    nbytes = _lib.load().si_linear_mxfp4_workspace_bytes(x_ptr, ldx, m, rows, n,
-                                                         1 if gated and weights[2] is not None else 0)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-    _call_on(device, name, *x_args, m, n, *(_vp(t) for t in weights), rows, _vp(y), _DTYPE[out_dtype], _vp(ws), nbytes)
+        raise TypeError(f"out_dtype {out_dtype}, expected one of {sorted(map(str, _ANY))}")
+    index = _same_device(x, *weights, *more)
+    y = x.new_empty((m, rows), dtype=out_dtype)
+    half = x_args[0] if len(x_args) == 3 else None
+    nbytes = (_lib._lib or _lib.load()).si_linear_mxfp4_workspace_bytes(half, ldx, m, rows, n, up)
+    ws = x.new_empty((nbytes,), dtype=torch.uint8).data_ptr() if nbytes else None
+    _call_on(index, name, *x_args, m, n, *(None if t is None else t.data_ptr() for t in weights), rows, y.data_ptr(),
+             _DTYPE[out_dtype], ws, nbytes)
     return y
 
 
@@ -524,19 +550,17 @@ def linear_mxfp4(x: torch.Tensor, q: torch.Tensor, scale: torch.Tensor, out_dtyp
     """``x W^T`` with MXFP4 weights ``q, scale`` of ``[rows][n]``
     (``si_linear_mxfp4``); ``x [m][n]`` fp16 or bf16, any row stride.  Returns
     ``[m][rows]`` in ``out_dtype`` (``x``'s type)."""
-    x, ld = _rows(x, "x", _HALF)
-    m, n = x.shape
-    return _product("si_linear_mxfp4", (_vp(x), _DTYPE[x.dtype], ld), _vp(x), ld, m, n, (q, scale),
-                    out_dtype or x.dtype, x.device)
+    m, n, ld = _rows(x, "x", _HALF)
+    return _product("si_linear_mxfp4", x, (x.data_ptr(), _DTYPE[x.dtype], ld), ld, m, n, (q, scale),
+                    out_dtype or x.dtype)
 
 
 def gated_linear_mxfp4(x: torch.Tensor, q_gate, s_gate, q_up=None, s_up=None, out_dtype=None) -> torch.Tensor:
     """``ReLU(x W_gate^T) * (x W_up^T)`` over every row, Eq. (1) steps 1-3 of a
     prompt (``si_gated_linear_mxfp4``); ``q_up=None``: ``ReLU(x W_fc1^T)``."""
-    x, ld = _rows(x, "x", _HALF)
-    m, n = x.shape
-    return _product("si_gated_linear_mxfp4", (_vp(x), _DTYPE[x.dtype], ld), _vp(x), ld, m, n,
-                    (q_gate, s_gate, q_up, s_up), out_dtype or x.dtype, x.device)
+    m, n, ld = _rows(x, "x", _HALF)
+    return _product("si_gated_linear_mxfp4", x, (x.data_ptr(), _DTYPE[x.dtype], ld), ld, m, n,
+                    (q_gate, s_gate, q_up, s_up), out_dtype or x.dtype)
 
 
 def linear_mxfp4_a4(xq: torch.Tensor, x_scale: torch.Tensor, q: torch.Tensor, scale: torch.Tensor,
@@ -544,18 +568,16 @@ def linear_mxfp4_a4(xq: torch.Tensor, x_scale: torch.Tensor, q: torch.Tensor, sc
     """``linear_mxfp4`` with the activations in MXFP4 too
     (``quantize_rows_mxfp4``), on the 4-bit matrix instructions."""
     m = _mx(xq, x_scale, "xq")
-    n = 2 * xq.shape[1]
-    return _product("si_linear_mxfp4_a4", (_vp(xq), _vp(x_scale)), None, 0, m, n, (q, scale), out_dtype,
-                    _same_device(xq, x_scale))
+    return _product("si_linear_mxfp4_a4", xq, (xq.data_ptr(), x_scale.data_ptr()), 0, m, 2 * xq.shape[1], (q, scale),
+                    out_dtype, x_scale)
 
 
 def gated_linear_mxfp4_a4(xq: torch.Tensor, x_scale: torch.Tensor, q_gate, s_gate, q_up=None, s_up=None,
                           out_dtype=torch.float16) -> torch.Tensor:
     """``gated_linear_mxfp4`` with the activations in MXFP4 too."""
     m = _mx(xq, x_scale, "xq")
-    n = 2 * xq.shape[1]
-    return _product("si_gated_linear_mxfp4_a4", (_vp(xq), _vp(x_scale)), None, 0, m, n,
-                    (q_gate, s_gate, q_up, s_up), out_dtype, _same_device(xq, x_scale))
+    return _product("si_gated_linear_mxfp4_a4", xq, (xq.data_ptr(), x_scale.data_ptr()), 0, m, 2 * xq.shape[1],
+                    (q_gate, s_gate, q_up, s_up), out_dtype, x_scale)
 
 
 def mxfp4_workspace_bytes(k: int, d: int, b: int = 1) -> int:
@@ -570,25 +592,25 @@ def new_workspace_mxfp4(k: int, d: int, b: int = 1, device=None) -> torch.Tensor
     return torch.zeros(n, dtype=torch.uint8, device=device or "cuda")
 
 
-def _mx_mlp_weights(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x):
+def _mx_mlp(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, y, workspace, *more):
+    """Checks of the two MXFP4 MLP calls: returns ``(k, d, b, device index,
+    y)`` and the addresses of the weights."""
     k = _mx(q_gate, s_gate, "q_gate")
     d = 2 * q_gate.shape[1]
     if q_up is not None and _mx(q_up, s_up, "q_up", d) != k:
         raise ValueError("q_up does not match q_gate")
     if _mx(q_down_t, s_down_t, "q_down_t", d) != k:
         raise ValueError("q_down_t does not match q_gate")
-    x = _x2(x, d)
-    _same_device(x, q_gate, s_gate, q_up, s_up, q_down_t, s_down_t)
-    return k, d, x, x.shape[0]
-
-
-def _out_y(y, b, d, x):
+    b = _x2(x, d).shape[0]
     if y is None:
-        return torch.empty(b, d, dtype=torch.float32, device=x.device)
-    _dev(y, "y", (torch.float32,))
-    if y.numel() != b * d:
-        raise ValueError(f"y must hold [{b}][{d}] floats")
-    return y
+        y = x.new_empty((b, d), dtype=torch.float32)
+    else:
+        _dev(y, "y", (torch.float32,))
+        if y.numel() != b * d:
+            raise ValueError(f"y must hold [{b}][{d}] floats")
+    index = _same_device(x, q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, y, workspace, *more)
+    up = (None, None) if q_up is None else (q_up.data_ptr(), s_up.data_ptr())
+    return k, d, b, index, y, (q_gate.data_ptr(), s_gate.data_ptr(), *up, q_down_t.data_ptr(), s_down_t.data_ptr())
 
 
 def sparse_mlp_mxfp4(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, workspace, mask, flags: int = 0,
@@ -596,15 +618,13 @@ def sparse_mlp_mxfp4(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, workspac
     """Eq. (1) over the rows kept by ``mask`` with MXFP4 weights
     (``si_sparse_mlp_mxfp4``); ``q_up=None``: the non-gated ReLU MLP.  Returns
     ``y [b][d]`` float32 (and the ``[3]`` work counters with ``counters``)."""
-    k, d, x, b = _mx_mlp_weights(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x)
     _dev(mask, "mask", (torch.uint8,), 1)
+    k, d, b, index, y, weights = _mx_mlp(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, y, workspace, mask)
     if mask.numel() != k:
         raise ValueError(f"mask must hold {k} rows")
-    device = _same_device(x, mask, workspace, y)
-    y = _out_y(y, b, d, x)
-    cnt = torch.empty(3, dtype=torch.int32, device=device) if counters else None
-    _call_on(device, "si_sparse_mlp_mxfp4", _vp(q_gate), _vp(s_gate), _vp(q_up), _vp(s_up), _vp(q_down_t),
-             _vp(s_down_t), k, d, _vp(x), b, _vp(mask), _vp(y), _vp(workspace), workspace.numel(), flags, _vp(cnt))
+    cnt = x.new_empty((3,), dtype=torch.int32) if counters else None
+    _call_on(index, "si_sparse_mlp_mxfp4", *weights, k, d, x.data_ptr(), b, mask.data_ptr(), y.data_ptr(),
+             workspace.data_ptr(), workspace.numel(), flags, _vp(cnt))
     return (y, cnt) if counters else y
 
 
@@ -614,22 +634,20 @@ def predict_sparse_mlp_mxfp4(signs, q_gate, s_gate, q_up, s_up, q_down_t, s_down
     (``si_predict_sparse_mlp_mxfp4``); ``signs`` from ``pack_signs_mxfp4``.
     Returns ``y`` (and ``(mask, active_idx, n_active, counters)`` with
     ``outputs``)."""
-    k, d, x, b = _mx_mlp_weights(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x)
     _dev(signs, "signs", (torch.int32,))
-    if signs.numel() * 4 != signs_bytes(k, d):
+    k, d, b, index, y, weights = _mx_mlp(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, y, workspace, signs)
+    if signs.numel() * 32 != (k + 63) // 64 * 64 * d:
         raise ValueError(f"signs do not belong to [{k}][{d}]")
-    device = _same_device(x, signs, workspace, y)
-    y = _out_y(y, b, d, x)
     if outputs:
-        mask = torch.empty(k, dtype=torch.uint8, device=device)
-        idx = torch.empty(k, dtype=torch.int32, device=device)
-        n = torch.empty(1, dtype=torch.int32, device=device)
-        cnt = torch.empty(3, dtype=torch.int32, device=device)
+        mask = x.new_empty((k,), dtype=torch.uint8)
+        idx = x.new_empty((k,), dtype=torch.int32)
+        n = x.new_empty((1,), dtype=torch.int32)
+        cnt = x.new_empty((3,), dtype=torch.int32)
+        out = (mask.data_ptr(), idx.data_ptr(), n.data_ptr())
     else:
-        mask = idx = n = cnt = None
-    _call_on(device, "si_predict_sparse_mlp_mxfp4", _vp(signs), _vp(q_gate), _vp(s_gate), _vp(q_up), _vp(s_up),
-             _vp(q_down_t), _vp(s_down_t), k, d, _vp(x), b, float(alpha), _vp(mask), _vp(idx), _vp(n), _vp(y),
-             _vp(workspace), workspace.numel(), flags, _vp(cnt))
+        out, cnt = (None, None, None), None
+    _call_on(index, "si_predict_sparse_mlp_mxfp4", signs.data_ptr(), *weights, k, d, x.data_ptr(), b, float(alpha), *out,
+             y.data_ptr(), workspace.data_ptr(), workspace.numel(), flags, _vp(cnt))
     return (y, (mask, idx, n, cnt)) if outputs else y
 
 
@@ -648,47 +666,43 @@ def norm_residual(h: torch.Tensor, branch: torch.Tensor = None, post_w: torch.Te
     ``[d]``.  Returns ``(h', x)``: ``h'`` in ``h``'s type (in ``out`` when given,
     which may be ``h``; None without a branch), ``x`` in ``x_dtype`` (None without
     ``pre_w``)."""
-    shape = h.shape if isinstance(h, torch.Tensor) else None
-    h2, ldh = _rows(h, "h", _ANY)
-    tokens, d = h2.shape
+    tokens, d, ldh = _rows(h, "h", _ANY)
     if x_dtype not in _ANY:
-        raise TypeError(f"x_dtype {x_dtype}, expected one of {_ANY}")
-    b2, ldb = h2, 0
+        raise TypeError(f"x_dtype {x_dtype}, expected one of {sorted(map(str, _ANY))}")
+    index = _same_device(h, branch, post_w, gate, pre_w, out)
+    hp, ht = h.data_ptr(), _DTYPE[h.dtype]
+    bp, bt, ldb, op, ldo, gp, per = None, ht, 0, None, 0, None, 1
     if branch is not None:
-        b2, ldb = _rows(branch, "branch", _ANY)
-        if b2.shape != h2.shape:
-            raise ValueError(f"branch {tuple(b2.shape)} does not match h {tuple(h2.shape)}")
+        bt_, bd, ldb = _rows(branch, "branch", _ANY)
+        if bt_ != tokens or bd != d:
+            raise ValueError(f"branch {tuple(branch.shape)} does not match h {tuple(h.shape)}")
+        bp, bt = branch.data_ptr(), _DTYPE[branch.dtype]
+        if out is None:
+            out = torch.empty_like(h, memory_format=torch.contiguous_format)
+            ldo = d
+        else:
+            ot, od, ldo = _rows(out, "out", (h.dtype,))
+            if ot != tokens or od != d:
+                raise ValueError(f"out {tuple(out.shape)} does not match h {tuple(h.shape)}")
+        op = out.data_ptr()
+        if gate is not None:
+            g = gate.shape[0] if gate.dim() == 2 else 1
+            gp = _floats(gate, (g, d) if gate.dim() == 2 else (d,), "gate")
+            if g < 1 or tokens % g:
+                raise ValueError(f"gate has {g} rows, which do not divide {tokens} tokens")
+            per = max(tokens // g, 1)
     elif post_w is not None or gate is not None or out is not None:
         raise ValueError("post_w, gate and out need a branch")
     elif pre_w is None:
         raise ValueError("nothing to compute: neither branch nor pre_w")
-    for t, name in ((post_w, "post_w"), (pre_w, "pre_w")):
-        if t is not None:
-            _dev(t, name, (torch.float32,), 1)
-            if t.numel() != d:
-                raise ValueError(f"{name} must hold {d} values")
-    per = 1
-    if gate is not None:
-        _dev(gate, "gate", (torch.float32,))
-        g2 = gate.view(1, -1) if gate.dim() == 1 else gate
-        if g2.dim() != 2 or g2.shape[1] != d or g2.shape[0] < 1 or tokens % g2.shape[0]:
-            raise ValueError(f"gate must be [{d}] or [g][{d}] with g dividing {tokens} tokens, got {tuple(gate.shape)}")
-        per = max(tokens // g2.shape[0], 1)
-    h_out = x = None
-    ldo = 0
-    if branch is not None:
-        if out is None:
-            out = torch.empty(shape, dtype=h.dtype, device=h.device)
-        h_out, ldo = _rows(out, "out", (h.dtype,))
-        if h_out.shape != h2.shape:
-            raise ValueError(f"out {tuple(out.shape)} does not match h {tuple(h.shape)}")
-    if pre_w is not None:
-        x = torch.empty(shape, dtype=x_dtype, device=h.device)
-    device = _same_device(h2, b2, post_w, gate, pre_w, h_out)
-    _call_on(device, "si_norm_residual", _vp(h2), _DTYPE[h2.dtype], ldh, _vp(b2) if branch is not None else None,
-             _DTYPE[b2.dtype], ldb, _vp(post_w), _vp(gate), per, float(scale), _vp(h_out), ldo, _vp(pre_w), _vp(x),
-             _DTYPE[x_dtype], d, tokens, d, float(eps))
-    return out if branch is not None else None, x
+    x = xp = None
+    wp = _floats(pre_w, (d,), "pre_w")
+    if wp is not None:
+        x = torch.empty_like(h, dtype=x_dtype, memory_format=torch.contiguous_format)
+        xp = x.data_ptr()
+    _call_on(index, "si_norm_residual", hp, ht, ldh, bp, bt, ldb, _floats(post_w, (d,), "post_w"), gp, per, float(scale), op,
+             ldo, wp, xp, _DTYPE[x_dtype], d, tokens, d, float(eps))
+    return out, x
 
 
 def _block(layer, h, norm_w, eps, alpha, flags, outputs, y, post_norm_w, gate, scale):

@@ -13,11 +13,16 @@
 //  * MXFP4 activations: one K = 128 instruction takes both codes and both scales.
 //
 // Two shapes of kernel:
-//  * k_mx_skinny, up to 16 tokens, bound by the bytes of W: a block owns 16 rows,
-//    its waves split n and every wave streams straight into registers.
-//  * k_mx_tile: tiles of W and x pass through LDS, double-buffered, written there
-//    by the loads themselves.  Where the tiles are fewer than the compute units,
-//    n is split over blocks as well and k_mx_join adds the parts in order.
+//  * k_mx_tile: tiles of W and x pass through LDS in stages of 128 to 1024 values,
+//    written there by the loads themselves, the next one or two in flight while
+//    one is used.  Where a stage has little work for its waves they form groups
+//    that each take a part of its values.  With few tiles and a long n, n is split
+//    over blocks as well and k_mx_join adds the parts in order.
+//  * k_mx_skinny, a few tokens and few rows: a block owns 16 rows, its waves split
+//    n and stream the codes straight into registers; the tokens pass through LDS.
+#include <algorithm>
+#include <type_traits>
+
 #include "layer_common.h"
 #include "mx.h"
 #include "mx_launch.h"
@@ -58,22 +63,33 @@ __device__ inline f32x4 mfma_mx(u32x4 a, u32x4 b, f32x4 c, uint32_t sa, uint32_t
 // max(g, 0) where a NaN stays one
 __device__ inline float relu(float g) { return g > 0.f || g != g ? g : 0.f; }
 
-// ---- up to 16 tokens ---------------------------------------------------------
+// ---- a few tokens and few rows ---------------------------------------------------
 
-constexpr int kSW = 8;       // waves of a block: each takes every 8th step
-constexpr int kSAhead = 4;   // steps of a wave in flight
+constexpr int kSW = 16;        // waves of a block: each takes every 16th step
+constexpr int kSAhead = 3;     // steps of a wave whose codes are in flight
+constexpr int kSLds = 72 * 1024;  // tokens of a block in LDS (two blocks a compute unit)
+constexpr int kSToks = 4;      // tokens
+
+// Steps of x that are in LDS at once (fp16 and bf16 activations).
+inline __host__ __device__ int skinny_chunk(int m) {
+  const int c = (kSLds / m - 16) / 256;
+  return c < kSW * kSAhead ? c : kSW * kSAhead;
+}
 
 template <int ACT, int MATS>
 __global__ __launch_bounds__(kSW * kWave) void k_mx_skinny(LinArgs a) {
-  constexpr int XV = ACT == kActMx ? 1 : 4;  // 16-byte pieces of x a lane and step
   __shared__ f32x4 red[kSW][MATS][kWave];
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  extern __shared__ __attribute__((aligned(16))) uint8_t xl[];  // [m][chunk * 256 + 16]
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int row0 = blockIdx.x * 16;
   const size_t pitch_q = (size_t)a.steps * 64, pitch_s = (size_t)a.steps * 4;
   const int row = min(row0 + r, a.rows - 1), tok = min(r, a.m - 1);
-  const uint8_t* xp = static_cast<const uint8_t*>(a.x) + (size_t)tok * a.ldx + g * (ACT == kActMx ? 16 : 64);
-  const uint8_t* xsp = ACT == kActMx ? a.xs + (size_t)tok * pitch_s + g : nullptr;
+  const int chunk = ACT == kActMx ? kSW * kSAhead : min(skinny_chunk(a.m), a.steps);
+  const int pitch_x = chunk * 256 + 16;  // 16 more, so that the tokens' pieces lie in different banks
+  const uint8_t* xq = static_cast<const uint8_t*>(a.x) + (size_t)tok * a.ldx + g * 16;  // MXFP4 activations
+  const uint8_t* xs = ACT == kActMx ? a.xs + (size_t)tok * pitch_s + g : nullptr;
+  const uint8_t* xt = xl + tok * pitch_x + g * 64;
   const uint8_t* qp[MATS];
   const uint8_t* sp[MATS];
   f32x4 acc[MATS];
@@ -83,34 +99,54 @@ __global__ __launch_bounds__(kSW * kWave) void k_mx_skinny(LinArgs a) {
     sp[w] = a.s[w] + (size_t)row * pitch_s + g;
     acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  for (int k0 = wv; k0 < a.steps; k0 += kSW * kSAhead) {
-    u32x4 c[kSAhead][MATS], x[kSAhead][XV];
+  for (int k0 = 0; k0 < a.steps; k0 += chunk) {
+    const int k1 = min(k0 + chunk, a.steps);
+    u32x4 c[kSAhead][MATS], x[kSAhead];
     uint32_t sc[kSAhead][MATS], sx[kSAhead];
 #pragma unroll
     for (int i = 0; i < kSAhead; ++i) {
-      const int k = min(k0 + kSW * i, a.steps - 1);
+      const int k = k0 + wv + kSW * i;
+      if (k < k1) {
 #pragma unroll
-      for (int w = 0; w < MATS; ++w) {
-        c[i][w] = load_nt(reinterpret_cast<const u32x4*>(qp[w] + (size_t)k * 64));
-        sc[i][w] = sp[w][k * 4];
+        for (int w = 0; w < MATS; ++w) {
+          c[i][w] = *reinterpret_cast<const u32x4*>(qp[w] + (size_t)k * 64);
+          sc[i][w] = sp[w][k * 4];
+        }
+        if constexpr (ACT == kActMx) {
+          x[i] = *reinterpret_cast<const u32x4*>(xq + (size_t)k * 64);
+          sx[i] = xs[k * 4];
+        }
       }
-#pragma unroll
-      for (int j = 0; j < XV; ++j)
-        x[i][j] = *reinterpret_cast<const u32x4*>(xp + (size_t)k * (ACT == kActMx ? 64 : 256) + j * 16);
-      sx[i] = ACT == kActMx ? xsp[k * 4] : 0u;
+    }
+    if constexpr (ACT != kActMx) {
+      // the tokens' values of these steps, read once for the block's 16 rows
+      const int per = (k1 - k0) * 16;  // 16-byte pieces a token
+      const uint8_t* src = static_cast<const uint8_t*>(a.x) + (size_t)k0 * 256;
+      if (k0 > 0) __syncthreads();
+      for (int t = 0; t < a.m; ++t)
+        for (int i = tid; i < per; i += kSW * kWave)
+          *reinterpret_cast<u32x4*>(xl + t * pitch_x + i * 16) =
+              *reinterpret_cast<const u32x4*>(src + (size_t)t * a.ldx + (size_t)i * 16);
+      __syncthreads();
     }
 #pragma unroll
     for (int i = 0; i < kSAhead; ++i) {
-      if (k0 + kSW * i < a.steps) {
+      const int k = k0 + wv + kSW * i;
+      if (k < k1) {
+        u32x4 v[4];
+        if constexpr (ACT != kActMx) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const u32x4*>(xt + (k - k0) * 256 + j * 16);
+        }
 #pragma unroll
         for (int w = 0; w < MATS; ++w) {
           if constexpr (ACT == kActMx) {
-            acc[w] = mfma_mx<0, 0>(c[i][w], x[i][0], acc[w], sc[i][w], sx[i]);
+            acc[w] = mfma_mx<0, 0>(c[i][w], x[i], acc[w], sc[i][w], sx[i]);
           } else {
             const float s = mx_scale(sc[i][w]);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              acc[w] = mfma_half(ACT == kActBF16, mx_half8<ACT == kActBF16>(c[i][w][j], s), x[i][j], acc[w]);
+              acc[w] = mfma_half(ACT == kActBF16, mx_half8<ACT == kActBF16>(c[i][w][j], s), v[j], acc[w]);
           }
         }
       }
@@ -136,23 +172,42 @@ __global__ __launch_bounds__(kSW * kWave) void k_mx_skinny(LinArgs a) {
 
 // ---- tiles ---------------------------------------------------------------------
 
-// A tile: BR rows of W (BR / MATS of each matrix) by BT tokens, WR x WT waves, KB
-// steps of 128 values a stage.
-template <int ACT, int MATS, int BR, int BT, int WR, int WT>
+// A tile: BR rows of W (BR / MATS of each matrix) by BT tokens, WR x WT waves of
+// its own part of each, WK groups of such waves that share out a stage's steps
+// (KB each, of 128 values), ST stages in LDS.
+template <int ACT, int MATS, int BR, int BT, int WR, int WT, int WK, int ST>
 struct Tile {
-  static constexpr int NW = WR * WT;
+  static constexpr int NW = WR * WT * WK;
   static constexpr int KB = ACT == kActMx ? 2 : 1;
+  static constexpr int SK = KB * WK;  // steps of a stage
   static constexpr int R = BR / WR / 16, T = BT / WT / 16;  // 16-row and 16-token pieces of a wave
-  static constexpr int WRow = 64 * KB;                      // bytes of a row's codes in a stage
-  static constexpr int XRow = ACT == kActMx ? 64 * KB : 256;
-  static constexpr int SRow = 4 * KB;                       // bytes of a row's scales
+  static constexpr int WRow = 64 * SK;                      // bytes of a row's codes in a stage
+  static constexpr int XRow = ACT == kActMx ? 64 * SK : 256 * SK;
+  static constexpr int SRow = 4 * SK;                       // bytes of a row's scales
   static constexpr int WBytes = BR * WRow, XBytes = BT * XRow;
   static constexpr int WsBytes = BR * SRow, XsBytes = ACT == kActMx ? BT * SRow : 0;
   static constexpr int Bytes = WBytes + XBytes + WsBytes + XsBytes;
   // wave requests of a stage: 1 KB of codes or activations, 256 bytes of scales
   static constexpr int IW = WBytes / 1024, IX = XBytes / 1024, IWs = WsBytes / 256, IXs = XsBytes / 256;
+  static constexpr int NS = IWs + IXs, MS = (NS + NW - 1) / NW;
+  // requests of a wave and stage, the same for every wave: the waits count them
+  static constexpr int Requests = IW / NW + IX / NW + MS;
+  static_assert(WRow <= 1024 && XRow <= 1024 && SK <= 64, "a request covers whole rows");
   static_assert(R % MATS == 0 && IW % NW == 0 && IX % NW == 0, "whole requests a wave");
+  static_assert(Requests * (ST - 2) < 64, "what a wait can leave outstanding");
+  static_assert(ST * Bytes <= kMaxLds, "LDS of a compute unit");
+  static_assert((WK - 1) * BR * BT * 4 <= ST * Bytes, "the groups' sums");
 };
+
+// Wait until at most N of the wave's vector memory requests and none of its LDS
+// reads are outstanding, then for the other waves.
+template <int N>
+__device__ inline void wait_stage() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | 0x0070 | ((N >> 4) << 14));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef const __attribute__((address_space(1))) uint8_t glb_u8;
@@ -169,10 +224,10 @@ __device__ inline int swizzle(int r, int p) {
     return p ^ (r & 15);
 }
 
-template <int ACT, int MATS, int BR, int BT, int WR, int WT>
-__global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
-  using P = Tile<ACT, MATS, BR, BT, WR, WT>;
-  constexpr int NW = P::NW, R = P::R, T = P::T, KB = P::KB;
+template <int ACT, int MATS, int BR, int BT, int WR, int WT, int WK, int ST>
+__global__ __launch_bounds__(WR* WT* WK* kWave) void k_mx_tile(LinArgs a) {
+  using P = Tile<ACT, MATS, BR, BT, WR, WT, WK, ST>;
+  constexpr int NW = P::NW, R = P::R, T = P::T, SK = P::SK;
   extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
   const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
   // XCD-aware order: blocks go to the XCDs in turn, so every XCD gets a run of
@@ -185,7 +240,7 @@ __global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
   const int gw = min(8, a.tok_tiles - grp * 8);
   const int tok0 = (grp * 8 + in % gw) * BT, row0 = (in / gw) * (BR / MATS);
   // the stages of this part of n
-  const int stages_all = a.steps / KB;
+  const int stages_all = a.steps / SK;
   const int k_first = (int)((long long)stages_all * part / a.split);
   const int k_last = (int)((long long)stages_all * (part + 1) / a.split);
 
@@ -209,19 +264,18 @@ __global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
     ox[i] = (uint32_t)rr * (uint32_t)a.ldx + 16 * swizzle<P::XRow>(r, lane % (64 / LX));
   }
   const uint8_t* bx = static_cast<const uint8_t*>(a.x) + (size_t)tok0 * a.ldx;
-  constexpr int NS = P::IWs + P::IXs;          // scale requests of a stage
-  constexpr int MS = (NS + NW - 1) / NW;
+  constexpr int NS = P::NS, MS = P::MS;  // scale requests of a stage; waves without one repeat another's
   uint32_t os[MS];
   const uint8_t* bs[MS];
 #pragma unroll
   for (int i = 0; i < MS; ++i) {
-    const int q = wv + NW * i;
+    const int q = (wv + NW * i) % NS;
     const bool of_x = q >= P::IWs;
-    const int r = (of_x ? q - P::IWs : q) * (64 / KB) + lane / KB;  // one 4-byte word a lane
+    const int r = (of_x ? q - P::IWs : q) * (64 / SK) + lane / SK;  // one 4-byte word a lane
     const int base = of_x ? tok0 : row0, last = (of_x ? a.m : a.rows) - 1;
     const int per = of_x ? BT : BR / MATS;
     const int rr = min(base + r % per, last) - base;
-    os[i] = (uint32_t)(rr * (int)pitch_s) + 4 * (lane % KB);
+    os[i] = (uint32_t)(rr * (int)pitch_s) + 4 * (lane % SK);
     const uint8_t* sc = a.s[0];  // a request of the small tile spans both matrices
     if (MATS == 2 && r >= BR / MATS) sc = a.s[1];
     bs[i] = (of_x ? a.xs : sc) + (size_t)base * pitch_s;
@@ -238,12 +292,11 @@ __global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
                                        (lds_u8*)(to + P::WBytes + (wv + NW * i) * 1024), 16, 0, 0);
 #pragma unroll
     for (int i = 0; i < MS; ++i)
-      if (wv + NW * i < NS)
-        __builtin_amdgcn_global_load_lds((glb_u8*)(bs[i] + (size_t)k * P::SRow + os[i]),
-                                         (lds_u8*)(to + P::WBytes + P::XBytes + (wv + NW * i) * 256), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((glb_u8*)(bs[i] + (size_t)k * P::SRow + os[i]),
+                                       (lds_u8*)(to + P::WBytes + P::XBytes + (wv + NW * i) % NS * 256), 4, 0, 0);
   };
 
-  const int wr = wv / WT, wt = wv % WT;
+  const int wk = wv / (WR * WT), wr = wv / WT % WR, wt = wv % WT;
   const int r = lane & 15, g = lane >> 4;
   f32x4 acc[R][T];
 #pragma unroll
@@ -267,22 +320,23 @@ __global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
       uint32_t sw[R], sx[T];
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        sw[i] = *reinterpret_cast<const uint16_t*>(sl + (piece_row(i) + r) * P::SRow + 2 * g);
+        sw[i] = *reinterpret_cast<const uint16_t*>(sl + (piece_row(i) + r) * P::SRow + 8 * wk + 2 * g);
 #pragma unroll
       for (int t = 0; t < T; ++t)
-        sx[t] = *reinterpret_cast<const uint16_t*>(sl + P::WsBytes + (wt * (BT / WT) + t * 16 + r) * P::SRow + 2 * g);
-      // step s: lane group g takes block 2 g + s of the stage's 8
+        sx[t] = *reinterpret_cast<const uint16_t*>(sl + P::WsBytes + (wt * (BT / WT) + t * 16 + r) * P::SRow +
+                                                 8 * wk + 2 * g);
+      // step s: lane group g takes block 2 g + s of the wave's 8
       u32x4 w[R], x[T];
       auto read = [&](int s) {
 #pragma unroll
         for (int t = 0; t < T; ++t) {
           const int row = wt * (BT / WT) + t * 16 + r;
-          x[t] = *reinterpret_cast<const u32x4*>(xl + row * P::XRow + 16 * swizzle<P::XRow>(row, 2 * g + s));
+          x[t] = *reinterpret_cast<const u32x4*>(xl + row * P::XRow + 16 * swizzle<P::XRow>(row, 8 * wk + 2 * g + s));
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
           const int row = piece_row(i) + r;
-          w[i] = *reinterpret_cast<const u32x4*>(wl + row * P::WRow + 16 * swizzle<P::WRow>(row, 2 * g + s));
+          w[i] = *reinterpret_cast<const u32x4*>(wl + row * P::WRow + 16 * swizzle<P::WRow>(row, 8 * wk + 2 * g + s));
         }
       };
       read(0);
@@ -301,8 +355,8 @@ __global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         const int row = piece_row(i) + r;
-        w[i] = *reinterpret_cast<const u32x4*>(wl + row * P::WRow + 16 * swizzle<P::WRow>(row, g));
-        sw[i] = mx_scale(sl[row * P::SRow + g]);
+        w[i] = *reinterpret_cast<const u32x4*>(wl + row * P::WRow + 16 * swizzle<P::WRow>(row, 4 * wk + g));
+        sw[i] = mx_scale(sl[row * P::SRow + 4 * wk + g]);
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -310,7 +364,7 @@ __global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
 #pragma unroll
         for (int t = 0; t < T; ++t) {
           const int row = wt * (BT / WT) + t * 16 + r;
-          x[t] = *reinterpret_cast<const u32x4*>(xl + row * P::XRow + 16 * swizzle<P::XRow>(row, 4 * g + j));
+          x[t] = *reinterpret_cast<const u32x4*>(xl + row * P::XRow + 16 * swizzle<P::XRow>(row, 16 * wk + 4 * g + j));
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -321,74 +375,105 @@ __global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
       }
     }
   };
-  // one stage computed while the next one's requests are in flight; the two
-  // halves of LDS are told apart by the pointers' restrict, without which every
+  // one stage computed while the requests of the next ST - 1 are in flight; the
+  // parts of LDS are told apart by the pointers' restrict, without which every
   // read of LDS would wait for all requests
   auto step = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from, int k, bool more) {
     if (more) request(to, k);
     compute(from);
   };
 
-  if (k_first < k_last) {
-    request(lds, k_first);
-    for (int k = k_first; k < k_last; ++k) {
-      const int cur = (k - k_first) & 1;
-      wait_all_requests();
-      __syncthreads();  // the stage is in LDS, and every wave has left the other half
-      step(lds + (cur ^ 1) * P::Bytes, lds + cur * P::Bytes, k + 1, k + 1 < k_last);
-    }
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i)
+    if (k_first + i < k_last) request(lds + i * P::Bytes, k_first + i);
+  int cur = 0;
+  for (int k = k_first; k < k_last; ++k) {
+    // stage k is in LDS, and every wave has left the part that k + ST - 1 goes to
+    if (k + ST - 2 < k_last)
+      wait_stage<P::Requests * (ST - 2)>();
+    else
+      wait_stage<0>();
+    const int nxt = cur == 0 ? ST - 1 : cur - 1;
+    step(lds + nxt * P::Bytes, lds + cur * P::Bytes, k + ST - 1, k + ST - 1 < k_last);
+    cur = cur == ST - 1 ? 0 : cur + 1;
   }
-  if (ACT == kActMx && a.steps % KB != 0 && part == a.split - 1) {
-    // the odd 128 values at the end, straight from memory
-    const int k = a.steps - 1;
-    u32x4 x[T];
-    uint32_t sx[T];
+  if constexpr (WK > 1) {
+    // the groups' sums, added by the first one
+    __syncthreads();
+    f32x4* sums = reinterpret_cast<f32x4*>(lds) + (wv % (WR * WT)) * kWave + lane;
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-      const size_t tok = min(tok0 + wt * (BT / WT) + t * 16 + r, a.m - 1);
-      x[t] = *reinterpret_cast<const u32x4*>(static_cast<const uint8_t*>(a.x) + tok * a.ldx + (size_t)k * 64 + g * 16);
-      sx[t] = a.xs[tok * pitch_s + (size_t)k * 4 + g];
-    }
+    for (int q = 1; q < WK; ++q)
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int tr = piece_row(i) + r, mat = MATS == 2 ? piece_row(i) / (BR / 2) : 0;
-      const size_t row = min(row0 + tr % (BR / MATS), a.rows - 1);
-      const u32x4 w = *reinterpret_cast<const u32x4*>(a.q[mat] + row * pitch_q + (size_t)k * 64 + g * 16);
-      const uint32_t sw = a.s[mat][row * pitch_s + (size_t)k * 4 + g];
+      for (int i = 0; i < R; ++i)
 #pragma unroll
-      for (int t = 0; t < T; ++t) acc[i][t] = mfma_mx<0, 0>(w, x[t], acc[i][t], sw, sx[t]);
+        for (int t = 0; t < T; ++t)
+          if (wk == q) sums[(((q - 1) * R + i) * T + t) * (WR * WT * kWave)] = acc[i][t];
+    __syncthreads();
+    if (wk != 0) return;
+#pragma unroll
+    for (int q = 1; q < WK; ++q)
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < T; ++t) acc[i][t] += sums[(((q - 1) * R + i) * T + t) * (WR * WT * kWave)];
+  }
+  if (SK > 1 && part == a.split - 1) {
+    // the last steps that do not fill a stage, straight from memory
+    for (int k = stages_all * SK; k < a.steps; ++k) {
+      constexpr int XV = ACT == kActMx ? 1 : 4;
+      u32x4 x[T][XV];
+      uint32_t sx[T];
+#pragma unroll
+      for (int t = 0; t < T; ++t) {
+        const size_t tok = min(tok0 + wt * (BT / WT) + t * 16 + r, a.m - 1);
+        const uint8_t* xp = static_cast<const uint8_t*>(a.x) + tok * a.ldx + (size_t)k * (64 * XV) + g * (16 * XV);
+#pragma unroll
+        for (int j = 0; j < XV; ++j) x[t][j] = *reinterpret_cast<const u32x4*>(xp + 16 * j);
+        sx[t] = ACT == kActMx ? a.xs[tok * pitch_s + (size_t)k * 4 + g] : 0u;
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        asm volatile("" ::: "memory");  // one piece's codes at a time: the registers are the sums'
+        const int tr = piece_row(i) + r;
+        const size_t row = min(row0 + tr % (BR / MATS), a.rows - 1);
+        const int mat = MATS == 2 ? i / (R / 2) : 0;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(a.q[mat] + row * pitch_q + (size_t)k * 64 + g * 16);
+        const uint32_t sw = a.s[mat][row * pitch_s + (size_t)k * 4 + g];
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+          if constexpr (ACT == kActMx) {
+            acc[i][t] = mfma_mx<0, 0>(w, x[t][0], acc[i][t], sw, sx[t]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < XV; ++j)
+              acc[i][t] = mfma_half(ACT == kActBF16, mx_half8<ACT == kActBF16>(w[j], mx_scale(sw)), x[t][j], acc[i][t]);
+          }
+        }
+      }
     }
   }
 
   // a lane holds rows 4 g .. 4 g + 3 of each piece for token r of each
-  const bool vec = (a.rows & 3) == 0;
-  auto put = [&](void* y, int dt, int i, int t, f32x4 v) {
+  auto put = [&](auto dtype, void* y, int i, int t, f32x4 v) {
+    constexpr int DT = decltype(dtype)::value;
     const int row = row0 + piece_row(i) % (BR / MATS) + 4 * g;
     const int tok = tok0 + wt * (BT / WT) + t * 16 + r;
     if (tok >= a.m || row >= a.rows) return;
     const size_t at = (size_t)tok * a.rows + row;
-    if (vec) {
-      if (dt == kF32)
+    if ((a.rows & 3) == 0) {
+      if constexpr (DT == kF32)
         *reinterpret_cast<f32x4*>(static_cast<float*>(y) + at) = v;
-      else if (dt == kBF16)
+      else if constexpr (DT == kBF16)
         *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(y) + at) = u32x2{pack_bf2(v.x, v.y), pack_bf2(v.z, v.w)};
       else
         *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(y) + at) = u32x2{pack_f2(v.x, v.y), pack_f2(v.z, v.w)};
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (row + e < a.rows) store_one(y, at + e, dt, v[e]);
+        if (row + e < a.rows) store_one(y, at + e, DT, v[e]);
     }
   };
-  if (a.part) {
-    const size_t mat_size = (size_t)a.m * a.rows;
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int mat = MATS == 2 ? i / (R / 2) : 0;
-#pragma unroll
-      for (int t = 0; t < T; ++t) put(a.part + (size_t)(part * MATS + mat) * mat_size, kF32, i, t, acc[i][t]);
-    }
-  } else {
+  auto finish = [&](auto dtype) {
 #pragma unroll
     for (int i = 0; i < R / MATS; ++i)
 #pragma unroll
@@ -402,8 +487,24 @@ __global__ __launch_bounds__(WR* WT* kWave) void k_mx_tile(LinArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = relu(v[e]);
         }
-        put(a.y, a.y_dtype, i, t, v);
+        put(dtype, a.y, i, t, v);
       }
+  };
+  if (a.part) {
+    const size_t mat_size = (size_t)a.m * a.rows;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int mat = MATS == 2 ? i / (R / 2) : 0;
+#pragma unroll
+      for (int t = 0; t < T; ++t)
+        put(std::integral_constant<int, kF32>{}, a.part + (size_t)(part * MATS + mat) * mat_size, i, t, acc[i][t]);
+    }
+  } else if (a.y_dtype == kF32) {
+    finish(std::integral_constant<int, kF32>{});
+  } else if (a.y_dtype == kBF16) {
+    finish(std::integral_constant<int, kBF16>{});
+  } else {
+    finish(std::integral_constant<int, kF16>{});
   }
 }
 
@@ -460,75 +561,130 @@ __global__ __launch_bounds__(256) void k_mx_pad(const uint16_t* __restrict__ x, 
 
 namespace {
 
+// The tiles, by size: rows of W, tokens, steps of a stage.
+struct Shape {
+  int br, bt, sk;
+};
+constexpr Shape kHalfTiles[] = {{32, 16, 4},  {64, 16, 4},  {128, 16, 2}, {64, 32, 4},  {128, 32, 2},
+                                {128, 48, 2}, {128, 64, 2}, {256, 64, 2}, {256, 128, 1}};
+constexpr Shape kMxTiles[] = {{32, 16, 8},  {64, 16, 8},   {64, 32, 4},   {64, 64, 4},
+                              {128, 64, 4}, {128, 128, 4}, {256, 128, 2}, {256, 256, 2}};
+constexpr int kHalfCount = sizeof kHalfTiles / sizeof *kHalfTiles, kMxCount = sizeof kMxTiles / sizeof *kMxTiles;
+constexpr long kBlocks = 256;  // compute units
+
 struct Plan {
-  bool pad;      // x is copied into the workspace first
-  bool skinny;
-  bool big;      // the large tile
+  bool pad;   // x is copied into the workspace first
+  int tile;   // -1: k_mx_skinny
   int split;
   size_t pad_bytes, part_bytes;
 };
 
 int act_of(const MxLinear& c) { return c.xq ? kActMx : c.x_dtype == kBF16 ? kActBF16 : kActF16; }
 
-constexpr int kSkinnyTokens = 16;
-constexpr int kSmallRows = 64, kSmallToks = 64;
-
+// Which kernel.  With one block a compute unit a tile's time is set by what it
+// streams, so the smallest tile whose blocks are at most the compute units is
+// the fastest (4096 x 4096, 64 tokens, us: 64 x 16 in 256 blocks 7.9, 64 x 32 in
+// 128 10.8, 64 x 64 in 64 16.8; 11008 x 4096, 128 tokens: 128 x 64 in 172 blocks
+// 23.5, 64 x 32 in 688 28.8).  Products too large for that take the largest tile,
+// or for up to 64 tokens the one that pads them least, with the most rows.  Fewer than
+// half as many blocks with a long n share it out (4096 x 11008, 16 tokens: 12.8
+// in one part, 12.1 in two; 512 x 11008, 10 tokens: 14.7 / 10.2 in four), at the
+// price of a second launch, so only where a part keeps five stages.
+// k_mx_skinny takes 16 rows a block: up to 4 tokens over at most 256 blocks, both
+// matrices counted (4096 x 11008: one token 7.9 against 11.5, 4 tokens 9.7
+// against 11.6, 8 tokens 14.7 against 12.2; 11008 x 4096, one token: 9.5 against
+// 8.1).
 Plan plan_of(const MxLinear& c) {
   Plan p;
   const int np = mx_padded(c.n), mats = c.q_up ? 2 : 1, act = act_of(c);
   p.pad = act != kActMx && (c.n % kMxPad != 0 || c.ldx % 8 != 0 || (reinterpret_cast<uintptr_t>(c.x) & 15u) != 0);
   p.pad_bytes = p.pad ? align256((size_t)c.m * np * 2) : 0;
-  p.skinny = c.m <= kSkinnyTokens;
   p.split = 1;
-  p.big = false;
-  if (!p.skinny) {
-    const int big_r = 256 / mats, big_t = act == kActMx ? 256 : 128;
-    const long big = (long)((c.rows + big_r - 1) / big_r) * ((c.m + big_t - 1) / big_t);
-    p.big = big >= 192;
-    if (!p.big) {
-      const long tiles = (long)((c.rows + kSmallRows / mats - 1) / (kSmallRows / mats)) * ((c.m + kSmallToks - 1) / kSmallToks);
-      const int stages = np / kMxPad / (act == kActMx ? 2 : 1);
-      long split = (512 + tiles - 1) / tiles;
-      if (split > stages / 4) split = stages / 4;
-      if (split > 16) split = 16;
-      p.split = split < 1 ? 1 : (int)split;
+  p.tile = -1;
+  if (c.m > kSToks || (long)c.rows * mats > 16 * kBlocks) {
+    const Shape* tiles = act == kActMx ? kMxTiles : kHalfTiles;
+    const int count = act == kActMx ? kMxCount : kHalfCount;
+    auto blocks = [&](const Shape& t) {
+      return (long)((c.rows + t.br / mats - 1) / (t.br / mats)) * ((c.m + t.bt - 1) / t.bt);
+    };
+    for (int i = 0; i < count && p.tile < 0; ++i)
+      if (blocks(tiles[i]) <= kBlocks) p.tile = i;
+    if (p.tile < 0) {
+      p.tile = count - 1;
+      if (c.m <= 64)
+        for (int i = 0; i < count; ++i)
+          if (tiles[i].bt >= c.m && tiles[i].bt <= tiles[p.tile].bt) p.tile = i;
     }
+    const Shape& t = tiles[p.tile];
+    const long n_blocks = blocks(t), stages = np / kMxPad / t.sk;
+    if (n_blocks * 2 <= kBlocks) p.split = (int)std::max(1l, std::min(kBlocks / n_blocks, std::min(stages / 5, 8l)));
   }
   p.part_bytes = p.split > 1 ? (size_t)p.split * mats * c.m * c.rows * sizeof(float) : 0;
   return p;
 }
 
-template <int ACT, int MATS, int BR, int BT, int WR, int WT>
+template <int ACT, int MATS, int BR, int BT, int WR, int WT, int WK, int ST>
 hipError_t tile_launch(LinArgs a, hipStream_t s) {
-  using P = Tile<ACT, MATS, BR, BT, WR, WT>;
+  using P = Tile<ACT, MATS, BR, BT, WR, WT, WK, ST>;
   static std::atomic<int> attr_set[kMaxDevices];
   const int ok = per_device_once(attr_set, [](int) -> int {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mx_tile<ACT, MATS, BR, BT, WR, WT>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, 2 * P::Bytes) == hipSuccess ? 1 : -1;
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mx_tile<ACT, MATS, BR, BT, WR, WT, WK, ST>),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, ST * P::Bytes) == hipSuccess ? 1 : -1;
   });
   if (ok != 1) return hipErrorInvalidConfiguration;
   a.row_tiles = (a.rows + BR / MATS - 1) / (BR / MATS);
   a.tok_tiles = (a.m + BT - 1) / BT;
-  k_mx_tile<ACT, MATS, BR, BT, WR, WT>
-      <<<(unsigned)(a.row_tiles * a.tok_tiles * a.split), WR * WT * kWave, 2 * P::Bytes, s>>>(a);
+  k_mx_tile<ACT, MATS, BR, BT, WR, WT, WK, ST>
+      <<<(unsigned)(a.row_tiles * a.tok_tiles * a.split), WR * WT * WK * kWave, ST * P::Bytes, s>>>(a);
   return hipGetLastError();
 }
 
 template <int ACT, int MATS>
 hipError_t linear_launch(const LinArgs& a, const Plan& p, hipStream_t s) {
-  if (p.skinny) {
-    k_mx_skinny<ACT, MATS><<<(unsigned)((a.rows + 15) / 16), kSW * kWave, 0, s>>>(a);
+  if (p.tile < 0) {
+    // the kernel's dynamic LDS limit, set once per device
+    static std::atomic<int> attr_set[kMaxDevices];
+    const int ok = per_device_once(attr_set, [](int) -> int {
+      return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mx_skinny<ACT, MATS>),
+                                 hipFuncAttributeMaxDynamicSharedMemorySize, kSLds) == hipSuccess ? 1 : -1;
+    });
+    if (ok != 1) return hipErrorInvalidConfiguration;
+    const int lds = ACT == kActMx ? 0 : a.m * (std::min(skinny_chunk(a.m), a.steps) * 256 + 16);
+    k_mx_skinny<ACT, MATS><<<(unsigned)((a.rows + 15) / 16), kSW * kWave, lds, s>>>(a);
     return hipGetLastError();
   }
-  hipError_t e;
-  if (p.big) {
-    if constexpr (ACT == kActMx)
-      e = tile_launch<ACT, MATS, 256, 256, 2, 4>(a, s);
-    else
-      e = tile_launch<ACT, MATS, 256, 128, 4, 2>(a, s);
-  } else {
-    e = tile_launch<ACT, MATS, kSmallRows, kSmallToks, 2, 2>(a, s);
+  hipError_t e = hipErrorInvalidValue;
+#define SI_TILE(I, TILES, WR, WT, WK, ST)                                                    \
+  case I: {                                                                                  \
+    static_assert(TILES[I].sk == WK * (ACT == kActMx ? 2 : 1), "steps of a stage");          \
+    e = tile_launch<ACT, MATS, TILES[I].br, TILES[I].bt, WR, WT, WK, ST>(a, s);              \
+    break;                                                                                   \
   }
+  if constexpr (ACT == kActMx) {
+    switch (p.tile) {
+      SI_TILE(0, kMxTiles, 1, 1, 4, 3)
+      SI_TILE(1, kMxTiles, 2, 1, 4, 3)
+      SI_TILE(2, kMxTiles, 2, 1, 2, 4)
+      SI_TILE(3, kMxTiles, 2, 2, 2, 3)
+      SI_TILE(4, kMxTiles, 2, 2, 2, 3)
+      SI_TILE(5, kMxTiles, 2, 2, 2, 2)
+      SI_TILE(6, kMxTiles, 4, 2, 1, 2)
+      SI_TILE(7, kMxTiles, 2, 4, 1, 2)
+    }
+  } else {
+    switch (p.tile) {
+      SI_TILE(0, kHalfTiles, 1, 1, 4, 3)
+      SI_TILE(1, kHalfTiles, 2, 1, 4, 3)
+      SI_TILE(2, kHalfTiles, 4, 1, 2, 4)
+      SI_TILE(3, kHalfTiles, 2, 1, 4, 2)
+      SI_TILE(4, kHalfTiles, 4, 1, 2, 3)
+      SI_TILE(5, kHalfTiles, 4, 1, 2, 3)
+      SI_TILE(6, kHalfTiles, 4, 1, 2, 3)
+      SI_TILE(7, kHalfTiles, 4, 1, 2, 2)
+      SI_TILE(8, kHalfTiles, 4, 2, 1, 2)
+    }
+  }
+#undef SI_TILE
   if (e != hipSuccess || !a.part) return e;
   const size_t size = (size_t)a.m * a.rows;
   k_mx_join<MATS><<<(unsigned)((size + 1023) / 1024), 256, 0, s>>>(a.part, a.split, size, a.y, a.y_dtype, a.relu);
@@ -543,8 +699,9 @@ hipError_t linear_mats(const LinArgs& a, const Plan& p, hipStream_t s) {
 }  // namespace
 
 bool mx_linear_fits(const MxLinear& c) {
-  // the finest tiles and the longest copy: fewer than 2^32 threads a launch
-  const double tiles = ((double)c.rows / 32 + 1) * ((double)c.m / 64 + 1);
+  // tiles of at least 128 x 16 past 256 blocks and the copy: fewer than 2^32
+  // threads a launch
+  const double tiles = ((double)c.rows / 64 + 1) * ((double)c.m / (c.m > 64 ? 128 : 16) + 1);
   return tiles * 512 < 4294967296.0 && (double)c.m * (mx_padded(c.n) / 8) < 4294967296.0;
 }
 

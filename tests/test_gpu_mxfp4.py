@@ -261,18 +261,18 @@ def test_product_extreme_scales(m):
 
 
 @pytest.mark.parametrize("a4", [False, True])
-def test_same_bits_and_bounds(a4):
-    """Two runs of a split product agree bit for bit, and nothing is written
+@pytest.mark.parametrize("m,rows,n,split", [(40, 72, 4096, False), (10, 100, 16384, True)])
+def test_same_bits_and_bounds(a4, m, rows, n, split):
+    """Runs of a product, split or not, agree bit for bit, and nothing is written
     behind y and the workspace."""
     from paper_2411_12692_amd import _lib
-    m, rows, n = 40, 72, 4096
     g = torch.Generator().manual_seed(3)
     w, x = torch.randn(rows, n, generator=g).to(DEV), torch.randn(m, n, generator=g).half().to(DEV)
     q, s = si.quantize_rows_mxfp4(w)
     xq, xs = si.quantize_rows_mxfp4(x)
     first = si.linear_mxfp4_a4(xq, xs, q, s, F32) if a4 else si.linear_mxfp4(x, q, s, F32)
     need = _lib.load().si_linear_mxfp4_workspace_bytes(None if a4 else x.data_ptr(), n, m, rows, n, 0)
-    assert need > 0  # n is split here
+    assert (need > 0) == split
     ws = torch.full((need + 256,), 0xA5, dtype=torch.uint8, device=DEV)
     y = torch.full((m * rows + 64,), -7.0, device=DEV)
     st = torch.cuda.current_stream().cuda_stream
@@ -317,3 +317,25 @@ def test_python_refusals():
     with pytest.raises(si.SparseInferError):  # out over the branch
         b = h.clone()
         si.norm_residual(h, b, out=b)
+
+
+# one shape for each tile of each kind of activations, and for the products larger
+# than every tile's 256 blocks with few tokens
+EVERY_TILE = [(9, 500, 640), (9, 9000, 384), (9, 18000, 256), (30, 8100, 640), (20, 20000, 256), (33, 32000, 256),
+              (40, 25000, 128), (60, 20000, 384), (64, 40000, 128), (130, 30000, 128), (700, 3000, 640),
+              (1100, 8100, 256), (5, 70000, 128), (3, 4097, 1152), (4, 1500, 13056)]
+
+
+@pytest.mark.parametrize("m,rows,n", EVERY_TILE)
+@pytest.mark.parametrize("act", ["f16", "a4"])
+@pytest.mark.parametrize("gated", [False, True])
+def test_product_exact_every_tile(m, rows, n, act, gated):
+    """n of odd numbers of 128 values, so that the last ones do not fill a stage."""
+    test_product_exact(m, rows, n, act, gated)
+
+
+@pytest.mark.parametrize("m,rows,n", [(10, 100, 16384), (300, 64, 8192), (1, 64, 20000)])
+@pytest.mark.parametrize("act", ["bf16", "a4"])
+@pytest.mark.parametrize("gated", [False, True])
+def test_product_exact_split(m, rows, n, act, gated):
+    test_product_exact(m, rows, n, act, gated)
