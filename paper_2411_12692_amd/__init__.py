@@ -596,21 +596,30 @@ def _mx_mlp(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, y, workspace, *mo
     """Checks of the two MXFP4 MLP calls: returns ``(k, d, b, device index,
     y)`` and the addresses of the weights."""
     k = _mx(q_gate, s_gate, "q_gate")
-    d = 2 * q_gate.shape[1]
-    if q_up is not None and _mx(q_up, s_up, "q_up", d) != k:
-        raise ValueError("q_up does not match q_gate")
-    if _mx(q_down_t, s_down_t, "q_down_t", d) != k:
-        raise ValueError("q_down_t does not match q_gate")
-    b = _x2(x, d).shape[0]
+    shape, s_shape = q_gate.shape, s_gate.shape
+    d = 2 * shape[1]
+    weights = [q_gate.data_ptr(), s_gate.data_ptr(), None, None, q_down_t.data_ptr(), s_down_t.data_ptr()]
+    for q, s, name in ((q_up, s_up, "q_up"), (q_down_t, s_down_t, "q_down_t")):
+        if q is None:
+            continue
+        if not (q.shape == shape and s.shape == s_shape and q.dtype is torch.uint8 and s.dtype is torch.uint8
+                and q.is_contiguous() and s.is_contiguous()):
+            _mx(q, s, name, d)
+            raise ValueError(f"{name} does not match q_gate")
+    if q_up is not None:
+        weights[2], weights[3] = q_up.data_ptr(), s_up.data_ptr()
+    if not (isinstance(x, torch.Tensor) and x.dim() == 2 and x.shape[1] == d and x.dtype in _F16
+            and x.is_contiguous()):
+        x = _x2(x, d)
+    b = x.shape[0]
     if y is None:
-        y = x.new_empty((b, d), dtype=torch.float32)
+        y = torch.empty_like(x, dtype=torch.float32)
     else:
         _dev(y, "y", (torch.float32,))
         if y.numel() != b * d:
             raise ValueError(f"y must hold [{b}][{d}] floats")
-    index = _same_device(x, q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, y, workspace, *more)
-    up = (None, None) if q_up is None else (q_up.data_ptr(), s_up.data_ptr())
-    return k, d, b, index, y, (q_gate.data_ptr(), s_gate.data_ptr(), *up, q_down_t.data_ptr(), s_down_t.data_ptr())
+    index = _same_device(q_gate, x, s_gate, q_up, s_up, q_down_t, s_down_t, y, workspace, *more)
+    return k, d, b, index, y, weights
 
 
 def sparse_mlp_mxfp4(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, workspace, mask, flags: int = 0,

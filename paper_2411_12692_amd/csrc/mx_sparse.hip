@@ -3,21 +3,20 @@
 //
 // k_mx_rows: a block owns 32 rows.  It counts the sign products of its rows from
 // the packed signs (lane = row and half of the units), applies Eq. (2) as N_neg <
-// T, writes the mask and the rows' kept bits, and runs gate/up of the kept rows,
-// a wave to a row: 16 bytes a lane hold one block of 32 codes, turned into fp16
-// exactly (a code has two significant bits), multiplied with the tokens in LDS by
-// two-way dot products in fp32, and scaled once a block, so every scale byte is
-// exact.  W_up is requested with W_gate where the row is surely kept, otherwise
-// only when some token's gate value is positive.  h3 goes to the workspace.
+// T, writes the mask, and runs gate/up of the kept rows, a wave to a row: 16 bytes
+// a lane hold one block of 32 codes, turned into fp16 exactly (a code has two
+// significant bits), multiplied with the tokens in LDS by two-way dot products in
+// fp32, and scaled once a block, so every scale byte is exact.  W_up is requested
+// with W_gate where the row is surely kept, otherwise only when some token's gate
+// value is positive.  h3 goes to the workspace, and a bit for each row whose h3 is
+// not 0 for every token.
 //
-// k_mx_down: block (tile of 512 columns, chunk of row groups) adds h3_i *
-// W_down^T[i, tile] over the kept rows of its chunk in registers, folds its
-// waves in LDS and leaves the chunk's tile in the workspace; the last block of a
-// tile to finish adds the chunks in their order.  No sum depends on which block
-// came first: y is the same bits in every run.
+// k_mx_down: a block owns 16 columns of y over all rows: it lists the rows whose bit
+// is set and its threads take one each, 8 bytes of codes (neighbouring columns lie
+// on the same XCD, so a row's line is fetched into one L2 and used by 16 blocks
+// there).  The threads' sums meet in registers and LDS in a fixed order: no partial
+// sums in memory, no atomics, and y is the same bits in every run.
 //
-// Bound at one token by two launches' latency chains (signs, gate/up; h3, down,
-// fold, sum), not by the bytes.
 #include "layer_common.h"
 #include "mx.h"
 #include "mx_launch.h"
@@ -27,45 +26,34 @@ namespace si {
 constexpr int kMG = 32;      // rows of a block of k_mx_rows
 constexpr int kMW = 8;       // waves of a block
 constexpr int kMT = kMW * kWave;
-// header words of the workspace that no other call uses: chunks of each tile of y
-// that are done (zero between calls)
-constexpr int kHdrDone = 16;
-static_assert(kHdrDone > H_H3_FORM && kHdrDone + kMaxD / kTile <= H_WORDS, "a counter for each tile");
-constexpr int kDownTarget = 512;  // blocks that k_mx_down aims at
+constexpr int kMCols = 16;   // columns of y of a block of k_mx_down
+constexpr int kSignUnits = kMaxD / 128 / (2 * kMW);  // sign units of a lane (4)
 
 inline __host__ __device__ int mx_groups(int k) { return (k + kMG - 1) / kMG; }
-inline __host__ __device__ int mx_tiles(int d) { return (d + kTile - 1) / kTile; }
-// chunks of row groups a tile of y is summed from
-inline __host__ __device__ int mx_chunks(int k, int d) {
-  const int g = mx_groups(k), c = kDownTarget / mx_tiles(d) < 64 ? kDownTarget / mx_tiles(d) : 64;
-  return g < c ? g : c;
-}
 
 // Behind the workspace's common part, at offsets that depend on b: nothing here is
-// read before the same call wrote it.  What has to last from call to call (the
-// tiles' counters) is in the header, which lies the same for every b.
+// read before the same call wrote it.
 struct MxWs {
-  size_t kmask;   // uint32 [groups] kept bits
+  size_t kmask;   // uint32 [groups] kept rows
+  size_t dmask;   // uint32 [groups] rows whose W_down^T row is read
   size_t counts;  // int32 [groups][2] rows whose W_up / W_down^T row was read
-  size_t part;    // float [chunks][b][d]
   size_t total;
 };
-static MxWs mx_ws(int k, int d, int b) {
+static MxWs mx_ws(int k, int b) {
   MxWs L;
   L.kmask = ws_layout(k, b).total;
-  L.counts = L.kmask + align256((size_t)mx_groups(k) * 4);
-  L.part = L.counts + align256((size_t)mx_groups(k) * 8);
-  L.total = L.part + align256((size_t)mx_chunks(k, d) * b * d * 4);
+  L.dmask = L.kmask + align256((size_t)mx_groups(k) * 4);
+  L.counts = L.dmask + align256((size_t)mx_groups(k) * 4);
+  L.total = L.counts + align256((size_t)mx_groups(k) * 8);
   return L;
 }
-size_t mx_mlp_workspace(int k, int d, int b) { return mx_ws(k, d, b).total; }
+size_t mx_mlp_workspace(int k, int b) { return mx_ws(k, b).total; }
 
 // Tokens in LDS: 8-value piece j of unit u (32 values) of token t at
 // xs[(t * 4 + j) * U + u], so that lanes with neighbouring units read
 // neighbouring 16 bytes.
 
-// The codes and scales of a row, unit lane + 64 j; lanes past the row's end
-// hold zero codes.
+// The codes and scales of a row, unit lane + 64 j.
 template <int NU>
 struct MxRow {
   u32x4 c[NU];
@@ -83,29 +71,47 @@ __device__ inline void mx_load_row(const u32x4* __restrict__ q, const uint8_t* _
     r.s[j] = sr[u];
   }
 }
-template <int B, int NU>
-__device__ inline void mx_dots(const MxRow<NU>& r, const u32x4* xs, int U, int lane, float (&out)[B]) {
+// Dot products of MATS rows with the tokens, each token's values read once for
+// all of them.
+template <int B, int NU, int MATS>
+__device__ inline void mx_dots(const MxRow<NU> (&r)[MATS], const u32x4* xs, int U, int lane, float (&out)[MATS][B]) {
 #pragma unroll
-  for (int t = 0; t < B; ++t) out[t] = 0.f;
+  for (int m = 0; m < MATS; ++m)
+#pragma unroll
+    for (int t = 0; t < B; ++t) out[m][t] = 0.f;
 #pragma unroll
   for (int j = 0; j < NU; ++j) {
     const int u = lane + kWave * j;
     if (u < U) {
-      u32x4 w[4];
+      float a[MATS][B];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = mx_half8<false>(r.c[j][i], 1.0f);
-      const float sc = mx_factor(r.s[j]);
+      for (int m = 0; m < MATS; ++m)
 #pragma unroll
-      for (int t = 0; t < B; ++t) {
-        float a = 0.f;
+        for (int t = 0; t < B; ++t) a[m][t] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a = dot8(w[i], xs[(t * 4 + i) * U + u], a);
-        out[t] = fmaf(a, sc, out[t]);
+      for (int i = 0; i < 4; ++i) {
+        u32x4 w[MATS];
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) w[m] = mx_half8<false>(r[m].c[j][i], 1.0f);
+#pragma unroll
+        for (int t = 0; t < B; ++t) {
+          const u32x4 x = xs[(t * 4 + i) * U + u];
+#pragma unroll
+          for (int m = 0; m < MATS; ++m) a[m][t] = dot8(w[m], x, a[m][t]);
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < MATS; ++m) {
+        const float sc = mx_factor(r[m].s[j]);
+#pragma unroll
+        for (int t = 0; t < B; ++t) out[m][t] = fmaf(a[m][t], sc, out[m][t]);
       }
     }
   }
 #pragma unroll
-  for (int t = 0; t < B; ++t) out[t] = wave_total(out[t]);
+  for (int m = 0; m < MATS; ++m)
+#pragma unroll
+    for (int t = 0; t < B; ++t) out[m][t] = wave_total(out[m][t]);
 }
 
 struct MxArgs {
@@ -123,60 +129,79 @@ struct MxArgs {
   uint32_t flags;
   uint32_t* hdr;
   uint32_t* kmask;
+  uint32_t* dmask;
   int32_t* counts;
-  uint32_t* done;
-  float* part;
   float* h3;
   float* y;
   int32_t* idx;
   int32_t* n_out;
   int32_t* counters;
-  int groups, tiles, chunks;
+  int groups, tiles;
 };
 
 template <int B, int NU>
 __global__ __launch_bounds__(kMT) void k_mx_rows(MxArgs a) {
   extern __shared__ u32x4 xs[];  // [B][4][U]
-  __shared__ __attribute__((aligned(16))) uint32_t xw[B * (kMaxD / 32)];
+  __shared__ __attribute__((aligned(16))) uint32_t xw[B * (NU * kWave)];
   __shared__ int cnt[kMW][B][kWave];
   __shared__ uint32_t kept[kMG];  // sure << 31 | row
-  __shared__ int s_n, s_up, s_down;
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int U = a.d >> 5;
+  __shared__ uint32_t s_kept, s_down, s_up;
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
+  const int U = a.d >> 5, units = U >> 2;
   const int v = blockIdx.x;
-
-  for (int i = tid; i < B * U * 4; i += kMT) {
-    const int t = i / (U * 4), p = i - t * (U * 4);
-    xs[(t * 4 + (p & 3)) * U + (p >> 2)] = a.x[i];
+  // the signs are requested first: everything up to the counts hides behind them
+  const int kpad = row_groups(a.k) * kRowGroup;
+  u32x4 sg[kSignUnits];
+  if (a.signs) {
+    const u32x4* p = a.signs + (size_t)v * kMG + (lane & (kMG - 1));
+#pragma unroll
+    for (int i = 0; i < kSignUnits; ++i) {
+      const int q = 2 * wv + (lane >> 5) + 2 * kMW * i;
+      if (q < units) sg[i] = load_nt(p + (size_t)q * kpad);
+    }
   }
+  // tokens to LDS with their sign bits (a byte for 8 values), all of a thread's
+  // pieces in flight together
+  uint8_t* xb = reinterpret_cast<uint8_t*>(xw);
+  constexpr int XP = (NU * kWave * 4 + kMT - 1) / kMT;  // 16-byte pieces of a token a thread
+  u32x4 xv[B][XP];
+#pragma unroll
+  for (int t = 0; t < B; ++t)
+#pragma unroll
+    for (int i = 0; i < XP; ++i) {
+      const int p = tid + kMT * i;
+      if (p < U * 4) xv[t][i] = a.x[(size_t)t * (U * 4) + p];
+    }
+#pragma unroll
+  for (int t = 0; t < B; ++t)
+#pragma unroll
+    for (int i = 0; i < XP; ++i) {
+      const int p = tid + kMT * i;
+      if (p < U * 4) {
+        xs[(t * 4 + (p & 3)) * U + (p >> 2)] = xv[t][i];
+        xb[t * (U * 4) + p] = (uint8_t)sign_byte(xv[t][i]);
+      }
+    }
   if (tid == 0) {
-    s_up = 0;
     s_down = 0;
+    s_up = 0;
     if (v == 0) a.hdr[H_H3_FORM] = kH3PlainByRow;
   }
   __syncthreads();
   if (a.signs) {
-    for (int i = tid; i < B * U; i += kMT) {
-      const int t = i / U, u = i - t * U;
-      uint32_t w = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w |= sign_byte(xs[(t * 4 + j) * U + u]) << (8 * j);
-      xw[i] = w;
-    }
-    __syncthreads();
     int c[B];
 #pragma unroll
     for (int t = 0; t < B; ++t) c[t] = 0;
-    const int kpad = row_groups(a.k) * kRowGroup;
-    const int units = U >> 2;
-    const u32x4* sg = a.signs + (size_t)v * kMG + (lane & (kMG - 1));
-#pragma unroll 4
-    for (int q = 2 * wv + (lane >> 5); q < units; q += 2 * kMW) {
-      const u32x4 s = load_nt(sg + (size_t)q * kpad);
 #pragma unroll
-      for (int t = 0; t < B; ++t) {
-        const u32x4 xv = *reinterpret_cast<const u32x4*>(&xw[t * U + 4 * q]);
-        c[t] += __popc(s.x ^ xv.x) + __popc(s.y ^ xv.y) + __popc(s.z ^ xv.z) + __popc(s.w ^ xv.w);
+    for (int i = 0; i < kSignUnits; ++i) {
+      const int q = 2 * wv + (lane >> 5) + 2 * kMW * i;
+      if (q < units) {
+        const u32x4 s = sg[i];
+#pragma unroll
+        for (int t = 0; t < B; ++t) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(&xw[t * U + 4 * q]);
+          c[t] += __popc(s.x ^ w.x) + __popc(s.y ^ w.y) + __popc(s.z ^ w.z) + __popc(s.w ^ w.w);
+        }
       }
     }
 #pragma unroll
@@ -203,56 +228,72 @@ __global__ __launch_bounds__(kMT) void k_mx_rows(MxArgs a) {
     }
     const uint64_t ballot = __ballot(keep);
     if (keep) kept[__popcll(ballot & lanes_below(lane))] = (uint32_t)row | (sure ? 0x80000000u : 0u);
-    if (lane == 0) {
-      s_n = __popcll(ballot);
-      a.kmask[v] = (uint32_t)ballot;
-    }
+    if (lane == 0) s_kept = (uint32_t)ballot;
   }
   __syncthreads();
-  const int n = s_n;
+  const int n = __popc(s_kept);
   const bool no_as = (a.flags & kNoAS) != 0, no_spec = (a.flags & kNoSpec) != 0;
-  int n_up = 0, n_down = 0;
   for (int i = wv; i < n; i += kMW) {
     const uint32_t e = (uint32_t)uniform((int)kept[i]);
     const int row = (int)(e & 0x7fffffffu);
     const bool early = a.qu && (no_as || ((e >> 31) && !no_spec));
-    MxRow<NU> rg, ru;
-    mx_load_row<NU>(a.qg, a.sg, row, U, lane, rg);
-    if (early) mx_load_row<NU>(a.qu, a.su, row, U, lane, ru);
-    float g[B], h[B];
-    mx_dots<B, NU>(rg, xs, U, lane, g);
+    float g[B], u[B], h[B];
+    bool up = early;
+    if (early) {
+      MxRow<NU> r[2];
+      mx_load_row<NU>(a.qg, a.sg, row, U, lane, r[0]);
+      mx_load_row<NU>(a.qu, a.su, row, U, lane, r[1]);
+      float o[2][B];
+      mx_dots<B, NU, 2>(r, xs, U, lane, o);
+#pragma unroll
+      for (int t = 0; t < B; ++t) {
+        g[t] = o[0][t];
+        u[t] = o[1][t];
+      }
+    } else {
+      MxRow<NU> r[1];
+      mx_load_row<NU>(a.qg, a.sg, row, U, lane, r[0]);
+      float o[1][B];
+      mx_dots<B, NU, 1>(r, xs, U, lane, o);
+#pragma unroll
+      for (int t = 0; t < B; ++t) g[t] = o[0][t];
+    }
     bool any = false;
 #pragma unroll
     for (int t = 0; t < B; ++t) {
       g[t] = g[t] > 0.f || g[t] != g[t] ? g[t] : 0.f;  // ReLU that keeps a NaN
       any |= g[t] != 0.f;
-      h[t] = a.qu ? 0.f : g[t];
     }
-    if (a.qu && (early || any)) {
-      if (!early) mx_load_row<NU>(a.qu, a.su, row, U, lane, ru);
-      float u[B];
-      mx_dots<B, NU>(ru, xs, U, lane, u);
+    if (a.qu && !early && any) {
+      up = true;
+      MxRow<NU> r[1];
+      mx_load_row<NU>(a.qu, a.su, row, U, lane, r[0]);
+      float o[1][B];
+      mx_dots<B, NU, 1>(r, xs, U, lane, o);
 #pragma unroll
-      for (int t = 0; t < B; ++t) h[t] = g[t] != 0.f ? g[t] * u[t] : 0.f;  // as where the row is skipped
-      ++n_up;
+      for (int t = 0; t < B; ++t) u[t] = o[0][t];
     }
     bool nz = no_as;
 #pragma unroll
-    for (int t = 0; t < B; ++t) nz |= h[t] != 0.f;
-    n_down += nz ? 1 : 0;
+    for (int t = 0; t < B; ++t) {  // as where the row is skipped: nothing of W_up where h1 is 0
+      h[t] = !a.qu ? g[t] : g[t] != 0.f ? g[t] * u[t] : 0.f;
+      nz |= h[t] != 0.f;
+    }
 #pragma unroll
     for (int t = 0; t < B; ++t)
       if (lane == t) a.h3[(size_t)row * B + t] = h[t];
-  }
-  if (a.counters) {
-    if (lane == 0 && (n_up | n_down)) {
-      atomicAdd(&s_up, n_up);
-      atomicAdd(&s_down, n_down);
+    if (lane == 0) {
+      if (nz) atomicOr(&s_down, 1u << (row - v * kMG));
+      if (up) atomicAdd(&s_up, 1u);
     }
-    __syncthreads();
-    if (tid == 0) {
-      a.counts[2 * v] = s_up;
-      a.counts[2 * v + 1] = s_down;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    a.kmask[v] = s_kept;
+    a.dmask[v] = s_down;
+    if (a.counters) {
+      a.counts[2 * v] = (int)s_up;
+      a.counts[2 * v + 1] = __popc(s_down);
     }
   }
 }
@@ -308,130 +349,114 @@ __device__ inline void mx_lists(const MxArgs& a, int* wsum) {
   if (a.n_out && tid == 0) *a.n_out = base;
 }
 
-constexpr int kDownRows = 256;  // kept rows a block lists at a time
+constexpr int kDownSpan = kMT * kMG;  // rows that a block lists at a time (16384)
 constexpr int kDownUnroll = 4;
+
+// Sum over the wave's lanes of N values each (N a power of two): while there is
+// more than one, a lane keeps half of them and gives the other half to the lane
+// a power of two away.  Lane l ends with the total of value l % N.
+template <int N>
+__device__ inline float lanes_total(float (&v)[N], int lane) {
+#pragma unroll
+  for (int w = N / 2, m = 1; w >= 1; w /= 2, m *= 2) {
+#pragma unroll
+    for (int i = 0; i < w; ++i) {
+      const bool odd = (lane & m) != 0;
+      const float keep = odd ? v[2 * i + 1] : v[2 * i], give = odd ? v[2 * i] : v[2 * i + 1];
+      v[i] = keep + __shfl_xor(give, m, kWave);
+    }
+  }
+  float s = v[0];
+#pragma unroll
+  for (int m = N; m < kWave; m *= 2) s += __shfl_xor(s, m, kWave);
+  return s;
+}
 
 template <int B>
 __global__ __launch_bounds__(kMT) void k_mx_down(MxArgs a) {
-  __shared__ float fold[kMW][kTile];
-  __shared__ int rows[kDownRows + kMG];
-  __shared__ float hs[kDownRows + kMG][B];
+  __shared__ uint16_t rows[kDownSpan];
+  __shared__ float fold[kMW][B][kMCols];
   __shared__ int wsum[kMW];
-  __shared__ int s_last;
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  if ((int)blockIdx.x == a.tiles * a.chunks) {
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
+  if ((int)blockIdx.x == a.tiles) {
     mx_lists(a, wsum);
     return;
   }
-  const int tile = blockIdx.x % a.tiles, chunk = blockIdx.x / a.tiles;
-  const int g0 = (int)((long long)a.groups * chunk / a.chunks), g1 = (int)((long long)a.groups * (chunk + 1) / a.chunks);
-  const int d = a.d, U = d >> 5;
-  const int col = tile * kTile + lane * 8;  // the lane's first column
-  const bool col_ok = col < d;
-  const bool no_as = (a.flags & kNoAS) != 0;
-  float acc[B][8];
+  // each XCD a run of neighbouring tiles (their number is a multiple of 8)
+  const int tile = (blockIdx.x & 7) * (a.tiles >> 3) + (blockIdx.x >> 3);
+  const int U = a.d >> 5, col = tile * kMCols;
+  const u32x2* qd = reinterpret_cast<const u32x2*>(a.qd) + (col >> 4);
+  const uint8_t* sd = a.sd + (col >> 5);
+  float acc[B][kMCols];
 #pragma unroll
   for (int t = 0; t < B; ++t)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[t][e] = 0.f;
+    for (int e = 0; e < kMCols; ++e) acc[t][e] = 0.f;
 
-  for (int gb = g0; gb < g1; gb += kDownRows / kMG) {
-    // the kept rows of up to 8 groups, a wave to a group, with their h3
-    const int g = gb + wv;
-    uint32_t bits = g < g1 ? (uint32_t)uniform((int)a.kmask[g]) : 0u;
-    const int row = g * kMG + lane;
-    bool use = lane < kMG && ((bits >> (lane & 31)) & 1u);
-    float h[B];
-#pragma unroll
-    for (int t = 0; t < B; ++t) h[t] = use ? a.h3[(size_t)row * B + t] : 0.f;
-    bool nz = no_as;
-#pragma unroll
-    for (int t = 0; t < B; ++t) nz |= h[t] != 0.f;
-    use = use && nz;
-    const uint64_t ballot = __ballot(use);
-    if (lane == 0) wsum[wv] = __popcll(ballot);
+  for (int g0 = 0; g0 < a.groups; g0 += kMT) {
+    uint32_t bits = g0 + tid < a.groups ? a.dmask[g0 + tid] : 0u;
+    const int incl = wave_incl_scan(__popc(bits));
+    if (g0 > 0) __syncthreads();  // the last span's list is read
+    if (lane == kWave - 1) wsum[wv] = incl;
     __syncthreads();
-    int at = 0, n = 0;
+    int at = incl - __popc(bits), n = 0;
 #pragma unroll
     for (int w = 0; w < kMW; ++w) {
       if (w < wv) at += wsum[w];
       n += wsum[w];
     }
-    if (use) {
-      at += __popcll(ballot & lanes_below(lane));
-      rows[at] = row;
-#pragma unroll
-      for (int t = 0; t < B; ++t) hs[at][t] = h[t];
-    }
+    for (; bits; bits &= bits - 1) rows[at++] = (uint16_t)(tid * kMG + __builtin_ctz(bits));
     __syncthreads();
-    for (int i0 = wv * kDownUnroll; i0 < n; i0 += kMW * kDownUnroll) {
-      uint32_t c[kDownUnroll], s[kDownUnroll];
+    // a thread takes every 512th row
+    for (int i0 = tid; i0 < n; i0 += kMT * kDownUnroll) {
+      u32x2 c[kDownUnroll];
+      uint32_t s[kDownUnroll];
+      float h[kDownUnroll][B];
 #pragma unroll
       for (int r = 0; r < kDownUnroll; ++r) {
-        const int i = min(i0 + r, n - 1);
-        const size_t rw = (size_t)uniform(rows[i]);
-        c[r] = 0;
+        const int i = i0 + kMT * r;
+        c[r] = u32x2{0, 0};
         s[r] = 0;
-        if (col_ok) {
-          c[r] = __builtin_nontemporal_load(a.qd + rw * (U * 4) + (col >> 3));
-          s[r] = a.sd[rw * U + (col >> 5)];
+#pragma unroll
+        for (int t = 0; t < B; ++t) h[r][t] = 0.f;
+        if (i < n) {
+          const size_t row = (size_t)g0 * kMG + rows[i];
+          c[r] = qd[row * (U * 2)];
+          s[r] = sd[row * U];
+#pragma unroll
+          for (int t = 0; t < B; ++t) h[r][t] = a.h3[row * B + t];
         }
       }
 #pragma unroll
       for (int r = 0; r < kDownUnroll; ++r) {
-        if (i0 + r < n) {
+        if (i0 + kMT * r < n) {
           const float sc = mx_scale(s[r]);
-          const f32x2 w0 = mx_f32x2<0>(c[r], sc), w1 = mx_f32x2<1>(c[r], sc), w2 = mx_f32x2<2>(c[r], sc),
-                      w3 = mx_f32x2<3>(c[r], sc);
-          const float w[8] = {w0.x, w0.y, w1.x, w1.y, w2.x, w2.y, w3.x, w3.y};
 #pragma unroll
-          for (int t = 0; t < B; ++t) {
-            const float hv = hs[i0 + r][t];
+          for (int p = 0; p < 2; ++p) {
+            const f32x2 w0 = mx_f32x2<0>(c[r][p], sc), w1 = mx_f32x2<1>(c[r][p], sc), w2 = mx_f32x2<2>(c[r][p], sc),
+                        w3 = mx_f32x2<3>(c[r][p], sc);
+            const float w[8] = {w0.x, w0.y, w1.x, w1.y, w2.x, w2.y, w3.x, w3.y};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[t][e] = fmaf(hv, w[e], acc[t][e]);
+            for (int t = 0; t < B; ++t)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) acc[t][8 * p + e] = fmaf(h[r][t], w[e], acc[t][8 * p + e]);
           }
         }
       }
     }
-    __syncthreads();
   }
-
-  // fold the waves: thread = column of the tile
-  const int mine = tile * kTile + tid;
-  float* part = a.part + (size_t)chunk * B * d;
 #pragma unroll
   for (int t = 0; t < B; ++t) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) fold[wv][lane * 8 + e] = acc[t][e];
-    __syncthreads();
-    float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < kMW; ++w) s += fold[w][tid];
-    __syncthreads();
-    if (mine < d) {
-      if (a.chunks == 1)
-        a.y[(size_t)t * d + mine] = s;
-      else
-        st_agent(reinterpret_cast<uint32_t*>(part + (size_t)t * d + mine), __float_as_uint(s));
-    }
-  }
-  if (a.chunks == 1) return;
-  wait_own_stores();
-  __syncthreads();
-  if (tid == 0) {
-    const uint32_t before = __hip_atomic_fetch_add(&a.done[tile], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    s_last = before == (uint32_t)a.chunks - 1u;
-    if (s_last) st_agent(&a.done[tile], 0u);
+    const float s = lanes_total<kMCols>(acc[t], lane);
+    if (lane < kMCols) fold[wv][t][lane] = s;
   }
   __syncthreads();
-  if (!s_last || mine >= d) return;
-#pragma unroll
-  for (int t = 0; t < B; ++t) {
+  if (tid < B * kMCols) {
+    const int t = tid / kMCols, e = tid % kMCols;
     float s = 0.f;
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(a.part) + (size_t)t * d + mine;
-#pragma unroll 8
-    for (int q = 0; q < a.chunks; ++q) s += __uint_as_float(ld_agent(p + (size_t)q * B * d));
-    a.y[(size_t)t * d + mine] = s;
+#pragma unroll
+    for (int w = 0; w < kMW; ++w) s += fold[w][t][e];
+    a.y[(size_t)t * a.d + col + e] = s;
   }
 }
 
@@ -457,13 +482,13 @@ static hipError_t mlp_b(const MxArgs& a, hipStream_t s) {
                  : nu <= 3 ? rows_launch<B, 3>(a, s) : rows_launch<B, 4>(a, s);
   if (e != hipSuccess) return e;
   const bool lists = a.idx || a.n_out || a.counters;
-  k_mx_down<B><<<a.tiles * a.chunks + (lists ? 1 : 0), kMT, 0, s>>>(a);
+  k_mx_down<B><<<a.tiles + (lists ? 1 : 0), kMT, 0, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_mx_mlp(const MxMlpCall& c, hipStream_t s) {
   const WsLayout L = ws_layout(c.k, c.b);
-  const MxWs M = mx_ws(c.k, c.d, c.b);
+  const MxWs M = mx_ws(c.k, c.b);
   char* base = static_cast<char*>(c.ws);
   MxArgs a;
   a.signs = reinterpret_cast<const u32x4*>(c.signs);
@@ -483,17 +508,15 @@ hipError_t launch_mx_mlp(const MxMlpCall& c, hipStream_t s) {
   a.flags = c.flags;
   a.hdr = reinterpret_cast<uint32_t*>(base);
   a.kmask = reinterpret_cast<uint32_t*>(base + M.kmask);
+  a.dmask = reinterpret_cast<uint32_t*>(base + M.dmask);
   a.counts = reinterpret_cast<int32_t*>(base + M.counts);
-  a.done = a.hdr + kHdrDone;
-  a.part = reinterpret_cast<float*>(base + M.part);
   a.h3 = reinterpret_cast<float*>(base + L.h3);
   a.y = c.y;
   a.idx = c.idx;
   a.n_out = c.n_out;
   a.counters = c.counters;
   a.groups = mx_groups(c.k);
-  a.tiles = mx_tiles(c.d);
-  a.chunks = mx_chunks(c.k, c.d);
+  a.tiles = c.d / kMCols;
   switch (c.b) {
     case 1: return mlp_b<1>(a, s);
     case 2: return mlp_b<2>(a, s);
