@@ -54,16 +54,15 @@ __device__ inline void load8(const void* w, size_t base, int c8, int n, float (&
   if (c8 + 8 <= n) {
     if constexpr (DT == kF32) {
       const float* p = static_cast<const float*>(w) + base + c8;
-      const u32x4 a = __builtin_nontemporal_load(reinterpret_cast<const u32x4_e4*>(p));
-      const u32x4 b = __builtin_nontemporal_load(reinterpret_cast<const u32x4_e4*>(p + 4));
+      const u32x4 a = *reinterpret_cast<const u32x4_e4*>(p);
+      const u32x4 b = *reinterpret_cast<const u32x4_e4*>(p + 4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         f[i] = __uint_as_float(a[i]);
         f[4 + i] = __uint_as_float(b[i]);
       }
     } else {
-      const u32x4 a = __builtin_nontemporal_load(
-          reinterpret_cast<const u32x4_e2*>(static_cast<const uint16_t*>(w) + base + c8));
+      const u32x4 a = *reinterpret_cast<const u32x4_e2*>(static_cast<const uint16_t*>(w) + base + c8);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if constexpr (DT == kBF16) {
@@ -133,7 +132,7 @@ __global__ __launch_bounds__(kQT) void k_dequantize_mx(const uint32_t* __restric
   for (int u = 0; u < kUnits; ++u) {
     p[u] = piece_of(first, threadIdx.x + kQT * u, per, row0, c0);
     if (p[u].row < rows) {
-      c[u] = __builtin_nontemporal_load(q + p[u].row * per + p[u].c);
+      c[u] = q[p[u].row * per + p[u].c];
       b[u] = scale[p[u].row * (per / 4) + (p[u].c >> 2)];
     }
   }

@@ -11,12 +11,14 @@
 // value is positive.  h3 goes to the workspace, and a bit for each row whose h3 is
 // not 0 for every token.
 //
-// k_mx_down: a block owns 16 columns of y over all rows: it lists the rows whose bit
-// is set and its threads take one each, 8 bytes of codes (neighbouring columns lie
-// on the same XCD, so a row's line is fetched into one L2 and used by 16 blocks
-// there).  The threads' sums meet in registers and LDS in a fixed order: no partial
+// k_mx_down: a block owns 32 columns of y (16 with 5 to 8 tokens) over all rows: it
+// lists the rows whose bit is set and its threads take one each, 16 bytes of codes
+// (neighbouring columns lie on the same XCD, so a row's line is fetched into one L2
+// and used by 8 blocks there).  The threads' sums meet in registers and LDS in a fixed order: no partial
 // sums in memory, no atomics, and y is the same bits in every run.
 //
+#include <type_traits>
+
 #include "layer_common.h"
 #include "mx.h"
 #include "mx_launch.h"
@@ -26,7 +28,9 @@ namespace si {
 constexpr int kMG = 32;      // rows of a block of k_mx_rows
 constexpr int kMW = 8;       // waves of a block
 constexpr int kMT = kMW * kWave;
-constexpr int kMCols = 16;   // columns of y of a block of k_mx_down
+// columns of y of a block of k_mx_down: one scale's where the sums of that many
+// fit the registers (5120 wide, 1700 rows, one token: 11.7 us with 16, ... with 32)
+constexpr int down_cols(int b) { return b <= 4 ? 32 : 16; }
 constexpr int kSignUnits = kMaxD / 128 / (2 * kMW);  // sign units of a lane (4)
 
 inline __host__ __device__ int mx_groups(int k) { return (k + kMG - 1) / kMG; }
@@ -67,7 +71,7 @@ __device__ inline void mx_load_row(const u32x4* __restrict__ q, const uint8_t* _
 #pragma unroll
   for (int j = 0; j < NU; ++j) {
     const int u = min(lane + kWave * j, U - 1);
-    r.c[j] = load_nt(qr + u);
+    r.c[j] = qr[u];
     r.s[j] = sr[u];
   }
 }
@@ -157,7 +161,7 @@ __global__ __launch_bounds__(kMT) void k_mx_rows(MxArgs a) {
 #pragma unroll
     for (int i = 0; i < kSignUnits; ++i) {
       const int q = 2 * wv + (lane >> 5) + 2 * kMW * i;
-      if (q < units) sg[i] = load_nt(p + (size_t)q * kpad);
+      if (q < units) sg[i] = p[(size_t)q * kpad];
     }
   }
   // tokens to LDS with their sign bits (a byte for 8 values), all of a thread's
@@ -374,24 +378,27 @@ __device__ inline float lanes_total(float (&v)[N], int lane) {
 
 template <int B>
 __global__ __launch_bounds__(kMT) void k_mx_down(MxArgs a) {
+  constexpr int CB = down_cols(B), CW = CB / 8;  // columns, words of codes
   __shared__ uint16_t rows[kDownSpan];
-  __shared__ float fold[kMW][B][kMCols];
+  __shared__ float fold[kMW][B][CB];
   __shared__ int wsum[kMW];
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   if ((int)blockIdx.x == a.tiles) {
     mx_lists(a, wsum);
     return;
   }
-  // each XCD a run of neighbouring tiles (their number is a multiple of 8)
-  const int tile = (blockIdx.x & 7) * (a.tiles >> 3) + (blockIdx.x >> 3);
-  const int U = a.d >> 5, col = tile * kMCols;
-  const u32x2* qd = reinterpret_cast<const u32x2*>(a.qd) + (col >> 4);
+  // each XCD a run of neighbouring tiles where their number allows
+  int tile = blockIdx.x;
+  if (a.tiles % 8 == 0) tile = (tile & 7) * (a.tiles >> 3) + (tile >> 3);
+  const int U = a.d >> 5, col = tile * CB;
+  typedef std::conditional_t<CW == 4, u32x4, u32x2> codes_t;
+  const codes_t* qd = reinterpret_cast<const codes_t*>(a.qd) + tile;
   const uint8_t* sd = a.sd + (col >> 5);
-  float acc[B][kMCols];
+  float acc[B][CB];
 #pragma unroll
   for (int t = 0; t < B; ++t)
 #pragma unroll
-    for (int e = 0; e < kMCols; ++e) acc[t][e] = 0.f;
+    for (int e = 0; e < CB; ++e) acc[t][e] = 0.f;
 
   for (int g0 = 0; g0 < a.groups; g0 += kMT) {
     uint32_t bits = g0 + tid < a.groups ? a.dmask[g0 + tid] : 0u;
@@ -409,22 +416,33 @@ __global__ __launch_bounds__(kMT) void k_mx_down(MxArgs a) {
     __syncthreads();
     // a thread takes every 512th row
     for (int i0 = tid; i0 < n; i0 += kMT * kDownUnroll) {
-      u32x2 c[kDownUnroll];
+      codes_t c[kDownUnroll];
       uint32_t s[kDownUnroll];
       float h[kDownUnroll][B];
 #pragma unroll
       for (int r = 0; r < kDownUnroll; ++r) {
         const int i = i0 + kMT * r;
-        c[r] = u32x2{0, 0};
+        c[r] = codes_t{};
         s[r] = 0;
 #pragma unroll
         for (int t = 0; t < B; ++t) h[r][t] = 0.f;
         if (i < n) {
           const size_t row = (size_t)g0 * kMG + rows[i];
-          c[r] = qd[row * (U * 2)];
+          c[r] = qd[row * (U * 4 / CW)];
           s[r] = sd[row * U];
+          const float* p = a.h3 + row * B;
 #pragma unroll
-          for (int t = 0; t < B; ++t) h[r][t] = a.h3[row * B + t];
+          for (int t = 0; t < B; t += 4) {
+            if constexpr (B >= 4) {
+              const int o = t < B - 3 ? t : B - 4;  // the last four overlap where B is no multiple
+              const u32x4 v = *reinterpret_cast<const u32x4_e4*>(p + o);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) h[r][o + e] = __uint_as_float(v[e]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < B; ++e) h[r][e] = p[e];
+            }
+          }
         }
       }
 #pragma unroll
@@ -432,7 +450,7 @@ __global__ __launch_bounds__(kMT) void k_mx_down(MxArgs a) {
         if (i0 + kMT * r < n) {
           const float sc = mx_scale(s[r]);
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
+          for (int p = 0; p < CW; ++p) {
             const f32x2 w0 = mx_f32x2<0>(c[r][p], sc), w1 = mx_f32x2<1>(c[r][p], sc), w2 = mx_f32x2<2>(c[r][p], sc),
                         w3 = mx_f32x2<3>(c[r][p], sc);
             const float w[8] = {w0.x, w0.y, w1.x, w1.y, w2.x, w2.y, w3.x, w3.y};
@@ -447,12 +465,12 @@ __global__ __launch_bounds__(kMT) void k_mx_down(MxArgs a) {
   }
 #pragma unroll
   for (int t = 0; t < B; ++t) {
-    const float s = lanes_total<kMCols>(acc[t], lane);
-    if (lane < kMCols) fold[wv][t][lane] = s;
+    const float s = lanes_total<CB>(acc[t], lane);
+    if (lane < CB) fold[wv][t][lane] = s;
   }
   __syncthreads();
-  if (tid < B * kMCols) {
-    const int t = tid / kMCols, e = tid % kMCols;
+  if (tid < B * CB) {
+    const int t = tid / CB, e = tid % CB;
     float s = 0.f;
 #pragma unroll
     for (int w = 0; w < kMW; ++w) s += fold[w][t][e];
@@ -516,7 +534,7 @@ hipError_t launch_mx_mlp(const MxMlpCall& c, hipStream_t s) {
   a.n_out = c.n_out;
   a.counters = c.counters;
   a.groups = mx_groups(c.k);
-  a.tiles = c.d / kMCols;
+  a.tiles = c.d / down_cols(c.b);
   switch (c.b) {
     case 1: return mlp_b<1>(a, s);
     case 2: return mlp_b<2>(a, s);

@@ -6,8 +6,8 @@
 //
 // Bound by memory: h and b are read once and stay in registers as float between
 // the two reductions, h' and x are written once; x is formed from the unrounded
-// h'.  GT threads take a row, U pieces of 8 values each, so a row's requests are
-// all in flight before the first sum.
+// h'.  A row's requests are all in flight before the first sum.
+#include "layer_common.h"
 #include "mx.h"
 #include "mx_launch.h"
 
@@ -21,18 +21,18 @@ struct Raw8 {
 
 // VEC: piece p of a row is its values 8 p .. 8 p + 7, whole (d, strides and
 // addresses allow 16-byte requests).  Otherwise value e of a thread's piece u is
-// row value i = t + GT (8 u + e), so that neighbouring lanes read neighbouring
+// row value i = t + gt (8 u + e), so that neighbouring lanes read neighbouring
 // values of rows that start anywhere.
-template <bool VEC, int GT>
-__device__ inline int index_of(int t, int u, int e) {
-  return VEC ? (t + GT * u) * 8 + e : t + GT * (8 * u + e);
+template <bool VEC>
+__device__ inline int index_of(int t, int gt, int u, int e) {
+  return VEC ? (t + gt * u) * 8 + e : t + gt * (8 * u + e);
 }
 
-template <bool VEC, int GT>
-__device__ inline Raw8 load_raw(const void* p, size_t base, int dt, int t, int u, int d) {
+template <bool VEC>
+__device__ inline Raw8 load_raw(const void* p, size_t base, int dt, int t, int gt, int u, int d) {
   Raw8 r = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}};
   if constexpr (VEC) {
-    const int i = (t + GT * u) * 8;
+    const int i = (t + gt * u) * 8;
     if (i < d) {
       if (dt == kF32) {
         const u32x4* q = reinterpret_cast<const u32x4*>(static_cast<const float*>(p) + base + i);
@@ -47,7 +47,7 @@ __device__ inline Raw8 load_raw(const void* p, size_t base, int dt, int t, int u
       const float* q = static_cast<const float*>(p) + base;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = index_of<VEC, GT>(t, u, e), j = index_of<VEC, GT>(t, u, 4 + e);
+        const int i = index_of<VEC>(t, gt, u, e), j = index_of<VEC>(t, gt, u, 4 + e);
         if (i < d) r.a[e] = __float_as_uint(q[i]);
         if (j < d) r.b[e] = __float_as_uint(q[j]);
       }
@@ -55,7 +55,7 @@ __device__ inline Raw8 load_raw(const void* p, size_t base, int dt, int t, int u
       const uint16_t* q = static_cast<const uint16_t*>(p) + base;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = index_of<VEC, GT>(t, u, 2 * e), j = index_of<VEC, GT>(t, u, 2 * e + 1);
+        const int i = index_of<VEC>(t, gt, u, 2 * e), j = index_of<VEC>(t, gt, u, 2 * e + 1);
         uint32_t v = i < d ? q[i] : 0u;
         if (j < d) v |= (uint32_t)q[j] << 16;
         r.a[e] = v;
@@ -87,10 +87,10 @@ __device__ inline void to_floats(const Raw8& r, int dt, float (&f)[8]) {
   }
 }
 
-template <bool VEC, int GT>
-__device__ inline void store8(void* p, size_t base, int dt, int t, int u, int d, const float (&f)[8]) {
+template <bool VEC>
+__device__ inline void store8(void* p, size_t base, int dt, int t, int gt, int u, int d, const float (&f)[8]) {
   if constexpr (VEC) {
-    const int i = (t + GT * u) * 8;
+    const int i = (t + gt * u) * 8;
     if (i >= d) return;
     if (dt == kF32) {
       f32x4* q = reinterpret_cast<f32x4*>(static_cast<float*>(p) + base + i);
@@ -106,42 +106,45 @@ __device__ inline void store8(void* p, size_t base, int dt, int t, int u, int d,
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int i = index_of<VEC, GT>(t, u, e);
+      const int i = index_of<VEC>(t, gt, u, e);
       if (i < d) store_one(p, base + i, dt, f[e]);
     }
   }
 }
 
-template <int GT>
+// Sum over the threads of a row: one wave (WAVE) or the block.
+template <bool WAVE>
 __device__ inline float row_sum(float v, float* part) {
-  v = wave_sum(v);
-  if constexpr (GT > kWave) {
-    const int wv = threadIdx.x / kWave;
+  v = wave_total(v);
+  if constexpr (!WAVE) {
     __syncthreads();  // the last sum's readers are done
-    if ((threadIdx.x & (kWave - 1)) == 0) part[wv] = v;
+    if ((threadIdx.x & (kWave - 1)) == 0) part[threadIdx.x / kWave] = v;
     __syncthreads();
     v = 0.f;
-#pragma unroll
-    for (int w = 0; w < GT / kWave; ++w) v += part[w];
+    for (int w = 0; w < (int)(blockDim.x / kWave); ++w) v += part[w];
   }
   return v;
 }
 
-template <bool VEC, int GT, int U>
-__global__ __launch_bounds__(GT < 256 ? 256 : GT) void k_norm_residual(NormArgs a) {
-  constexpr int NT = GT < 256 ? 256 : GT;
-  __shared__ float part[NT / kWave];
-  const int t = threadIdx.x % GT;
-  const size_t row = (size_t)blockIdx.x * (NT / GT) + threadIdx.x / GT;
-  if (row >= a.tokens) return;  // whole waves, and only where a row is one wave's
+constexpr int kNormThreads = 512;
+
+// gt threads take a row, U pieces of 8 values each: a wave (four rows a block), or
+// the block.
+template <bool VEC, bool WAVE, int U>
+__global__ __launch_bounds__(WAVE ? 256 : kNormThreads) void k_norm_residual(NormArgs a) {
+  __shared__ float part[kNormThreads / kWave];
+  const int gt = WAVE ? kWave : (int)blockDim.x;
+  const int t = WAVE ? threadIdx.x & (kWave - 1) : threadIdx.x;
+  const size_t row = WAVE ? (size_t)blockIdx.x * 4 + threadIdx.x / kWave : blockIdx.x;
+  if (WAVE && row >= a.tokens) return;  // whole waves, which meet no barrier
   const int d = a.d;
   Raw8 hr[U], br[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) hr[u] = load_raw<VEC, GT>(a.h, row * a.ldh, a.h_dtype, t, u, d);
+  for (int u = 0; u < U; ++u) hr[u] = load_raw<VEC>(a.h, row * a.ldh, a.h_dtype, t, gt, u, d);
   float h[U][8];
   if (a.b) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) br[u] = load_raw<VEC, GT>(a.b, row * a.ldb, a.b_dtype, t, u, d);
+    for (int u = 0; u < U; ++u) br[u] = load_raw<VEC>(a.b, row * a.ldb, a.b_dtype, t, gt, u, d);
     float rs = 1.f;
     if (a.post_w) {
       float ss = 0.f;
@@ -152,7 +155,7 @@ __global__ __launch_bounds__(GT < 256 ? 256 : GT) void k_norm_residual(NormArgs 
 #pragma unroll
         for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
       }
-      rs = 1.0f / sqrtf(row_sum<GT>(ss, part) / (float)d + a.eps);
+      rs = 1.0f / sqrtf(row_sum<WAVE>(ss, part) / (float)d + a.eps);
     }
     const size_t grow = a.gate ? row / a.rows_per_gate : 0;
 #pragma unroll
@@ -160,12 +163,12 @@ __global__ __launch_bounds__(GT < 256 ? 256 : GT) void k_norm_residual(NormArgs 
       float f[8], m[8];
       to_floats(br[u], a.b_dtype, f);
       if (a.post_w) {
-        to_floats(load_raw<VEC, GT>(a.post_w, 0, kF32, t, u, d), kF32, m);
+        to_floats(load_raw<VEC>(a.post_w, 0, kF32, t, gt, u, d), kF32, m);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = f[e] * rs * m[e];
       }
       if (a.gate) {
-        to_floats(load_raw<VEC, GT>(a.gate, grow * (size_t)d, kF32, t, u, d), kF32, m);
+        to_floats(load_raw<VEC>(a.gate, grow * (size_t)d, kF32, t, gt, u, d), kF32, m);
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] *= m[e];
       }
@@ -175,7 +178,7 @@ __global__ __launch_bounds__(GT < 256 ? 256 : GT) void k_norm_residual(NormArgs 
     }
     if (a.h_out) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) store8<VEC, GT>(a.h_out, row * a.ldo, a.h_dtype, t, u, d, h[u]);
+      for (int u = 0; u < U; ++u) store8<VEC>(a.h_out, row * a.ldo, a.h_dtype, t, gt, u, d, h[u]);
     }
   } else {
 #pragma unroll
@@ -187,33 +190,38 @@ __global__ __launch_bounds__(GT < 256 ? 256 : GT) void k_norm_residual(NormArgs 
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (index_of<VEC, GT>(t, u, e) < d) ss = fmaf(h[u][e], h[u][e], ss);
-  const float rs = 1.0f / sqrtf(row_sum<GT>(ss, part) / (float)d + a.eps);
+      if (index_of<VEC>(t, gt, u, e) < d) ss = fmaf(h[u][e], h[u][e], ss);
+  const float rs = 1.0f / sqrtf(row_sum<WAVE>(ss, part) / (float)d + a.eps);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float m[8];
-    to_floats(load_raw<VEC, GT>(a.pre_w, 0, kF32, t, u, d), kF32, m);
+    to_floats(load_raw<VEC>(a.pre_w, 0, kF32, t, gt, u, d), kF32, m);
 #pragma unroll
     for (int e = 0; e < 8; ++e) m[e] *= h[u][e] * rs;
-    store8<VEC, GT>(a.x, row * a.ldx, a.x_dtype, t, u, d, m);
+    store8<VEC>(a.x, row * a.ldx, a.x_dtype, t, gt, u, d, m);
   }
-}
-
-template <bool VEC, int GT, int U>
-static hipError_t norm_launch(const NormArgs& a, hipStream_t s) {
-  constexpr int NT = GT < 256 ? 256 : GT;
-  constexpr size_t rows = NT / GT;
-  k_norm_residual<VEC, GT, U><<<(unsigned)((a.tokens + rows - 1) / rows), NT, 0, s>>>(a);
-  return hipGetLastError();
 }
 
 template <bool VEC>
 static hipError_t norm_shape(const NormArgs& a, hipStream_t s) {
-  if (a.d <= 512) return norm_launch<VEC, 64, 1>(a, s);
-  if (a.d <= 2048) return norm_launch<VEC, 256, 1>(a, s);
-  if (a.d <= 4096) return norm_launch<VEC, 512, 1>(a, s);
-  if (a.d <= 8192) return norm_launch<VEC, 512, 2>(a, s);
-  return norm_launch<VEC, 512, 4>(a, s);
+  const int pieces = (a.d + 7) / 8;
+  if (pieces <= kWave) {
+    k_norm_residual<VEC, true, 1><<<(unsigned)((a.tokens + 3) / 4), 256, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  // as many pieces a thread as 512 threads need, then no more threads than that
+  // takes (5120 values: 320 threads of 2 pieces)
+  const int u = (pieces + kNormThreads - 1) / kNormThreads;
+  const int per = u <= 1 ? 1 : u <= 2 ? 2 : 4;
+  const unsigned threads = (unsigned)((pieces + per - 1) / per + kWave - 1) / kWave * kWave;
+  const unsigned grid = (unsigned)a.tokens;
+  if (per == 1)
+    k_norm_residual<VEC, false, 1><<<grid, threads, 0, s>>>(a);
+  else if (per == 2)
+    k_norm_residual<VEC, false, 2><<<grid, threads, 0, s>>>(a);
+  else
+    k_norm_residual<VEC, false, 4><<<grid, threads, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 hipError_t launch_norm_residual(const NormArgs& a, hipStream_t s) {
