@@ -11,6 +11,8 @@ the device of their tensors.
 
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import _lib
@@ -418,10 +420,18 @@ def _call_on(index: int, name: str, *args) -> None:
     """``name(*args, stream)`` on the current stream of device ``index``, which
     need not be the current one."""
     if index == _current_device():
-        _lib.call(name, *args, _stream())
+        _lib.call(name, *args, _raw_stream(index) if _raw_stream is not None else _stream())
     else:
         with torch.cuda.device(index):
             _lib.call(name, *args, _stream())
+
+
+@functools.lru_cache(maxsize=4096)
+def _product_workspace(aligned, ldx: int, m: int, rows: int, n: int, gated: bool) -> int:
+    """``si_linear_mxfp4_workspace_bytes`` for activations at an address that is a
+    multiple of 16 or not (None: MXFP4 activations)."""
+    address = None if aligned is None else 16 if aligned else 18
+    return int(_lib.load().si_linear_mxfp4_workspace_bytes(address, ldx, m, rows, n, gated))
 
 
 def _same_device(*tensors) -> int:
@@ -538,8 +548,7 @@ def _product(name, x, x_args, ldx, m, n, weights, out_dtype, *more):
         raise TypeError(f"out_dtype {out_dtype}, expected one of {sorted(map(str, _ANY))}")
     index = _same_device(x, *weights, *more)
     y = x.new_empty((m, rows), dtype=out_dtype)
-    half = x_args[0] if len(x_args) == 3 else None
-    nbytes = (_lib._lib or _lib.load()).si_linear_mxfp4_workspace_bytes(half, ldx, m, rows, n, up)
+    nbytes = _product_workspace(x_args[0] & 15 == 0 if len(x_args) == 3 else None, ldx, m, rows, n, up)
     ws = x.new_empty((nbytes,), dtype=torch.uint8).data_ptr() if nbytes else None
     _call_on(index, name, *x_args, m, n, *(None if t is None else t.data_ptr() for t in weights), rows, y.data_ptr(),
              _DTYPE[out_dtype], ws, nbytes)

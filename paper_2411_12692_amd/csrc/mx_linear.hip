@@ -566,10 +566,10 @@ struct Shape {
   int br, bt, sk;
 };
 constexpr Shape kHalfTiles[] = {{32, 16, 4},  {64, 16, 4},  {128, 16, 2}, {64, 32, 4},  {128, 32, 2},
-                                {128, 48, 2}, {128, 64, 2}, {256, 64, 2}, {256, 128, 1}};
+                                {128, 48, 2}, {128, 64, 2}, {256, 64, 2}, {256, 64, 1}};
 constexpr Shape kMxTiles[] = {{32, 16, 8},  {64, 16, 8},   {64, 32, 4},   {64, 64, 4},
-                              {128, 64, 4}, {128, 128, 4}, {256, 128, 2}, {256, 256, 2}};
-constexpr int kHalfCount = sizeof kHalfTiles / sizeof *kHalfTiles, kMxCount = sizeof kMxTiles / sizeof *kMxTiles;
+                              {128, 64, 4}, {128, 128, 4}, {128, 128, 2}, {256, 256, 2}};
+constexpr int kHalfSmall = 8, kMxSmall = 6;  // those for at most a block a compute unit
 constexpr long kBlocks = 256;  // compute units
 
 struct Plan {
@@ -585,9 +585,14 @@ int act_of(const MxLinear& c) { return c.xq ? kActMx : c.x_dtype == kBF16 ? kAct
 // streams, so the smallest tile whose blocks are at most the compute units is
 // the fastest (4096 x 4096, 64 tokens, us: 64 x 16 in 256 blocks 7.9, 64 x 32 in
 // 128 10.8, 64 x 64 in 64 16.8; 11008 x 4096, 128 tokens: 128 x 64 in 172 blocks
-// 23.5, 64 x 32 in 688 28.8).  Products too large for that take the largest tile,
-// or for up to 64 tokens the one that pads them least, with the most rows.  Fewer than
-// half as many blocks with a long n share it out (4096 x 11008, 16 tokens: 12.8
+// 23.5, 64 x 32 in 688 28.8).  Products too large for that take tiles two of which
+// share a compute unit, so that one's products cover the other's waits (256 x 64
+// against one 256 x 128: 4096 x 4096, 4096 tokens, 117 against 121, 11008 x 4096,
+// 700 tokens, 65 against 116), and with 4-bit activations 256 x 256 where those
+// fill three quarters of their rounds (13824 x 5120, 4096 tokens: 200 against 208
+// with 128 x 128; 4096 x 4096, 2048 tokens, half a round: 41 against 28).  With up
+// to 64 tokens they take the tile that pads them least, with the most rows.
+// Fewer than half as many blocks with a long n share it out (4096 x 11008, 16 tokens: 12.8
 // in one part, 12.1 in two; 512 x 11008, 10 tokens: 14.7 / 10.2 in four), at the
 // price of a second launch, so only where a part keeps five stages.
 // k_mx_skinny takes 16 rows a block: up to 4 tokens over at most 256 blocks, both
@@ -603,17 +608,21 @@ Plan plan_of(const MxLinear& c) {
   p.tile = -1;
   if (c.m > kSToks || (long)c.rows * mats > 16 * kBlocks) {
     const Shape* tiles = act == kActMx ? kMxTiles : kHalfTiles;
-    const int count = act == kActMx ? kMxCount : kHalfCount;
+    const int small = act == kActMx ? kMxSmall : kHalfSmall;
     auto blocks = [&](const Shape& t) {
       return (long)((c.rows + t.br / mats - 1) / (t.br / mats)) * ((c.m + t.bt - 1) / t.bt);
     };
-    for (int i = 0; i < count && p.tile < 0; ++i)
+    for (int i = 0; i < small && p.tile < 0; ++i)
       if (blocks(tiles[i]) <= kBlocks) p.tile = i;
     if (p.tile < 0) {
-      p.tile = count - 1;
-      if (c.m <= 64)
-        for (int i = 0; i < count; ++i)
+      p.tile = small;
+      if (c.m <= 64) {
+        for (int i = 0; i < small; ++i)
           if (tiles[i].bt >= c.m && tiles[i].bt <= tiles[p.tile].bt) p.tile = i;
+      } else if (act == kActMx) {
+        const long b = blocks(tiles[small + 1]), rounds = (b + kBlocks - 1) / kBlocks;
+        if (4 * b >= 3 * rounds * kBlocks) p.tile = small + 1;
+      }
     }
     const Shape& t = tiles[p.tile];
     const long n_blocks = blocks(t), stages = np / kMxPad / t.sk;
@@ -668,7 +677,7 @@ hipError_t linear_launch(const LinArgs& a, const Plan& p, hipStream_t s) {
       SI_TILE(3, kMxTiles, 2, 2, 2, 3)
       SI_TILE(4, kMxTiles, 2, 2, 2, 3)
       SI_TILE(5, kMxTiles, 2, 2, 2, 2)
-      SI_TILE(6, kMxTiles, 4, 2, 1, 2)
+      SI_TILE(6, kMxTiles, 2, 2, 1, 2)
       SI_TILE(7, kMxTiles, 2, 4, 1, 2)
     }
   } else {
@@ -681,7 +690,7 @@ hipError_t linear_launch(const LinArgs& a, const Plan& p, hipStream_t s) {
       SI_TILE(5, kHalfTiles, 4, 1, 2, 3)
       SI_TILE(6, kHalfTiles, 4, 1, 2, 3)
       SI_TILE(7, kHalfTiles, 4, 1, 2, 2)
-      SI_TILE(8, kHalfTiles, 4, 2, 1, 2)
+      SI_TILE(8, kHalfTiles, 4, 1, 1, 2)
     }
   }
 #undef SI_TILE
@@ -699,10 +708,12 @@ hipError_t linear_mats(const LinArgs& a, const Plan& p, hipStream_t s) {
 }  // namespace
 
 bool mx_linear_fits(const MxLinear& c) {
-  // tiles of at least 128 x 16 past 256 blocks and the copy: fewer than 2^32
-  // threads a launch
-  const double tiles = ((double)c.rows / 64 + 1) * ((double)c.m / (c.m > 64 ? 128 : 16) + 1);
-  return tiles * 512 < 4294967296.0 && (double)c.m * (mx_padded(c.n) / 8) < 4294967296.0;
+  // past 256 blocks, and with half the rows where there are two matrices: from 65
+  // tokens tiles of at least 64 x 64 and 256 threads, else of 32 x 16 and 512; and
+  // the copy: fewer than 2^32 threads a launch
+  const double r = c.rows, m = c.m;
+  const double threads = c.m > 64 ? (r / 64 + 1) * (m / 64 + 1) * 256 : (r / 32 + 1) * (m / 16 + 1) * 512;
+  return threads < 4294967296.0 && m * (mx_padded(c.n) / 8) < 4294967296.0;
 }
 
 size_t mx_linear_workspace(const MxLinear& c) {
