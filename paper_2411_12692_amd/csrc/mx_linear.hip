@@ -184,6 +184,8 @@ struct Tile {
   static constexpr int WRow = 64 * SK;                      // bytes of a row's codes in a stage
   static constexpr int XRow = ACT == kActMx ? 64 * SK : 256 * SK;
   static constexpr int SRow = 4 * SK;                       // bytes of a row's scales
+  // pieces from one lane group's to the next one's
+  static constexpr int WDelta = ACT == kActMx ? 2 : 1, XDelta = ACT == kActMx ? 2 : 4;
   static constexpr int WBytes = BR * WRow, XBytes = BT * XRow;
   static constexpr int WsBytes = BR * SRow, XsBytes = ACT == kActMx ? BT * SRow : 0;
   static constexpr int Bytes = WBytes + XBytes + WsBytes + XsBytes;
@@ -212,16 +214,17 @@ __device__ inline void wait_stage() {
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef const __attribute__((address_space(1))) uint8_t glb_u8;
 
-// Where 16-byte piece p of row r of a stage lies in its row: rows that share
-// banks hold their pieces in different places.
-template <int ROW>
+// Where 16-byte piece p of row r of a stage lies in its row.  A read of 16 bytes a
+// lane is served 16 lanes at a time, and those are not neighbours: lanes 0-3,
+// 12-15, 20-23 and 24-27 go together (4-11, 16-19 and 28-31 next, and so on), that
+// is rows 0-3 and 12-15 for one lane group and rows 4-11 for the next, whose piece
+// lies DELTA (a power of two) further.  With DELTA taken back for rows 4-11 the 16
+// rows' pieces cover all 64 banks.  (Rows in plain order instead, as 16 neighbours
+// would want them: two lanes to a bank in each of these reads.)
+template <int ROW, int DELTA>
 __device__ inline int swizzle(int r, int p) {
-  if constexpr (ROW == 64)
-    return p ^ ((r >> 1) & 3);
-  else if constexpr (ROW == 128)
-    return p ^ (r & 7);
-  else
-    return p ^ (r & 15);
+  const int base = ROW == 64 ? (r >> 2) & 3 : ROW == 128 ? (r >> 1) & 7 : r & 15;
+  return p ^ base ^ ((((r >> 2) ^ (r >> 3)) & 1) * DELTA);
 }
 
 template <int ACT, int MATS, int BR, int BT, int WR, int WT, int WK, int ST>
@@ -254,14 +257,14 @@ __global__ __launch_bounds__(WR* WT* WK* kWave) void k_mx_tile(LinArgs a) {
     const int r = (wv + NW * i) * LW + lane / (64 / LW);  // row of the tile
     const int mat = r / (BR / MATS);
     const int rr = min(row0 + r % (BR / MATS), a.rows - 1) - row0;
-    ow[i] = (uint32_t)(rr * (int)pitch_q) + 16 * swizzle<P::WRow>(r, lane % (64 / LW));
+    ow[i] = (uint32_t)(rr * (int)pitch_q) + 16 * swizzle<P::WRow, P::WDelta>(r, lane % (64 / LW));
     bw[i] = a.q[MATS == 2 ? uniform(mat) : 0] + (size_t)row0 * pitch_q;
   }
 #pragma unroll
   for (int i = 0; i < P::IX / NW; ++i) {
     const int r = (wv + NW * i) * LX + lane / (64 / LX);
     const int rr = min(tok0 + r, a.m - 1) - tok0;
-    ox[i] = (uint32_t)rr * (uint32_t)a.ldx + 16 * swizzle<P::XRow>(r, lane % (64 / LX));
+    ox[i] = (uint32_t)rr * (uint32_t)a.ldx + 16 * swizzle<P::XRow, P::XDelta>(r, lane % (64 / LX));
   }
   const uint8_t* bx = static_cast<const uint8_t*>(a.x) + (size_t)tok0 * a.ldx;
   constexpr int NS = P::NS, MS = P::MS;  // scale requests of a stage; waves without one repeat another's
@@ -331,12 +334,12 @@ __global__ __launch_bounds__(WR* WT* WK* kWave) void k_mx_tile(LinArgs a) {
 #pragma unroll
         for (int t = 0; t < T; ++t) {
           const int row = wt * (BT / WT) + t * 16 + r;
-          x[t] = *reinterpret_cast<const u32x4*>(xl + row * P::XRow + 16 * swizzle<P::XRow>(row, 8 * wk + 2 * g + s));
+          x[t] = *reinterpret_cast<const u32x4*>(xl + row * P::XRow + 16 * swizzle<P::XRow, P::XDelta>(row, 8 * wk + 2 * g + s));
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
           const int row = piece_row(i) + r;
-          w[i] = *reinterpret_cast<const u32x4*>(wl + row * P::WRow + 16 * swizzle<P::WRow>(row, 8 * wk + 2 * g + s));
+          w[i] = *reinterpret_cast<const u32x4*>(wl + row * P::WRow + 16 * swizzle<P::WRow, P::WDelta>(row, 8 * wk + 2 * g + s));
         }
       };
       read(0);
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(WR* WT* WK* kWave) void k_mx_tile(LinArgs a) {
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         const int row = piece_row(i) + r;
-        w[i] = *reinterpret_cast<const u32x4*>(wl + row * P::WRow + 16 * swizzle<P::WRow>(row, 4 * wk + g));
+        w[i] = *reinterpret_cast<const u32x4*>(wl + row * P::WRow + 16 * swizzle<P::WRow, P::WDelta>(row, 4 * wk + g));
         sw[i] = mx_scale(sl[row * P::SRow + 4 * wk + g]);
       }
 #pragma unroll
@@ -364,7 +367,7 @@ __global__ __launch_bounds__(WR* WT* WK* kWave) void k_mx_tile(LinArgs a) {
 #pragma unroll
         for (int t = 0; t < T; ++t) {
           const int row = wt * (BT / WT) + t * 16 + r;
-          x[t] = *reinterpret_cast<const u32x4*>(xl + row * P::XRow + 16 * swizzle<P::XRow>(row, 16 * wk + 4 * g + j));
+          x[t] = *reinterpret_cast<const u32x4*>(xl + row * P::XRow + 16 * swizzle<P::XRow, P::XDelta>(row, 16 * wk + 4 * g + j));
         }
 #pragma unroll
         for (int i = 0; i < R; ++i) {
