@@ -14,9 +14,14 @@
 // k_mx_down: a block owns 32 columns of y (16 with 5 to 8 tokens) over all rows: it
 // lists the rows whose bit is set and its threads take one each, 16 bytes of codes
 // (neighbouring columns lie on the same XCD, so a row's line is fetched into one L2
-// and used by 8 blocks there).  The threads' sums meet in registers and LDS in a fixed order: no partial
-// sums in memory, no atomics, and y is the same bits in every run.
+// and used by 8 blocks there).  The threads' sums meet in registers and LDS in a
+// fixed order: no partial sums in memory, no atomics, and y is the same bits in
+// every run.  (With tiles of 512 columns by chunks of rows and partial sums 13.2 us,
+// the last block of a tile reading them alone.)
 //
+// Bound by the two launches' chains of round trips (signs, then rows; list, then
+// pieces): 7B-shaped layer, one token, s = 0.9, 6.3 + 7.4 us for 12.8 MB (2.5 us of
+// a copy's rate); with four tokens at 13B, 15.9 + 12.1, also by the dot products.
 #include <type_traits>
 
 #include "layer_common.h"
@@ -29,7 +34,9 @@ constexpr int kMG = 32;      // rows of a block of k_mx_rows
 constexpr int kMW = 8;       // waves of a block
 constexpr int kMT = kMW * kWave;
 // columns of y of a block of k_mx_down: one scale's where the sums of that many
-// fit the registers (5120 wide, 1700 rows, one token: 11.7 us with 16, ... with 32)
+// fit the registers (5120 wide, 1700 rows: one token 11.7 us with 16, 8.6 with 32,
+// four tokens 14.0 and 12.0: every block asks its L2 for every row, so fewer, wider
+// blocks ask less)
 constexpr int down_cols(int b) { return b <= 4 ? 32 : 16; }
 constexpr int kSignUnits = kMaxD / 128 / (2 * kMW);  // sign units of a lane (4)
 
