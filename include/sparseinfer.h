@@ -433,7 +433,7 @@ size_t si_mxfp4_scales_bytes(int rows, int n);
  * m = 0 gives the scale byte 0; a block with an infinity or a NaN the byte 255
  * and codes of signs alone, so that it reads back as NaN.
  *   w     : rows of n values of type w_dtype, ldw elements from row to row
- *           (ldw >= n where rows > 1), at any address that fits an element.
+ *           (n to 2^32 where rows > 1), at any address that fits an element.
  *   q, scale : written, si_mxfp4_codes_bytes / si_mxfp4_scales_bytes.
  *   rows  : 0 to 2^24 (0 does nothing); n: 1 to 2^24, any length.
  */
@@ -462,7 +462,7 @@ si_status si_pack_signs_mxfp4(const uint8_t* q_gate, int k, int d, uint32_t* sig
  *                           every row; q_up = s_up = NULL: the non-gated
  *                           max(sum_j x[t][j] W_fc1[i][j], 0).
  *   x  : m rows of n values, fp16 or bf16 (x_dtype), ldx elements from row to
- *        row (ldx >= n where m > 1), at any address that fits an element.
+ *        row (n to 2^21 where m > 1), at any address that fits an element.
  *        With fp16 activations the weights take part as their fp16 values (the
  *        values themselves for weights quantized from fp16; beyond fp16's range
  *        infinities, and multiples of 2^-24 below its normal numbers); with bf16
@@ -538,8 +538,8 @@ si_status si_predict_sparse_mlp_mxfp4(const uint32_t* signs, const uint8_t* q_ga
  *   gate     : [ceil(tokens / rows_per_gate)][d] float32: token t is multiplied
  *        with row t / rows_per_gate (rows_per_gate = tokens: one gate for all).
  *   x        : rows of type x_dtype, ldx, written.
- *   tokens 0 to 2^23 - 1 (0 does nothing), d 1 to 16384, strides >= d where
- *   tokens > 1, addresses that fit an element.  At least one of h_out and x.
+ *   tokens 0 to 2^23 - 1 (0 does nothing), d 1 to 16384, strides d to 2^32
+ *   where tokens > 1, addresses that fit an element.  At least one of h_out and x.
  *   Outputs must not overlap anything else (columns of one matrix do not).
  */
 si_status si_norm_residual(const void* h, int h_dtype, size_t ldh, const void* branch, int branch_dtype, size_t ldb,

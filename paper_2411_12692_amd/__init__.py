@@ -611,7 +611,7 @@ def _mx_mlp(q_gate, s_gate, q_up, s_up, q_down_t, s_down_t, x, y, workspace, *mo
     for q, s, name in ((q_up, s_up, "q_up"), (q_down_t, s_down_t, "q_down_t")):
         if q is None:
             continue
-        if not (q.shape == shape and s.shape == s_shape and q.dtype is torch.uint8 and s.dtype is torch.uint8
+        if s is None or not (q.shape == shape and s.shape == s_shape and q.dtype is torch.uint8 and s.dtype is torch.uint8
                 and q.is_contiguous() and s.is_contiguous()):
             _mx(q, s, name, d)
             raise ValueError(f"{name} does not match q_gate")
