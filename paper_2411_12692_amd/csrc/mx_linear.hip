@@ -199,6 +199,8 @@ struct Tile {
   // requests of a wave and stage, the same for every wave: the waits count them
   static constexpr int Requests = IW / NW + IX / NW + MS;
   static_assert(WRow <= 1024 && XRow <= 1024 && SK <= 64, "a request covers whole rows");
+  static_assert(WBytes % 1024 == 0 && XBytes % 1024 == 0 && WsBytes % 256 == 0 && XsBytes % 256 == 0, "whole requests");
+  static_assert(BR / MATS % (1024 / WRow) == 0, "a request's codes are of one matrix");
   static_assert(R % MATS == 0 && IW % NW == 0 && IX % NW == 0, "whole requests a wave");
   static_assert(Requests * (ST - 2) < 64, "what a wait can leave outstanding");
   static_assert(ST * Bytes <= kMaxLds, "LDS of a compute unit");
