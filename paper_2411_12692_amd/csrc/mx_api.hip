@@ -52,13 +52,19 @@ si_status check_ld(const char* what, size_t ld, int n, int rows, size_t max_ld) 
   return SI_OK;
 }
 
-si_status run_linear(MxLinear& c, bool gated, void* workspace, size_t workspace_bytes, void* stream) {
+// The sizes of a product, for the call and for the size of its workspace.
+si_status check_product(const MxLinear& c) {
   if (si_status s = check_rows_n("m", c.m, c.n, kMaxN)) return s;
-  if (si_status s = check_rows_n("rows", c.rows, c.n, kMaxN)) return s;
-  if (c.rows < 1) return fail(SI_ERR_SHAPE, "rows=%d outside [1, 2^24]", c.rows);
+  if (c.rows < 1 || c.rows > (1 << 24)) return fail(SI_ERR_SHAPE, "rows=%d outside [1, 2^24]", c.rows);
+  if (c.m > 0 && !mx_linear_fits(c))
+    return fail(SI_ERR_SHAPE, "m=%d rows=%d n=%d: more than one launch can hold", c.m, c.rows, c.n);
+  return SI_OK;
+}
+
+si_status run_linear(MxLinear& c, bool gated, void* workspace, size_t workspace_bytes, void* stream) {
+  if (si_status s = check_product(c)) return s;
   REQUIRE_DTYPE(c.y_dtype);
   if (c.m == 0) return SI_OK;
-  if (!mx_linear_fits(c)) return fail(SI_ERR_SHAPE, "m=%d rows=%d n=%d: more than one launch can hold", c.m, c.rows, c.n);
   const uint8_t *q_up = c.q_up, *s_up = c.s_up;
   if ((q_up == nullptr) != (s_up == nullptr)) return fail(SI_ERR_NULL, "q_up and s_up must both be given or both be NULL");
   const void* y = c.y;
@@ -205,7 +211,6 @@ si_status si_pack_signs_mxfp4(const uint8_t* q_gate, int k, int d, uint32_t* sig
 }
 
 size_t si_linear_mxfp4_workspace_bytes(const void* x, size_t ldx, int m, int rows, int n, int gated) {
-  if (check_rows_n("m", m, n, kMaxN) != SI_OK || check_rows_n("rows", rows, n, kMaxN) != SI_OK || m == 0) return 0;
   static const uint8_t some = 0;
   MxLinear c;
   c.x = x;
@@ -215,6 +220,7 @@ size_t si_linear_mxfp4_workspace_bytes(const void* x, size_t ldx, int m, int row
   c.m = m;
   c.rows = rows;
   c.n = n;
+  if (check_product(c) != SI_OK || m == 0) return 0;
   return mx_linear_workspace(c);
 }
 
