@@ -124,11 +124,11 @@ def signs_to_canonical(signs: torch.Tensor, k: int, d: int) -> torch.Tensor:
 
 
 def transpose_down(w_down: torch.Tensor) -> torch.Tensor:
-    """``W_down [d][k]`` -> ``W_down^T [k][d]`` (fp16)."""
+    """``W_down [d][k]`` -> ``W_down^T [k][d]`` (fp16), on ``w_down``'s device."""
     _dev(w_down, "w_down", _F16, 2)
     d, k = w_down.shape
     out = torch.empty(k, d, dtype=w_down.dtype, device=w_down.device)
-    _lib.call("si_transpose_down", _vp(w_down), d, k, _vp(out), _stream())
+    _call_on(w_down.get_device(), "si_transpose_down", _vp(w_down), d, k, _vp(out))
     return out
 
 
