@@ -538,7 +538,8 @@ def _product(name, x, x_args, ldx, m, n, weights, out_dtype, *more):
     """One of the four products; ``weights`` is ``q, scale`` or ``q_gate,
     s_gate, q_up, s_up``, ``more`` further tensors that have to be on ``x``'s
     device.  Scratch comes from torch's allocator, in the stream's order like any
-    tensor."""
+    tensor, and is held until the call returns: another thread may allocate while
+    the call makes its launches."""
     gated = len(weights) == 4
     rows = _mx(weights[0], weights[1], "q_gate" if gated else "q", n)
     up = gated and weights[2] is not None
@@ -549,9 +550,9 @@ def _product(name, x, x_args, ldx, m, n, weights, out_dtype, *more):
     index = _same_device(x, *weights, *more)
     y = x.new_empty((m, rows), dtype=out_dtype)
     nbytes = _product_workspace(x_args[0] & 15 == 0 if len(x_args) == 3 else None, ldx, m, rows, n, up)
-    ws = x.new_empty((nbytes,), dtype=torch.uint8).data_ptr() if nbytes else None
+    ws = x.new_empty((nbytes,), dtype=torch.uint8) if nbytes else None
     _call_on(index, name, *x_args, m, n, *(None if t is None else t.data_ptr() for t in weights), rows, y.data_ptr(),
-             _DTYPE[out_dtype], ws, nbytes)
+             _DTYPE[out_dtype], _vp(ws), nbytes)
     return y
 
 
