@@ -498,9 +498,9 @@ si_status si_gated_linear_mxfp4_a4(const uint8_t* xq, const uint8_t* x_scale, in
 size_t si_linear_mxfp4_workspace_bytes(const void* x, size_t ldx, int m, int rows, int n, int gated);
 
 /* Bytes of the workspace of the two calls below (0 for unsupported shapes): a
- * si_workspace_bytes() workspace with more behind it, under the same rules
- * (zero-filled before its first use, one call at a time); si_read_h3 and
- * si_workspace_check accept it. */
+ * si_workspace_bytes() workspace, under the same rules (zero-filled before its
+ * first use, one call at a time), which fp16, INT8 and MXFP4 calls may share;
+ * si_read_h3 and si_workspace_check accept it. */
 size_t si_mxfp4_workspace_bytes(int k, int d, int b);
 
 /*

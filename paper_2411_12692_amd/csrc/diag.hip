@@ -26,6 +26,8 @@ __global__ __launch_bounds__(1024) void k_read_h3(const uint32_t* __restrict__ h
         if (form == kH3ByRow) {
           const uint64_t w = h3e[(size_t)i * b + t];
           v = (uint32_t)(w >> 32) == tag ? __uint_as_float((uint32_t)w) : nan;
+        } else if (form == kH3Untagged) {
+          v = __uint_as_float((uint32_t)h3e[(size_t)i * b + t]);
         } else if (form == kH3PlainByRow) {
           v = h3p[(size_t)i * b + t];
         } else {

@@ -28,6 +28,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 // 16 bytes at any element boundary (rows of an odd length start anywhere)
 typedef u32x4 u32x4_e2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_e4 __attribute__((aligned(4)));
+typedef u32x4 u32x4_e8 __attribute__((aligned(8)));
 typedef u32x2 u32x2_e2 __attribute__((aligned(2)));
 
 // A scale byte as the float whose exponent field it is: the operand of the

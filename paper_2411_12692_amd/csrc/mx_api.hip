@@ -298,7 +298,7 @@ si_status mlp_impl(bool predict, const uint32_t* signs, const uint8_t* q_gate, c
   if (xa < ya + yn && ya < xa + xn) return fail(SI_ERR_ARG, "x and y overlap");
   REQUIRE_PTR(workspace);
   REQUIRE_ALIGNED(workspace);
-  const size_t need = mx_mlp_workspace(k, b);
+  const size_t need = ws_layout(k, b).total;
   if (workspace_bytes < need)
     return fail(SI_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
   MxMlpCall c;
@@ -334,7 +334,7 @@ extern "C" {
 
 size_t si_mxfp4_workspace_bytes(int k, int d, int b) {
   if (check_kd(k, d) != SI_OK || check_b(b) != SI_OK) return 0;
-  return mx_mlp_workspace(k, b);
+  return ws_layout(k, b).total;
 }
 
 si_status si_sparse_mlp_mxfp4(const uint8_t* q_gate, const uint8_t* s_gate, const uint8_t* q_up, const uint8_t* s_up,

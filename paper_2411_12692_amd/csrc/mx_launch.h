@@ -76,7 +76,6 @@ struct MxMlpCall {
   void* ws = nullptr;
   int32_t* counters = nullptr;
 };
-size_t mx_mlp_workspace(int k, int b);
 hipError_t launch_mx_mlp(const MxMlpCall& c, hipStream_t s);
 
 }  // namespace si

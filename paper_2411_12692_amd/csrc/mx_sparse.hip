@@ -9,7 +9,10 @@
 // fp32, and scaled once a block, so every scale byte is exact.  W_up is requested
 // with W_gate where the row is surely kept, otherwise only when some token's gate
 // value is positive.  h3 goes to the workspace, and a bit for each row whose h3 is
-// not 0 for every token.
+// not 0 for every token, in 64-bit words that no single-launch call takes for its
+// own (si_device.h; as plain floats, half as many bytes to gather, the 7B-shaped
+// layer's two launches took 13.1 us with one token and 30.9 with eight instead of
+// 13.4 and 31.4).
 //
 // k_mx_down: a block owns 32 columns of y (16 with 5 to 8 tokens) over all rows: it
 // lists the rows whose bit is set and its threads take one each, 16 bytes of codes
@@ -42,23 +45,10 @@ constexpr int kSignUnits = kMaxD / 128 / (2 * kMW);  // sign units of a lane (4)
 
 inline __host__ __device__ int mx_groups(int k) { return (k + kMG - 1) / kMG; }
 
-// Behind the workspace's common part, at offsets that depend on b: nothing here is
-// read before the same call wrote it.
-struct MxWs {
-  size_t kmask;   // uint32 [groups] kept rows
-  size_t dmask;   // uint32 [groups] rows whose W_down^T row is read
-  size_t counts;  // int32 [groups][2] rows whose W_up / W_down^T row was read
-  size_t total;
-};
-static MxWs mx_ws(int k, int b) {
-  MxWs L;
-  L.kmask = ws_layout(k, b).total;
-  L.dmask = L.kmask + align256((size_t)mx_groups(k) * 4);
-  L.counts = L.dmask + align256((size_t)mx_groups(k) * 4);
-  L.total = L.counts + align256((size_t)mx_groups(k) * 8);
-  return L;
-}
-size_t mx_mlp_workspace(int k, int b) { return mx_ws(k, b).total; }
+// The groups' row sets lie in the list region of the workspace (4 k bytes at an
+// offset that is the same for every b; these calls keep no list there): two words a
+// group of 32 rows, at most 16 (k / 32 + 1) bytes, which 4 k rounded up to 256 holds
+// for every k.  A set is the low half of its word.
 
 // Tokens in LDS: 8-value piece j of unit u (32 values) of token t at
 // xs[(t * 4 + j) * U + u], so that lanes with neighbouring units read
@@ -139,10 +129,9 @@ struct MxArgs {
   int k, d, T, margin;
   uint32_t flags;
   uint32_t* hdr;
-  uint32_t* kmask;
-  uint32_t* dmask;
-  int32_t* counts;
-  float* h3;
+  uint64_t* kmask;  // [groups] kept rows; high half: how many W_up rows were read
+  uint64_t* dmask;  // [groups] rows whose W_down^T row is read; high half 0
+  uint64_t* h3;     // [k][b] fp32 bits; high half 0
   float* y;
   int32_t* idx;
   int32_t* n_out;
@@ -196,7 +185,7 @@ __global__ __launch_bounds__(kMT) void k_mx_rows(MxArgs a) {
   if (tid == 0) {
     s_down = 0;
     s_up = 0;
-    if (v == 0) a.hdr[H_H3_FORM] = kH3PlainByRow;
+    if (v == 0) a.hdr[H_H3_FORM] = kH3Untagged;
   }
   __syncthreads();
   if (a.signs) {
@@ -292,7 +281,7 @@ __global__ __launch_bounds__(kMT) void k_mx_rows(MxArgs a) {
     }
 #pragma unroll
     for (int t = 0; t < B; ++t)
-      if (lane == t) a.h3[(size_t)row * B + t] = h[t];
+      if (lane == t) a.h3[(size_t)row * B + t] = __float_as_uint(h[t]);
     if (lane == 0) {
       if (nz) atomicOr(&s_down, 1u << (row - v * kMG));
       if (up) atomicAdd(&s_up, 1u);
@@ -300,12 +289,8 @@ __global__ __launch_bounds__(kMT) void k_mx_rows(MxArgs a) {
   }
   __syncthreads();
   if (tid == 0) {
-    a.kmask[v] = s_kept;
+    a.kmask[v] = (uint64_t)s_up << 32 | s_kept;
     a.dmask[v] = s_down;
-    if (a.counters) {
-      a.counts[2 * v] = (int)s_up;
-      a.counts[2 * v + 1] = __popc(s_down);
-    }
   }
 }
 
@@ -316,7 +301,8 @@ __device__ inline void mx_lists(const MxArgs& a, int* wsum) {
   int base = 0, up = 0, down = 0;
   for (int g0 = 0; g0 < a.groups; g0 += kMT) {
     const int g = g0 + tid;
-    uint32_t bits = g < a.groups ? a.kmask[g] : 0u;
+    const uint64_t word = g < a.groups ? a.kmask[g] : 0u;
+    uint32_t bits = (uint32_t)word;
     const int n = __popc(bits);
     const int incl = wave_incl_scan(n);
     if (lane == kWave - 1) wsum[wv] = incl;
@@ -334,8 +320,8 @@ __device__ inline void mx_lists(const MxArgs& a, int* wsum) {
       }
     }
     if (a.counters && g < a.groups) {
-      up += a.counts[2 * g];
-      down += a.counts[2 * g + 1];
+      up += (int)(word >> 32);
+      down += __popc((uint32_t)a.dmask[g]);
     }
     __syncthreads();
   }
@@ -408,7 +394,7 @@ __global__ __launch_bounds__(kMT) void k_mx_down(MxArgs a) {
     for (int e = 0; e < CB; ++e) acc[t][e] = 0.f;
 
   for (int g0 = 0; g0 < a.groups; g0 += kMT) {
-    uint32_t bits = g0 + tid < a.groups ? a.dmask[g0 + tid] : 0u;
+    uint32_t bits = g0 + tid < a.groups ? (uint32_t)a.dmask[g0 + tid] : 0u;
     const int incl = wave_incl_scan(__popc(bits));
     if (g0 > 0) __syncthreads();  // the last span's list is read
     if (lane == kWave - 1) wsum[wv] = incl;
@@ -437,17 +423,16 @@ __global__ __launch_bounds__(kMT) void k_mx_down(MxArgs a) {
           const size_t row = (size_t)g0 * kMG + rows[i];
           c[r] = qd[row * (U * 4 / CW)];
           s[r] = sd[row * U];
-          const float* p = a.h3 + row * B;
+          const uint64_t* p = a.h3 + row * B;
+          if constexpr (B == 1) {
+            h[r][0] = __uint_as_float((uint32_t)p[0]);
+          } else {
 #pragma unroll
-          for (int t = 0; t < B; t += 4) {
-            if constexpr (B >= 4) {
-              const int o = t < B - 3 ? t : B - 4;  // the last four overlap where B is no multiple
-              const u32x4 v = *reinterpret_cast<const u32x4_e4*>(p + o);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) h[r][o + e] = __uint_as_float(v[e]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < B; ++e) h[r][e] = p[e];
+            for (int t = 0; t < B; t += 2) {
+              const int o = t < B - 1 ? t : B - 2;  // the last two overlap where B is odd
+              const u32x4 v = *reinterpret_cast<const u32x4_e8*>(p + o);
+              h[r][o] = __uint_as_float(v.x);
+              h[r][o + 1] = __uint_as_float(v.z);
             }
           }
         }
@@ -513,7 +498,6 @@ static hipError_t mlp_b(const MxArgs& a, hipStream_t s) {
 
 hipError_t launch_mx_mlp(const MxMlpCall& c, hipStream_t s) {
   const WsLayout L = ws_layout(c.k, c.b);
-  const MxWs M = mx_ws(c.k, c.b);
   char* base = static_cast<char*>(c.ws);
   MxArgs a;
   a.signs = reinterpret_cast<const u32x4*>(c.signs);
@@ -532,15 +516,14 @@ hipError_t launch_mx_mlp(const MxMlpCall& c, hipStream_t s) {
   a.margin = c.margin;
   a.flags = c.flags;
   a.hdr = reinterpret_cast<uint32_t*>(base);
-  a.kmask = reinterpret_cast<uint32_t*>(base + M.kmask);
-  a.dmask = reinterpret_cast<uint32_t*>(base + M.dmask);
-  a.counts = reinterpret_cast<int32_t*>(base + M.counts);
-  a.h3 = reinterpret_cast<float*>(base + L.h3);
+  a.groups = mx_groups(c.k);
+  a.kmask = reinterpret_cast<uint64_t*>(base + L.idx);
+  a.dmask = a.kmask + a.groups;
+  a.h3 = reinterpret_cast<uint64_t*>(base + L.h3e);
   a.y = c.y;
   a.idx = c.idx;
   a.n_out = c.n_out;
   a.counters = c.counters;
-  a.groups = mx_groups(c.k);
   a.tiles = c.d / down_cols(c.b);
   switch (c.b) {
     case 1: return mlp_b<1>(a, s);

@@ -29,6 +29,7 @@ constexpr uint32_t kErrRow = 4u;           // kept-row index outside [0, k)
 
 // Where the last MLP call left h3 (Eq. (1) step 3) in the workspace.
 constexpr uint32_t kH3ByRow = 1u;       // h3e[row][b]: this call's tag | fp32 bits
+constexpr uint32_t kH3Untagged = 2u;    // h3e[row][b]: 0 | fp32 bits, valid on the kept rows
 constexpr uint32_t kH3PlainByRow = 3u;  // h3[row][b] fp32, valid on the kept rows
 
 constexpr int kGateUpMaxBlocks = 2048;     // grid cap of the list-driven gate/up kernel
@@ -127,7 +128,10 @@ __device__ inline uint64_t lanes_below(int lane) {
 }
 
 // Tag that marks a word as written in the call with this epoch.  The high
-// bit is always set, so a zero-filled workspace never carries a valid tag.
+// bit is always set, so a zero-filled workspace never carries a valid tag.  A
+// workspace serves calls of every kind, k and b, whose regions lie over each other:
+// what a call leaves there without a tag keeps the top bit of each aligned 64-bit
+// word clear, so that no later call takes it for one of its own words.
 __device__ inline uint32_t epoch_tag(uint32_t epoch) { return (epoch & 0x7fffffffu) | 0x80000000u; }
 
 // Wait until this wave's outstanding memory operations have completed.  The

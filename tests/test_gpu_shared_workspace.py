@@ -1,0 +1,116 @@
+"""One workspace under calls of different kinds and numbers of tokens.
+
+A single-launch call takes a 64-bit word of the workspace as published when its
+high half is the call's tag, ``0x80000000 | call counter``.  Whatever other
+calls leave there must never read as one: a 64-bit word whose top bit is clear
+cannot, whatever the counter is.
+"""
+
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2411_12692_amd as si
+from paper_2411_12692_amd import _lib, synth
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+def tokens(d, b, seed):
+    g = torch.Generator().manual_seed(seed)
+    return torch.randn(b, d, generator=g).half().to(DEV)
+
+
+def layer_weights(d, k, s=0.5, seed=1):
+    L = synth.planted_layer(d, k, s, config=seed)
+    return [t.to(DEV) for t in (L.w_gate, L.w_up, L.w_down)]
+
+
+def counter(ws):
+    return int(ws[:4].view(torch.int32).item()) & 0xffffffff
+
+
+def assert_no_tag(ws, what):
+    words = ws[:ws.numel() // 8 * 8].view(torch.int64)
+    assert not bool((words < 0).any()), what
+
+
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("d,k", [(512, 1376), (640, 65), (128, 1)])
+def test_mxfp4_calls_leave_no_tags(d, k, gated):
+    wg, wu, wd = layer_weights(d, k)
+    layer = si.MXFP4MLPLayer(wg, wu if gated else None, wd, max_batch=8)
+    every = torch.ones(k, dtype=torch.uint8, device=DEV)
+    for b in range(1, 9):
+        for mask in (None, every):
+            layer.workspace.zero_()
+            x = tokens(d, b, b)
+            if mask is None:
+                layer(x, 1.0, outputs=True)
+            else:
+                layer.sparse_mlp(x, mask, counters=True)
+            torch.cuda.synchronize()
+            assert_no_tag(layer.workspace, (b, mask is None))
+
+
+def layers(d, k):
+    wg, wu, wd = layer_weights(d, k)
+    made = {"fp16": si.MLPLayer(wg, wu, wd, 8), "int8": si.Int8MLPLayer(wg, wu, wd, 8),
+            "mxfp4": si.MXFP4MLPLayer(wg, wu, wd, 8)}
+    ws = si.new_workspace_mxfp4(k, d, 8)
+    return made, ws
+
+
+@pytest.mark.parametrize("mx_b,b", [(p, q) for p in (1, 2, 3, 5, 8) for q in (1, 2, 3, 4, 6, 8)])
+@pytest.mark.parametrize("kind", ["fp16", "int8"])
+def test_row_sets_are_not_taken_for_h3(kind, mx_b, b):
+    """MXFP4 calls whose kept rows, as a number, are the next single-launch call's
+    tag (row 31 and the counter's bits of every 32 rows): that call's y is the one
+    of a workspace of its own."""
+    d, k = 512, 1376
+    made, ws = layers(d, k)
+    every = torch.ones(k, dtype=torch.uint8, device=DEV)
+    lay, mx = made[kind], made["mxfp4"]
+    x = tokens(d, b, 7)
+    want = lay.sparse_mlp(x, every)
+    scale = want.abs().max()
+    lay.workspace = mx.workspace = ws
+    for _ in range(3):
+        now = counter(ws)
+        bits = torch.tensor([(now >> i) & 1 for i in range(31)] + [1], dtype=torch.uint8, device=DEV)
+        mx.sparse_mlp(tokens(d, mx_b, 9), bits.repeat(k // 32))
+        y = lay.sparse_mlp(x, every)
+        assert counter(ws) == now + 1
+        assert bool(((y - want).abs() <= 1e-4 * scale).all())
+        h3 = si.read_h3(ws, k, d, b, every)
+        assert not torch.isnan(h3).any()
+
+
+def test_calls_of_every_kind_in_turn():
+    """fp16, INT8 and MXFP4 calls of 1 to 8 tokens, each after each: y, and h3 read
+    back, as from a workspace of the call's own."""
+    d, k = 640, 1000
+    made, ws = layers(d, k)
+    every = torch.ones(k, dtype=torch.uint8, device=DEV)
+    want = {}
+    for (name, lay), b in itertools.product(made.items(), range(1, 9)):
+        y, (mask, *_) = lay(tokens(d, b, b), 1.0, outputs=True)
+        want[name, b] = (y, mask, si.read_h3(lay.workspace, k, d, b, mask))
+    for lay in made.values():
+        lay.workspace = ws
+    order = list(want)
+    rng = np.random.default_rng(5)
+    for _ in range(6):
+        rng.shuffle(order)
+        for name, b in order:
+            b = int(b)
+            y, (mask, *_) = made[name](tokens(d, b, b), 1.0, outputs=True)
+            y0, mask0, h30 = want[name, b]
+            assert torch.equal(mask, mask0), (name, b)
+            assert torch.equal(si.read_h3(ws, k, d, b, mask), h30), (name, b)
+            assert bool(((y - y0).abs() <= 1e-4 * y0.abs().max()).all()), (name, b)
+            assert _lib.status("si_workspace_check", ws.data_ptr(), ws.numel(), 0) == 0
