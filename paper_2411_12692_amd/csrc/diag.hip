@@ -13,8 +13,8 @@ namespace si {
 // Kept rows get the value the call published for them in this call, or NaN
 // when there is none; other rows get 0.
 __global__ __launch_bounds__(1024) void k_read_h3(const uint32_t* __restrict__ hdr, const uint64_t* __restrict__ h3e,
-                                                  const float* __restrict__ h3p, const uint8_t* __restrict__ mask,
-                                                  int k, int b, float* __restrict__ out) {
+                                                  const uint8_t* __restrict__ mask, int k, int b,
+                                                  float* __restrict__ out) {
   const uint32_t form = hdr[H_H3_FORM];
   const uint32_t tag = epoch_tag(hdr[H_EPOCH] - 1u);  // the last call's tag (each call advances the counter once)
   const float nan = __builtin_nanf("");
@@ -28,8 +28,6 @@ __global__ __launch_bounds__(1024) void k_read_h3(const uint32_t* __restrict__ h
           v = (uint32_t)(w >> 32) == tag ? __uint_as_float((uint32_t)w) : nan;
         } else if (form == kH3Untagged) {
           v = __uint_as_float((uint32_t)h3e[(size_t)i * b + t]);
-        } else if (form == kH3PlainByRow) {
-          v = h3p[(size_t)i * b + t];
         } else {
           v = nan;
         }
@@ -43,7 +41,7 @@ hipError_t launch_read_h3(const void* ws, int k, int b, const uint8_t* mask, flo
   const WsLayout L = ws_layout(k, b);
   const char* base = static_cast<const char*>(ws);
   k_read_h3<<<1, 1024, 0, s>>>(reinterpret_cast<const uint32_t*>(base), reinterpret_cast<const uint64_t*>(base + L.h3e),
-                               reinterpret_cast<const float*>(base + L.h3), mask, k, b, out);
+                               mask, k, b, out);
   return hipGetLastError();
 }
 

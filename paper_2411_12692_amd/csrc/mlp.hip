@@ -24,7 +24,7 @@ template <int B>
 __global__ __launch_bounds__(256) void k_gate_up(const u32x4* __restrict__ wg, const u32x4* __restrict__ wu,
                                                  int k, int d, const uint16_t* __restrict__ x,
                                                  const int32_t* __restrict__ idx,
-                                                 const int32_t* __restrict__ n_ptr, float* __restrict__ h3row,
+                                                 const int32_t* __restrict__ n_ptr, uint64_t* __restrict__ h3row,
                                                  uint8_t* __restrict__ upflag, int32_t* __restrict__ counts,
                                                  uint32_t* __restrict__ hdr, float* __restrict__ y,
                                                  uint32_t flags) {
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256) void k_gate_up(const u32x4* __restrict__ wg, c
   const int U = d >> 3;
   if (blockIdx.x == 0) {  // y is accumulated with atomics by k_down
     for (int i = tid; i < B * d; i += 256) y[i] = 0.f;
-    if (tid == 0) hdr[H_H3_FORM] = kH3PlainByRow;
+    if (tid == 0) hdr[H_H3_FORM] = kH3Untagged;
   }
   const int n = min(max(*n_ptr, 0), k);
   if ((int)blockIdx.x * 4 >= n) {
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256) void k_gate_up(const u32x4* __restrict__ wg, c
 template <int B>
 __global__ __launch_bounds__(kDownWaves * kWave) void k_down(
     const u32x4* __restrict__ wdt, int k, int d, const int32_t* __restrict__ idx,
-    const int32_t* __restrict__ n_ptr, const float* __restrict__ h3row, float* __restrict__ y,
+    const int32_t* __restrict__ n_ptr, const uint64_t* __restrict__ h3row, float* __restrict__ y,
     const int32_t* __restrict__ counts, int slots, int32_t* __restrict__ counters, uint32_t flags, int tiles) {
   __shared__ float red[B][kTile];
   constexpr int NT = kDownWaves * kWave;
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kDownWaves * kWave) void k_down(
       bool any = false;
 #pragma unroll
       for (int t = 0; t < B; ++t) {
-        hv[r][t] = ok ? h3row[(size_t)row * B + t] : 0.f;
+        hv[r][t] = ok ? __uint_as_float((uint32_t)h3row[(size_t)row * B + t]) : 0.f;
         any |= hv[r][t] != 0.f;
       }
       w[r] = u32x4{0, 0, 0, 0};
@@ -194,7 +194,7 @@ static hipError_t down_b(const uint16_t* w_down_t, int k, int d, const int32_t* 
   const int tiles = (d + kTile - 1) / kTile;
   const int blocks = tiles * kDownChunks + (counters ? 1 : 0);
   k_down<B><<<blocks, kDownWaves * kWave, 0, s>>>(
-      reinterpret_cast<const u32x4*>(w_down_t), k, d, idx, n_active, reinterpret_cast<const float*>(base + L.h3),
+      reinterpret_cast<const u32x4*>(w_down_t), k, d, idx, n_active, reinterpret_cast<const uint64_t*>(base + L.h3e),
       y, reinterpret_cast<const int32_t*>(base + L.counts), slots, counters, flags, tiles);
   return hipGetLastError();
 }
@@ -218,7 +218,7 @@ static hipError_t gate_up_b(const uint16_t* w_gate, const uint16_t* w_up, int k,
   *slots = blocks;
   k_gate_up<B><<<blocks, 256, lds, s>>>(
       reinterpret_cast<const u32x4*>(w_gate), reinterpret_cast<const u32x4*>(w_up), k, d, x, idx, n_active,
-      reinterpret_cast<float*>(base + L.h3), reinterpret_cast<uint8_t*>(base + L.upflag),
+      reinterpret_cast<uint64_t*>(base + L.h3e), reinterpret_cast<uint8_t*>(base + L.upflag),
       reinterpret_cast<int32_t*>(base + L.counts), reinterpret_cast<uint32_t*>(base), y, flags);
   return hipGetLastError();
 }

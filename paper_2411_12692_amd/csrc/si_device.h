@@ -30,7 +30,6 @@ constexpr uint32_t kErrRow = 4u;           // kept-row index outside [0, k)
 // Where the last MLP call left h3 (Eq. (1) step 3) in the workspace.
 constexpr uint32_t kH3ByRow = 1u;       // h3e[row][b]: this call's tag | fp32 bits
 constexpr uint32_t kH3Untagged = 2u;    // h3e[row][b]: 0 | fp32 bits, valid on the kept rows
-constexpr uint32_t kH3PlainByRow = 3u;  // h3[row][b] fp32, valid on the kept rows
 
 constexpr int kGateUpMaxBlocks = 2048;     // grid cap of the list-driven gate/up kernel
 constexpr int kMaxLayerBlocks = 1024;      // grid cap of the single-kernel path
@@ -47,8 +46,7 @@ struct WsLayout {
   size_t upflag;  // uint8 [k] 1 where the W_up row was read
   size_t zflag;   // uint64 [64] single-kernel "tile of y zeroed" flags
   size_t opub;    // uint64 [kMaxLayerBlocks][kOwnPubStride] row-owning kernel: masks and count per block
-  size_t h3;      // float [k][b] h3 per row (valid on kept rows)
-  size_t h3e;     // uint64 [groups][64][b] single-kernel h3 exchange words
+  size_t h3e;     // uint64 [groups][64][b] h3 per row (valid on kept rows), the single kernel's exchange words
   size_t total;
 };
 
@@ -71,8 +69,7 @@ __host__ __device__ inline WsLayout ws_layout(int k, int b) {
   L.upflag = L.mask + align256((size_t)k);
   L.zflag = L.upflag + align256((size_t)k);
   L.opub = L.zflag + align256(64 * sizeof(uint64_t));
-  L.h3 = L.opub + align256((size_t)kMaxLayerBlocks * kOwnPubStride * sizeof(uint64_t));
-  L.h3e = L.h3 + align256((size_t)k * b * sizeof(float));
+  L.h3e = L.opub + align256((size_t)kMaxLayerBlocks * kOwnPubStride * sizeof(uint64_t));
   L.total = L.h3e + align256(groups * kRowGroup * (size_t)b * sizeof(uint64_t));
   return L;
 }
@@ -193,11 +190,11 @@ __device__ inline void row_dot(const u32x4* __restrict__ row, const u32x4* xs, i
 // through h[] the B values h3 = ReLU(W_gate,row . x) * (W_up,row . x); the
 // W_up row is read only if some token has a positive gate value (or always
 // with no_as).  Without W_up (wu == nullptr: the non-gated ReLU MLP of
-// blocks without step 2) h3 = ReLU(W_gate,row . x).  Stores h3 per row, the
-// up-read flag, and counts the work.
+// blocks without step 2) h3 = ReLU(W_gate,row . x).  Stores h3 per row (in the
+// low halves of words without a tag), the up-read flag, and counts the work.
 template <int B>
 __device__ inline void gate_up_row(const u32x4* __restrict__ wg, const u32x4* __restrict__ wu, int row, int U,
-                                   const u32x4* xs, int lane, bool no_as, float* __restrict__ h3row,
+                                   const u32x4* xs, int lane, bool no_as, uint64_t* __restrict__ h3row,
                                    uint8_t* __restrict__ upflag, int& n_up, int& n_down) {
   float g[B];
   row_dot<B>(wg + (size_t)row * U, xs, U, lane, g);
@@ -228,7 +225,7 @@ __device__ inline void gate_up_row(const u32x4* __restrict__ wg, const u32x4* __
   n_down += (nz || no_as) ? 1 : 0;
 #pragma unroll
   for (int t = 0; t < B; ++t)
-    if (lane == t) h3row[(size_t)row * B + t] = h[t];
+    if (lane == t) h3row[(size_t)row * B + t] = __float_as_uint(h[t]);
   if (lane == 0) upflag[row] = up ? 1 : 0;
 }
 

@@ -114,3 +114,52 @@ def test_calls_of_every_kind_in_turn():
             assert torch.equal(si.read_h3(ws, k, d, b, mask), h30), (name, b)
             assert bool(((y - y0).abs() <= 1e-4 * y0.abs().max()).all()), (name, b)
             assert _lib.status("si_workspace_check", ws.data_ptr(), ws.numel(), 0) == 0
+
+
+class TestTwoLaunches:
+    """A layer with more rows than the single-launch kernel takes, except from a
+    list: the calls of two launches leave h3 of either sign in the workspace."""
+
+    d, k = 1152, 65400
+
+    @pytest.fixture(scope="class")
+    def big(self):
+        g = torch.Generator(device=DEV).manual_seed(3)
+        return [0.05 * torch.randn(*shape, generator=g, device=DEV) for shape in ((self.k, self.d),) * 3]
+
+    @pytest.fixture(scope="class")
+    def weights(self, big):
+        return [w.half() for w in big]
+
+    @pytest.mark.parametrize("b", [1, 2, 5, 8])
+    @pytest.mark.parametrize("form", ["mask", "predict", "relu"])
+    def test_calls_leave_no_tags(self, weights, form, b):
+        wg, wu, wdt = weights
+        assert _lib.load().si_single_launch(self.k, self.d, b) == 0
+        ws = si.new_workspace(self.k, self.d, 8)
+        x = tokens(self.d, b, b)
+        if form == "predict":
+            si.predict_sparse_mlp(si.pack_signs(wg), wg, wu, wdt, x, 1.0, ws, outputs=True)
+            status = 256 + (self.k + 63) // 64 * 8  # look-back words, tagged: the header and they come first
+            assert_no_tag(ws[(status + 255) // 256 * 256:], b)
+        else:
+            every = torch.ones(self.k, dtype=torch.uint8, device=DEV)
+            si.sparse_mlp(wg, wu if form == "mask" else None, wdt, x, ws, mask=every, counters=True)
+            assert_no_tag(ws, b)
+
+    @pytest.mark.parametrize("b", [1, 2, 4])
+    def test_list_call_after_a_mask_call(self, weights, b):
+        """The list call is a single launch on the same workspace, with its counter
+        still 0: h3 of the tokens whose gate value is 0 must not be its tag."""
+        every = torch.ones(self.k, dtype=torch.uint8, device=DEV)
+        idx = torch.arange(self.k, dtype=torch.int32, device=DEV)
+        n = torch.tensor([self.k], dtype=torch.int32, device=DEV)
+        x = tokens(self.d, b, 11)
+        want = si.sparse_mlp(*weights, x, si.new_workspace(self.k, self.d, b), active_idx=idx, n_active=n)
+        ws = si.new_workspace(self.k, self.d, 8)
+        si.sparse_mlp(*weights, tokens(self.d, 8, 12), ws, mask=every)
+        assert counter(ws) == 0
+        got = si.sparse_mlp(*weights, x, ws, active_idx=idx, n_active=n)
+        assert counter(ws) == 1 and bool(((got - want).abs() <= 1e-4 * want.abs().max()).all())
+        h3 = si.read_h3(ws, self.k, self.d, b, every)
+        assert not torch.isnan(h3).any()
