@@ -392,7 +392,7 @@ si_status si_norm_residual(const void* h, int h_dtype, size_t ldh, const void* b
   const Rows rh = {h, t, ldh * eh, d * eh}, rb = {branch, t, ldb * eb, d * eb}, ro = {h_out, t, ldo * eh, d * eh},
              rx = {x, t, ldx * ex, d * ex}, rp = {post_w, 1, params, params}, rg = {gate, 1, gates, gates},
              rw = {pre_w, 1, params, params};
-  const bool in_place = h_out == h && ldo == ldh;  // each value is read before it is written
+  const bool in_place = h_out == h && (ldo == ldh || tokens == 1);  // each value is read before it is written
   for (const Rows& in : {rb, rp, rg, rw})
     if (overlap(ro, in) || overlap(rx, in)) return fail(SI_ERR_ARG, "an output overlaps an input");
   if ((!in_place && overlap(ro, rh)) || overlap(rx, rh) || overlap(rx, ro))

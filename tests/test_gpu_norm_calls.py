@@ -1,0 +1,22 @@
+"""Forms of the norm and block calls beside those of the values' tests."""
+
+import pytest
+import torch
+
+import paper_2411_12692_amd as si
+from paper_2411_12692_amd import _lib
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+
+
+@pytest.mark.parametrize("ldh,ldo", [(64, 64), (64, 0), (0, 64), (64, 1000)])
+def test_one_token_in_place_at_any_stride(ldh, ldo):
+    """A single row has no next one: h_out may be h whatever the two strides say."""
+    d = 64
+    h, b = torch.randn(2, 1, d, device=DEV)
+    want, _ = si.norm_residual(h, b, scale=0.5)
+    _lib.call("si_norm_residual", h.data_ptr(), _lib.SI_F32, ldh, b.data_ptr(), _lib.SI_F32, d, None, None, 1, 0.5,
+              h.data_ptr(), ldo, None, None, _lib.SI_F32, d, 1, d, 1e-5, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(h, want)
