@@ -736,8 +736,10 @@ def _block(layer, h, norm_w, eps, alpha, flags, outputs, y, post_norm_w, gate, s
         _dev(y, "y", (torch.float32,))
         if y.numel() != h2.numel():
             raise ValueError(f"y must hold [{h2.shape[0]}][{layer.d}] floats")
-        y = y.view(h2.shape)
-    out, _ = norm_residual(h2, branch, post_w=post_norm_w, gate=gate, scale=scale, eps=eps, out=y)
+    out, _ = norm_residual(h2, branch, post_w=post_norm_w, gate=gate, scale=scale, eps=eps,
+                           out=None if y is None else y.view(h2.shape))
+    if y is not None:
+        out = y
     return (out, res[1]) if outputs else out
 
 
