@@ -497,6 +497,14 @@ si_status si_gated_linear_mxfp4_a4(const uint8_t* xq, const uint8_t* x_scale, in
  * unsupported shapes and where none is needed.  Host-only. */
 size_t si_linear_mxfp4_workspace_bytes(const void* x, size_t ldx, int m, int rows, int n, int gated);
 
+/*
+ * Diagnostic, host-only: which kernel a product of these sizes takes (`a4`
+ * nonzero: one of the _a4 forms; `gated` as above).  -1: the one for a few tokens
+ * and rows; 0 and up: the place of its tile in the library's list for that kind of
+ * activations, smallest first; -2: a shape that the product refuses, or m = 0.
+ */
+int si_linear_mxfp4_tile(int a4, int m, int rows, int n, int gated);
+
 /* Bytes of the workspace of the two calls below (0 for unsupported shapes): a
  * si_workspace_bytes() workspace, under the same rules (zero-filled before its
  * first use, one call at a time), which fp16, INT8 and MXFP4 calls may share;

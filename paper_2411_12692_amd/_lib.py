@@ -76,6 +76,7 @@ SIGNATURES = {
     "si_linear_mxfp4_a4": (_i, [_p, _p, _i, _i, _p, _p, _i, _p, _i, _p, _sz, _p]),
     "si_gated_linear_mxfp4_a4": (_i, [_p, _p, _i, _i, _p, _p, _p, _p, _i, _p, _i, _p, _sz, _p]),
     "si_linear_mxfp4_workspace_bytes": (_sz, [_p, _sz, _i, _i, _i, _i]),
+    "si_linear_mxfp4_tile": (_i, [_i, _i, _i, _i, _i]),
     "si_mxfp4_workspace_bytes": (_sz, [_i, _i, _i]),
     "si_sparse_mlp_mxfp4": (_i, [_p, _p, _p, _p, _p, _p, _i, _i, _p, _i, _p, _p, _p, _sz, _u32, _p, _p]),
     "si_predict_sparse_mlp_mxfp4": (_i, [_p, _p, _p, _p, _p, _p, _p, _i, _i, _p, _i, _f, _p, _p, _p, _p, _p, _sz,

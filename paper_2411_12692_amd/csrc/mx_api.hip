@@ -97,6 +97,21 @@ si_status run_linear(MxLinear& c, bool gated, void* workspace, size_t workspace_
   return hip_status(launch_mx_linear(c, (hipStream_t)stream), "MXFP4 product launch");
 }
 
+alignas(16) const uint8_t kSome[16] = {};  // stands for operands of which only the presence counts
+
+// A call of which only the sizes are known (x NULL: MXFP4 activations).
+MxLinear sizes_of(const void* x, size_t ldx, int m, int rows, int n, int gated) {
+  MxLinear c;
+  c.x = x;
+  c.ldx = ldx;
+  c.xq = x ? nullptr : kSome;
+  c.q_up = gated ? kSome : nullptr;
+  c.m = m;
+  c.rows = rows;
+  c.n = n;
+  return c;
+}
+
 si_status linear_f(bool gated, const void* x, int x_dtype, size_t ldx, int m, int n, const uint8_t* q,
                    const uint8_t* scale, const uint8_t* q_up, const uint8_t* s_up, int rows, void* y, int y_dtype,
                    void* workspace, size_t workspace_bytes, void* stream) {
@@ -211,17 +226,13 @@ si_status si_pack_signs_mxfp4(const uint8_t* q_gate, int k, int d, uint32_t* sig
 }
 
 size_t si_linear_mxfp4_workspace_bytes(const void* x, size_t ldx, int m, int rows, int n, int gated) {
-  static const uint8_t some = 0;
-  MxLinear c;
-  c.x = x;
-  c.ldx = ldx;
-  c.xq = x ? nullptr : &some;
-  c.q_up = gated ? &some : nullptr;
-  c.m = m;
-  c.rows = rows;
-  c.n = n;
-  if (check_product(c) != SI_OK || m == 0) return 0;
-  return mx_linear_workspace(c);
+  const MxLinear c = sizes_of(x, ldx, m, rows, n, gated);
+  return check_product(c) != SI_OK || m == 0 ? 0 : mx_linear_workspace(c);
+}
+
+int si_linear_mxfp4_tile(int a4, int m, int rows, int n, int gated) {
+  const MxLinear c = sizes_of(a4 ? nullptr : kSome, (size_t)(n > 0 ? n : 0), m, rows, n, gated);
+  return check_product(c) != SI_OK || m == 0 ? -2 : mx_linear_tile(c);
 }
 
 si_status si_linear_mxfp4(const void* x, int x_dtype, size_t ldx, int m, int n, const uint8_t* q, const uint8_t* scale,

@@ -35,6 +35,8 @@ struct MxLinear {
 // Scratch of a call: a padded copy of activations that cannot be read in whole
 // 16-byte pieces, and the partial sums of products whose n is split.
 size_t mx_linear_workspace(const MxLinear& c);
+// Place of the call's tile in its list; -1 for the kernel of a few tokens and rows.
+int mx_linear_tile(const MxLinear& c);
 // Whether the call's grids stay within what a launch can hold.
 bool mx_linear_fits(const MxLinear& c);
 hipError_t launch_mx_linear(const MxLinear& c, hipStream_t s);

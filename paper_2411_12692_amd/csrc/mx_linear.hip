@@ -730,6 +730,8 @@ size_t mx_linear_workspace(const MxLinear& c) {
   return p.pad_bytes + p.part_bytes;
 }
 
+int mx_linear_tile(const MxLinear& c) { return plan_of(c).tile; }
+
 hipError_t launch_mx_linear(const MxLinear& c, hipStream_t s) {
   const Plan p = plan_of(c);
   const int np = mx_padded(c.n), act = act_of(c);
