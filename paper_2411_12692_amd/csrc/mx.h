@@ -29,7 +29,6 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef u32x4 u32x4_e2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_e4 __attribute__((aligned(4)));
 typedef u32x4 u32x4_e8 __attribute__((aligned(8)));
-typedef u32x2 u32x2_e2 __attribute__((aligned(2)));
 
 // A scale byte as the float whose exponent field it is: the operand of the
 // conversion instructions, which read that field alone (0 is 2^-127, 255 NaN).

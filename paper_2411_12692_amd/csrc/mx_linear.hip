@@ -71,26 +71,23 @@ __device__ inline float relu(float g) { return g > 0.f || g != g ? g : 0.f; }
 
 constexpr int kSW = 16;        // waves of a block: each takes every 16th step
 constexpr int kSAhead = 3;     // steps of a wave whose codes are in flight
-constexpr int kSLds = 72 * 1024;  // tokens of a block in LDS (two blocks a compute unit)
 constexpr int kSToks = 4;      // tokens
-
-// Steps of x that are in LDS at once (fp16 and bf16 activations).
-inline __host__ __device__ int skinny_chunk(int m) {
-  const int c = (kSLds / m - 16) / 256;
-  return c < kSW * kSAhead ? c : kSW * kSAhead;
-}
+constexpr int kSChunk = kSW * kSAhead;  // steps of a round: their codes in flight, their x in LDS
+// bytes of a token's x in LDS: 16 more than its values, so that the tokens' pieces
+// lie in different banks
+inline __host__ __device__ int skinny_pitch(int steps) { return (steps < kSChunk ? steps : kSChunk) * 256 + 16; }
+static_assert(kSToks * (kSChunk * 256 + 16) + kSW * 2 * kWave * 16 <= kMaxLds, "x and the waves' sums");
 
 template <int ACT, int MATS>
 __global__ __launch_bounds__(kSW * kWave) void k_mx_skinny(LinArgs a) {
   __shared__ f32x4 red[kSW][MATS][kWave];
-  extern __shared__ __attribute__((aligned(16))) uint8_t xl[];  // [m][chunk * 256 + 16]
+  extern __shared__ __attribute__((aligned(16))) uint8_t xl[];  // [m][pitch_x]
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
   const int row0 = blockIdx.x * 16;
   const size_t pitch_q = (size_t)a.steps * 64, pitch_s = (size_t)a.steps * 4;
   const int row = min(row0 + r, a.rows - 1), tok = min(r, a.m - 1);
-  const int chunk = ACT == kActMx ? kSW * kSAhead : min(skinny_chunk(a.m), a.steps);
-  const int pitch_x = chunk * 256 + 16;  // 16 more, so that the tokens' pieces lie in different banks
+  const int pitch_x = skinny_pitch(a.steps);
   const uint8_t* xq = static_cast<const uint8_t*>(a.x) + (size_t)tok * a.ldx + g * 16;  // MXFP4 activations
   const uint8_t* xs = ACT == kActMx ? a.xs + (size_t)tok * pitch_s + g : nullptr;
   const uint8_t* xt = xl + tok * pitch_x + g * 64;
@@ -103,8 +100,8 @@ __global__ __launch_bounds__(kSW * kWave) void k_mx_skinny(LinArgs a) {
     sp[w] = a.s[w] + (size_t)row * pitch_s + g;
     acc[w] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  for (int k0 = 0; k0 < a.steps; k0 += chunk) {
-    const int k1 = min(k0 + chunk, a.steps);
+  for (int k0 = 0; k0 < a.steps; k0 += kSChunk) {
+    const int k1 = min(k0 + kSChunk, a.steps);
     u32x4 c[kSAhead][MATS], x[kSAhead];
     uint32_t sc[kSAhead][MATS], sx[kSAhead];
 #pragma unroll
@@ -664,10 +661,11 @@ hipError_t linear_launch(const LinArgs& a, const Plan& p, hipStream_t s) {
     static std::atomic<int> attr_set[kMaxDevices];
     const int ok = per_device_once(attr_set, [](int) -> int {
       return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_mx_skinny<ACT, MATS>),
-                                 hipFuncAttributeMaxDynamicSharedMemorySize, kSLds) == hipSuccess ? 1 : -1;
+                                 hipFuncAttributeMaxDynamicSharedMemorySize,
+                                 kSToks * skinny_pitch(kSChunk)) == hipSuccess ? 1 : -1;
     });
     if (ok != 1) return hipErrorInvalidConfiguration;
-    const int lds = ACT == kActMx ? 0 : a.m * (std::min(skinny_chunk(a.m), a.steps) * 256 + 16);
+    const int lds = ACT == kActMx ? 0 : a.m * skinny_pitch(a.steps);
     k_mx_skinny<ACT, MATS><<<(unsigned)((a.rows + 15) / 16), kSW * kWave, lds, s>>>(a);
     return hipGetLastError();
   }

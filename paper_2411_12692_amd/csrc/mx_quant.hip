@@ -34,7 +34,7 @@ struct Piece {
 // The pieces of a block: blockIdx.x covers kQT * kUnits consecutive pieces of
 // the padded rows, `per` of them a row.  One wide division a block (uniform),
 // the rest in 32 bits.
-__device__ inline Piece piece_of(size_t first, uint32_t off, uint32_t per, size_t row0, uint32_t c0) {
+__device__ inline Piece piece_of(uint32_t off, uint32_t per, size_t row0, uint32_t c0) {
   uint32_t c = c0 + off;  // < 2^24 / 8 + 128 + 1024
   size_t row = row0;
   if (c >= per) {
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kQT) void k_quantize_mx(const void* __restrict__ w,
   Piece p[kUnits];
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
-    p[u] = piece_of(first, threadIdx.x + kQT * u, per, row0, c0);
+    p[u] = piece_of(threadIdx.x + kQT * u, per, row0, c0);
     if (p[u].row < rows) load8<DT>(w, p[u].row * ldw, p[u].c * 8, n, f[u]);
   }
 #pragma unroll
@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kQT) void k_dequantize_mx(const uint32_t* __restric
   Piece p[kUnits];
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
-    p[u] = piece_of(first, threadIdx.x + kQT * u, per, row0, c0);
+    p[u] = piece_of(threadIdx.x + kQT * u, per, row0, c0);
     if (p[u].row < rows) {
       c[u] = __builtin_nontemporal_load(q + p[u].row * per + p[u].c);
       b[u] = scale[p[u].row * (per / 4) + (p[u].c >> 2)];
