@@ -47,7 +47,7 @@ si_status check_rows_n(const char* what, int rows, int n, int max_n) {
 }
 
 si_status check_ld(const char* what, size_t ld, int n, int rows, size_t max_ld) {
-  if (ld > max_ld || (rows > 1 && ld < (size_t)n))
+  if (rows > 1 && (ld > max_ld || ld < (size_t)n))  // a single row's stride leads nowhere
     return fail(SI_ERR_SHAPE, "%s=%zu outside [n=%d, %zu]", what, ld, n, max_ld);
   return SI_OK;
 }
