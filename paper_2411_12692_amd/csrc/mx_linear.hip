@@ -585,6 +585,11 @@ struct Plan {
   size_t pad_bytes, part_bytes;
 };
 
+// Whether x is copied first: rows that end inside 128 values or start off 16 bytes.
+bool copies_x(const MxLinear& c) {
+  return !c.xq && (c.n % kMxPad != 0 || c.ldx % 8 != 0 || (reinterpret_cast<uintptr_t>(c.x) & 15u) != 0);
+}
+
 int act_of(const MxLinear& c) { return c.xq ? kActMx : c.x_dtype == kBF16 ? kActBF16 : kActF16; }
 
 // Which kernel.  With one block a compute unit a tile's time is set by what it
@@ -608,7 +613,7 @@ int act_of(const MxLinear& c) { return c.xq ? kActMx : c.x_dtype == kBF16 ? kAct
 Plan plan_of(const MxLinear& c) {
   Plan p;
   const int np = mx_padded(c.n), mats = c.q_up ? 2 : 1, act = act_of(c);
-  p.pad = act != kActMx && (c.n % kMxPad != 0 || c.ldx % 8 != 0 || (reinterpret_cast<uintptr_t>(c.x) & 15u) != 0);
+  p.pad = copies_x(c);
   p.pad_bytes = p.pad ? align256((size_t)c.m * np * 2) : 0;
   p.split = 1;
   p.tile = -1;
@@ -717,10 +722,10 @@ hipError_t linear_mats(const LinArgs& a, const Plan& p, hipStream_t s) {
 bool mx_linear_fits(const MxLinear& c) {
   // past 256 blocks, and with half the rows where there are two matrices: from 65
   // tokens tiles of at least 64 x 64 and 256 threads, else of 32 x 16 and 512; and
-  // the copy: fewer than 2^32 threads a launch
+  // the copy where x needs one: fewer than 2^32 threads a launch
   const double r = c.rows, m = c.m;
   const double threads = c.m > 64 ? (r / 64 + 1) * (m / 64 + 1) * 256 : (r / 32 + 1) * (m / 16 + 1) * 512;
-  return threads < 4294967296.0 && m * (mx_padded(c.n) / 8) < 4294967296.0;
+  return threads < 4294967296.0 && (!copies_x(c) || m * (mx_padded(c.n) / 8) < 4294967296.0);
 }
 
 size_t mx_linear_workspace(const MxLinear& c) {

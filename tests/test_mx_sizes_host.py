@@ -43,3 +43,12 @@ def test_refusal_of_no_rows():
     status, text = ask("(lib.si_linear_mxfp4(A, 0, 128, 5, 128, A, A, 0, A, 2, None, 0, None) == _lib.SI_ERR_SHAPE, "
                        "lib.si_last_error().decode())")
     assert status and "rows=0" in text
+
+
+def test_the_copy_of_x_limits_only_calls_that_make_one():
+    """2^24 tokens of 4096 values: x that can be read in place needs no launch for
+    its copy (2^33 threads), which is refused where x has to be copied."""
+    m, rows, n = 1 << 24, 3, 4096
+    got = ask(f"[lib.si_linear_mxfp4_tile(1, {m}, {rows}, {n}, 0), lib.si_linear_mxfp4_tile(0, {m}, {rows}, {n}, 0), "
+              f"lib.si_linear_mxfp4(A + 2, 0, {n}, {m}, {n}, A, A, {rows}, A, 2, A, 1 << 60, None) == _lib.SI_ERR_SHAPE]")
+    assert got[0] >= 0 and got[1] >= 0 and got[2]
