@@ -783,6 +783,8 @@ class MXFP4MLPLayer:
         """The dense MLP of a prompt, ``x [m][d]`` fp16 or bf16: ``ReLU(x
         W_gate^T) * (x W_up^T)`` in ``x``'s type, then the product with
         ``W_down^T``; returns ``[m][d]`` in ``out_dtype`` (``x``'s type).
+        With fp16 tokens a hidden value above 65504 becomes infinite, which in
+        decode, where it is float32, it does not; bf16 holds it.
         ``a4``: both products take their activations in MXFP4."""
         if self.q_down is None:
             raise ValueError("the layer was made without prompt=True")

@@ -18,12 +18,14 @@
 //    one is used.  Where a stage has little work for its waves they form groups
 //    that each take a part of its values.  With few tiles and a long n, n is split
 //    over blocks as well and k_mx_join adds the parts in order.
-//    (2048 tokens, 4096 x 11008 fp16: 157 us = 1.17 PFLOP/s; 4096 tokens, 13824 x
-//    5120 with MXFP4 activations: 198 us = 2.9 PFLOP/s; 16 tokens, 11008 x 4096:
-//    8.3 us = 2.9 TB/s of weights; gated, 37 tokens, 13824 x 5120: 24 us.)
+//    (2048 tokens, 4096 x 11008 fp16: 158 us = 1.17 PFLOP/s; 4096 tokens, 13824 x
+//    5120 with MXFP4 activations: 194-213 us = 2.7-3.0 PFLOP/s; 16 tokens, 11008 x
+//    4096: 8.4 us = 2.9 TB/s of weights; gated, 37 tokens, 13824 x 5120: 27.6 us.)
 //  * k_mx_skinny, a few tokens and few rows: a block owns 16 rows, its waves split
-//    n and stream the codes straight into registers; the tokens pass through LDS.
-//    (One token, 4096 x 11008: 7.9 us = 3 TB/s; the bytes alone would take 4.7.)
+//    n and stream the codes straight into registers, 48 steps of 128 values at a
+//    time; the tokens pass through LDS.  (One token, 4096 x 11008: 7.8 us = 3 TB/s;
+//    the bytes alone would take 4.7, but its 86 steps are two rounds, the second
+//    asked for once the first is multiplied.)
 #include <algorithm>
 #include <type_traits>
 

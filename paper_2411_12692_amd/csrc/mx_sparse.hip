@@ -24,7 +24,7 @@
 //
 // Bound by the two launches' chains of round trips (signs, then rows; list, then
 // pieces): 7B-shaped layer, one token, s = 0.9, 6.3 + 7.4 us for 12.8 MB (2.5 us of
-// a copy's rate); with four tokens at 13B, 15.9 + 12.1, also by the dot products.
+// a copy's rate); with four tokens at 13B, 15.7 + 12.0, also by the dot products.
 #include <type_traits>
 
 #include "layer_common.h"

@@ -7,8 +7,9 @@
 // Bound by memory: h and b are read once and stay in registers as float between
 // the two reductions, h' and x are written once; x is formed from the unrounded
 // h'.  A row's requests are all in flight before the first sum.
-// (4096 x 5120 bf16 with both norms and a gate: 37 us, 168 MB = 4.5 TB/s; with 512
-// threads a row, a third of them idle, 41 us.  One token of 4096: 3.4 us.)
+// (4096 x 5120 bf16 with both norms and a gate: 39 us, 168 MB = 4.3 TB/s; with 512
+// threads a row, a third of them idle, 4 us more.  Rows that do not start on 16
+// bytes go value by value: 4096 x 5119, 91 us.  One token of 4096: 3.3 us.)
 #include "layer_common.h"
 #include "mx.h"
 #include "mx_launch.h"
