@@ -116,6 +116,32 @@ def test_calls_of_every_kind_in_turn():
             assert _lib.status("si_workspace_check", ws.data_ptr(), ws.numel(), 0) == 0
 
 
+def test_layers_of_different_sizes_in_turn():
+    """Layers of other k and d, whose regions lie over each other's, on one
+    workspace that holds the largest."""
+    sizes = [(640, 1000), (512, 1376), (1152, 300), (128, 4000)]
+    calls, want = {}, {}
+    for d, k in sizes:
+        made, _ = layers(d, k)
+        for (name, lay), b in itertools.product(made.items(), (1, 2, 4, 7)):
+            y, (mask, *_) = lay(tokens(d, b, b), 1.0, outputs=True)
+            calls[d, name, b] = lay
+            want[d, name, b] = (y, mask)
+    ws = torch.zeros(max(si.workspace_bytes(k, d, 8) for d, k in sizes), dtype=torch.uint8, device=DEV)
+    for lay in calls.values():
+        lay.workspace = ws
+    order = list(calls)
+    rng = np.random.default_rng(6)
+    for _ in range(5):
+        for i in rng.permutation(len(order)):
+            d, name, b = order[i]
+            y, (mask, *_) = calls[order[i]](tokens(d, b, b), 1.0, outputs=True)
+            y0, mask0 = want[order[i]]
+            assert torch.equal(mask, mask0), order[i]
+            assert bool(((y - y0).abs() <= 1e-4 * y0.abs().max()).all()), order[i]
+    assert _lib.status("si_workspace_check", ws.data_ptr(), ws.numel(), 0) == 0
+
+
 class TestTwoLaunches:
     """A layer with more rows than the single-launch kernel takes, except from a
     list: the calls of two launches leave h3 of either sign in the workspace."""
