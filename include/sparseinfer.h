@@ -555,6 +555,142 @@ si_status si_norm_residual(const void* h, int h_dtype, size_t ldh, const void* b
                            size_t ldo, const float* pre_w, void* x, int x_dtype, size_t ldx, int tokens, int d,
                            float eps, void* stream);
 
+/*
+ * The dense MLP outside decode: products over every row of fp16 or bf16 weights
+ * (`dtype`, the type of x and W and of their gradients), float32 accumulation on
+ * the matrix cores, with their gradients.
+ *   si_linear       : y[t][i] = sum_j x[t][j] W[i][j]
+ *   si_gated_linear : h[t][i] = max(g, 0) * u with g = sum_j x[t][j] W_gate[i][j] and
+ *                     u = sum_j x[t][j] W_up[i][j], Eq. (1) steps 1-3 over every row
+ *                     in one launch; w_up NULL: the non-gated max(g, 0).
+ *   x   : m rows of n values, ldx elements from row to row (n to 2^21 where m > 1),
+ *         at any address that fits an element.
+ *   w   : [rows][n], at any address that fits an element; with w_transposed nonzero
+ *         W^T, [n][rows] (what si_transpose_down makes of W_down: y = h W_down^T).
+ *   y, h: [m][rows] of type y_dtype / h_dtype, written.
+ *   g, u: both or neither: the two sums themselves, [m][rows] of type dtype, kept for
+ *         the backward pass.  A positive g that the type rounds to 0 is kept as the
+ *         type's smallest value, so that its sign survives.  With w_up only.
+ *   m 0 to 2^24 (0 does nothing), rows and n 1 to 2^20, m times rows or n below 2^35
+ *         and few enough blocks for one launch (else SI_ERR_SHAPE).
+ *   workspace: the ..._workspace_bytes() of the call: scratch for split sums and for
+ *         copies of operands that cannot be read in 16-byte pieces (rows of a multiple
+ *         of 8 values that start on 16 bytes can).  Nothing is kept in it from one call
+ *         to the next; two calls that can run at the same time need one each.
+ * The sums' order depends on the shapes and addresses' alignment alone: the same call
+ * gives the same bits.
+ */
+si_status si_linear(const void* x, int dtype, size_t ldx, int m, int n, const void* w, int rows, int w_transposed,
+                    void* y, int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
+si_status si_gated_linear(const void* x, int dtype, size_t ldx, int m, int n, const void* w_gate, const void* w_up,
+                          int rows, void* h, int h_dtype, void* g, void* u, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * Their gradients, for a loss whose derivatives with respect to y (h) are dy (dh):
+ *   si_linear_backward       : dx = dy W,  dw = dy^T x (in w's layout)
+ *   si_gated_linear_backward : dg = dh u where g > 0, else 0;  du = dh max(g, 0);
+ *                              dx = dg W_gate + du W_up,  dw_gate = dg^T x,
+ *                              dw_up = du^T x
+ *   dy  : m rows of type dtype or float32, lddy elements from row to row; dh of any
+ *         type.  dy (as an operand of the products), dg and du are rounded to dtype.
+ *   g, u: as si_gated_linear kept them.  w_up NULL: u NULL, and g is its output h,
+ *         [m][rows] of type g_dtype.
+ *   dx, dw, dw_gate, dw_up: [m][n] and the weights' shapes, of type dtype, written;
+ *         each may be NULL.  With m = 0 the weights' gradients are zeros.
+ *   workspace: ..._workspace_bytes() of the call; want_dx and want_dw say which of the
+ *         gradients are not NULL.
+ */
+si_status si_linear_backward(const void* dy, int dy_dtype, size_t lddy, const void* x, int dtype, size_t ldx, int m, int n,
+                             const void* w, int rows, int w_transposed, void* dx, void* dw, void* workspace,
+                             size_t workspace_bytes, void* stream);
+si_status si_gated_linear_backward(const void* dh, int dh_dtype, size_t lddh, const void* g, int g_dtype, const void* u,
+                                   const void* x, int dtype, size_t ldx, int m, int n, const void* w_gate,
+                                   const void* w_up, int rows, void* dx, void* dw_gate, void* dw_up, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of the four calls above (0 for unsupported shapes and where none
+ * is needed).  Of the operands only alignment, and of w_up the presence, counts.
+ * Host-only. */
+size_t si_linear_workspace_bytes(const void* x, size_t ldx, int m, int n, const void* w, int rows, int w_transposed);
+size_t si_gated_linear_workspace_bytes(const void* x, size_t ldx, int m, int n, const void* w_gate, const void* w_up,
+                                       int rows);
+size_t si_linear_backward_workspace_bytes(const void* dy, int dy_dtype, size_t lddy, const void* x, size_t ldx, int m,
+                                          int n, const void* w, int rows, int w_transposed, int want_dx, int want_dw);
+size_t si_gated_linear_backward_workspace_bytes(const void* x, size_t ldx, int m, int n, const void* w_gate,
+                                                const void* w_up, int rows, int want_dx, int want_dw);
+
+/*
+ * FP8 weights: e4m3 values (sign, 4 bits of exponent, 3 of fraction; largest 448, no
+ * infinities) with float32 scales.  A row of n values is stored as n rounded up to
+ * 16 codes (zeros behind the n-th); a value is its code times its scale:
+ *   tokens  : a scale for each 128 values of a row, [rows][ceil(n / 128)];
+ *   weights : one for each 128 x 128 block, [ceil(rows / 128)][ceil(n / 128)].
+ */
+
+/* Bytes of the codes, and of the scales of tokens and of weights (0 for rows outside
+ * [0, 2^24] or n outside [1, 2^24]).  Host-only. */
+size_t si_fp8_codes_bytes(int rows, int n);
+size_t si_fp8_scales_bytes(int rows, int n);
+size_t si_fp8_block_scales_bytes(int rows, int n);
+
+/*
+ * Rows (tokens) and blocks (weights, once at load) to FP8.  With m the largest |v| of
+ * a block: scale = m / 448, the code of v is the e4m3 value nearest to v / scale, ties
+ * to the even code; both quotients are correctly rounded float32 ones.  A scale of 0
+ * (m = 0, or so small that the quotient is 0) has codes 0; a block with an infinity or
+ * a NaN the scale NaN and codes 0, so that it reads back as NaN.
+ *   x (w) : rows of n values of type x_dtype, ldx elements from row to row (n to 2^32
+ *           where rows > 1), at any address that fits an element.
+ *   rows 0 to 2^24 (0 does nothing), n 1 to 2^24.
+ */
+si_status si_quantize_rows_fp8(const void* x, int x_dtype, size_t ldx, int rows, int n, uint8_t* q, float* scale,
+                               void* stream);
+si_status si_quantize_blocks_fp8(const void* w, int w_dtype, size_t ldw, int rows, int n, uint8_t* q, float* scale,
+                                 void* stream);
+
+/* FP8 rows as values: w [rows][n] of type w_dtype; rows_per_scale 1 (tokens) or 128
+ * (weights). */
+si_status si_dequantize_fp8(const uint8_t* q, const float* scale, int rows_per_scale, int rows, int n, void* w, int w_dtype,
+                            void* stream);
+
+/*
+ * si_linear and si_gated_linear with FP8 weights (q, scale from si_quantize_blocks_fp8,
+ * or a checkpoint's of that form) and FP8 tokens (xq, x_scale from
+ * si_quantize_rows_fp8): the products of 128 codes are summed in float32 on the matrix
+ * cores, then multiplied with both scales and added in float32.
+ *   y (h) : [m][rows] of type y_dtype, written.  Sizes as si_linear.
+ *   workspace: si_linear_fp8_workspace_bytes() bytes (gated nonzero: with q_up).
+ */
+si_status si_linear_fp8(const uint8_t* xq, const float* x_scale, int m, int n, const uint8_t* q, const float* scale,
+                        int rows, void* y, int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
+si_status si_gated_linear_fp8(const uint8_t* xq, const float* x_scale, int m, int n, const uint8_t* q_gate,
+                              const float* s_gate, const uint8_t* q_up, const float* s_up, int rows, void* h, int h_dtype,
+                              void* workspace, size_t workspace_bytes, void* stream);
+size_t si_linear_fp8_workspace_bytes(int m, int rows, int n, int gated);
+
+/*
+ * LayerNorm (center nonzero) and RMSNorm (0) with their gradients, in float32:
+ *   c = x - mean(x), or x;  r = 1 / sqrt(mean(c^2) + eps);  y = c r w + b
+ *   with n = c r and e = dy w:  dx = r (e - mean(e) - n mean(e n))  (mean(e) with
+ *   center alone),  dw = sum over tokens of dy n,  db = sum over tokens of dy.
+ *   x, dy   : tokens rows of d values of type dtype, ldx and lddy elements from row to
+ *             row (to 2^32 where tokens > 1).     y, dx : [tokens][d] of that type.
+ *   w, b    : [d] of type w_dtype, as dw and db; b may be NULL.
+ *   mean, rstd : [tokens] float32, the means and r of the rows, written by the forward
+ *             pass where given (mean with center alone), read by the backward pass.
+ *   dx, dw, db : written; each may be NULL.  With tokens = 0 dw and db are zeros.
+ *   tokens 0 to 2^23 - 1, d 1 to 16384, addresses that fit an element.
+ *   workspace: si_layer_norm_backward_workspace_bytes(), where dw or db is given.
+ * The gradients' sums are taken in an order that depends on the sizes alone.
+ */
+si_status si_layer_norm(const void* x, int dtype, size_t ldx, const void* w, const void* b, int w_dtype, int center,
+                        float eps, void* y, float* mean, float* rstd, int tokens, int d, void* stream);
+si_status si_layer_norm_backward(const void* dy, size_t lddy, const void* x, int dtype, size_t ldx, const void* w,
+                                 int w_dtype, int center, const float* mean, const float* rstd, void* dx, void* dw, void* db,
+                                 int tokens, int d, void* workspace, size_t workspace_bytes, void* stream);
+size_t si_layer_norm_backward_workspace_bytes(int tokens, int d);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,9 +4,10 @@ Thin PyTorch-facing binding of ``libsparseinfer.so`` (see
 ``include/sparseinfer.h``).  PyTorch only provides device memory and the
 current stream; every step of the path runs in the library's HIP kernels.
 The functions take contiguous CUDA tensors: fp16 weights/inputs (``float16``
-or ``int16`` bit patterns), and return new tensors.  The MXFP4 products and
-``norm_residual`` also take bf16 and float32 and rows with a stride, and run on
-the device of their tensors.
+or ``int16`` bit patterns), and return new tensors.  The MXFP4, FP8 and dense
+products and the norms also take bf16 and float32 and rows with a stride, and run
+on the device of their tensors.  ``linear``, ``gated_linear``, ``mlp``,
+``layer_norm`` and ``rms_norm`` have gradients.
 """
 
 from __future__ import annotations
@@ -27,6 +28,8 @@ __all__ = [
     "quantize_rows_mxfp4", "dequantize_rows_mxfp4", "pack_signs_mxfp4", "linear_mxfp4", "gated_linear_mxfp4",
     "linear_mxfp4_a4", "gated_linear_mxfp4_a4", "mxfp4_workspace_bytes", "new_workspace_mxfp4", "sparse_mlp_mxfp4",
     "predict_sparse_mlp_mxfp4", "MXFP4MLPLayer", "norm_residual",
+    "linear", "gated_linear", "mlp", "layer_norm", "rms_norm", "quantize_rows_fp8", "quantize_blocks_fp8",
+    "dequantize_fp8", "linear_fp8", "gated_linear_fp8", "FP8MLPLayer",
 ]
 
 
@@ -277,6 +280,14 @@ class MLPLayer:
     def sparse_mlp(self, x, mask=None, active_idx=None, n_active=None, flags: int = 0, counters: bool = False):
         return sparse_mlp(self.w_gate, self.w_up, self.w_down_t, x, self.workspace, mask, active_idx, n_active,
                           flags, counters)
+
+    def prompt(self, x, out_dtype=None):
+        """The dense MLP of a prompt, ``x [..., d]`` fp16: ``ReLU(x W_gate^T) * (x
+        W_up^T)`` in fp16, then the product with ``W_down^T``; returns ``[..., d]`` in
+        ``out_dtype`` (``x``'s type).  A hidden value above 65504 becomes infinite,
+        which in decode, where it is float32, it does not."""
+        h = gated_linear(x, self.w_gate, self.w_up)
+        return linear(h, self.w_down_t, transposed=True, out_dtype=out_dtype or x.dtype)
 
 
 # ---- INT8 weights ---------------------------------------------------------
@@ -803,5 +814,404 @@ class MXFP4MLPLayer:
         RMSNorm(h') * next_norm_w`` for what follows (None without it)."""
         _, x = norm_residual(h, pre_w=norm_w, eps=eps, x_dtype=x_dtype)
         branch = self.prompt(x, a4=a4)
+        return norm_residual(h, branch.view(h.shape), post_w=post_norm_w, gate=gate, scale=scale, pre_w=next_norm_w,
+                             eps=eps, x_dtype=x_dtype, out=out)
+
+
+# ---- dense products with their gradients --------------------------------------
+
+@functools.lru_cache(maxsize=4096)
+def _dense_workspace(name: str, *args) -> int:
+    """Workspace bytes of a dense call: ``args`` as the C function takes them, with
+    ``_like`` addresses."""
+    return int(getattr(_lib.load(), name)(*args))
+
+
+def _like(t):
+    """An address that is a multiple of 16 where ``t``'s is, as the workspaces'
+    sizes ask; None for None."""
+    return None if t is None else 16 if t.data_ptr() & 15 == 0 else 18
+
+
+def _scratch(x, nbytes: int):
+    return x.new_empty((nbytes,), dtype=torch.uint8) if nbytes else None
+
+
+def _flat(x, name: str, dtypes):
+    """``x [..., n]`` as rows: returns ``(x2, rows, n, stride)``."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor")
+    if x.dim() == 0:
+        raise ValueError(f"{name} must be [..., n]")
+    x2 = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+    return (x2, *_rows(x2, name, dtypes))
+
+
+def _grad_rows(dy):
+    """A gradient as rows of any stride; those that autograd hands on expanded or
+    transposed are copied.  Returns ``(dy2, stride)``."""
+    dy2 = dy if dy.dim() == 2 else dy.reshape(-1, dy.shape[-1])
+    m, n = dy2.shape
+    if (n > 1 and dy2.stride(1) != 1) or (m > 1 and not n <= dy2.stride(0) <= 1 << 21):
+        dy2 = dy2.contiguous()
+    return dy2, dy2.stride(0) if m > 1 else n
+
+
+def _weight(w, name: str, x, shape=None):
+    """A contiguous matrix of ``x``'s type."""
+    _dev(w, name, _HALF, 2)
+    if _DTYPE[w.dtype] != _DTYPE[x.dtype]:
+        raise TypeError(f"{name} has dtype {w.dtype}, x {x.dtype}")
+    if shape is not None and tuple(w.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(w.shape)}")
+    return w.shape
+
+
+def _out_type(dtype, x):
+    dtype = x.dtype if dtype is None else dtype
+    if dtype not in _ANY:
+        raise TypeError(f"out_dtype {dtype}, expected one of {sorted(map(str, _ANY))}")
+    return dtype
+
+
+def _wants_grad(*tensors) -> bool:
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
+def _linear_forward(x2, m, n, ld, w, rows, transposed, out_dtype):
+    index = _same_device(x2, w)
+    y = x2.new_empty((m, rows), dtype=out_dtype)
+    nbytes = _dense_workspace("si_linear_workspace_bytes", _like(x2), ld, m, n, _like(w), rows, transposed)
+    ws = _scratch(x2, nbytes)
+    _call_on(index, "si_linear", x2.data_ptr(), _DTYPE[x2.dtype], ld, m, n, w.data_ptr(), rows, transposed, y.data_ptr(),
+             _DTYPE[out_dtype], _vp(ws), nbytes)
+    return y
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x2, w, m, n, ld, rows, transposed, out_dtype):
+        ctx.save_for_backward(x2, w)
+        ctx.args = (m, n, ld, rows, transposed)
+        return _linear_forward(x2, m, n, ld, w, rows, transposed, out_dtype)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x2, w = ctx.saved_tensors
+        m, n, ld, rows, transposed = ctx.args
+        if _DTYPE[dy.dtype] not in (_DTYPE[x2.dtype], _lib.SI_F32):
+            dy = dy.float()
+        dy, ldd = _grad_rows(dy)
+        want_x, want_w = ctx.needs_input_grad[:2]
+        dx = x2.new_empty((m, n)) if want_x else None
+        dw = torch.empty_like(w) if want_w else None
+        nbytes = _dense_workspace("si_linear_backward_workspace_bytes", _like(dy), _DTYPE[dy.dtype], ldd, _like(x2), ld, m, n,
+                                  _like(w), rows, transposed, want_x, want_w)
+        ws = _scratch(x2, nbytes)
+        _call_on(_same_device(x2, dy, w), "si_linear_backward", dy.data_ptr(), _DTYPE[dy.dtype], ldd, x2.data_ptr(),
+                 _DTYPE[x2.dtype], ld, m, n, w.data_ptr(), rows, transposed, _vp(dx), _vp(dw), _vp(ws), nbytes)
+        return dx, dw, None, None, None, None, None, None
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, transposed: bool = False, out_dtype=None) -> torch.Tensor:
+    """``x W^T`` (``si_linear``) with ``x [..., n]`` and ``W [rows][n]`` (``[n][rows]``
+    when ``transposed``) in fp16 or bf16; ``[..., rows]`` in ``out_dtype`` (``x``'s
+    type).  Differentiable with respect to both."""
+    x2, m, n, ld = _flat(x, "x", _HALF)
+    shape = _weight(w, "w", x)
+    rows = shape[1] if transposed else shape[0]
+    if shape[0 if transposed else 1] != n:
+        raise ValueError(f"w {tuple(shape)} does not take rows of {n} values")
+    out_dtype = _out_type(out_dtype, x)
+    if _wants_grad(x, w):
+        y = _Linear.apply(x2, w, m, n, ld, rows, bool(transposed), out_dtype)
+    else:
+        y = _linear_forward(x2, m, n, ld, w, rows, bool(transposed), out_dtype)
+    return y if x.dim() == 2 else y.view(*x.shape[:-1], rows)
+
+
+def _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, keep):
+    """``(h, g, u)``; g and u (with ``keep`` and ``w_up``) in ``x``'s type."""
+    index = _same_device(x2, w_gate, w_up)
+    h = x2.new_empty((m, rows), dtype=out_dtype)
+    g = u = None
+    if keep and w_up is not None:
+        g, u = x2.new_empty((m, rows)), x2.new_empty((m, rows))
+    nbytes = _dense_workspace("si_gated_linear_workspace_bytes", _like(x2), ld, m, n, _like(w_gate), _like(w_up), rows)
+    ws = _scratch(x2, nbytes)
+    _call_on(index, "si_gated_linear", x2.data_ptr(), _DTYPE[x2.dtype], ld, m, n, w_gate.data_ptr(), _vp(w_up), rows,
+             h.data_ptr(), _DTYPE[out_dtype], _vp(g), _vp(u), _vp(ws), nbytes)
+    return h, g, u
+
+
+class _GatedLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x2, w_gate, w_up, m, n, ld, rows, out_dtype):
+        h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, True)
+        ctx.save_for_backward(x2, w_gate, w_up, h if w_up is None else g, u)
+        ctx.args = (m, n, ld, rows)
+        return h
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh):
+        x2, w_gate, w_up, g, u = ctx.saved_tensors
+        m, n, ld, rows = ctx.args
+        dh, ldd = _grad_rows(dh)
+        want_x, want_g, want_u = ctx.needs_input_grad[:3]
+        dx = x2.new_empty((m, n)) if want_x else None
+        dg = torch.empty_like(w_gate) if want_g else None
+        du = torch.empty_like(w_up) if want_u else None
+        nbytes = _dense_workspace("si_gated_linear_backward_workspace_bytes", _like(x2), ld, m, n, _like(w_gate), _like(w_up),
+                                  rows, want_x, want_g or want_u)
+        ws = _scratch(x2, nbytes)
+        _call_on(_same_device(x2, dh, w_gate, w_up), "si_gated_linear_backward", dh.data_ptr(), _DTYPE[dh.dtype], ldd,
+                 g.data_ptr(), _DTYPE[g.dtype], _vp(u), x2.data_ptr(), _DTYPE[x2.dtype], ld, m, n, w_gate.data_ptr(),
+                 _vp(w_up), rows, _vp(dx), _vp(dg), _vp(du), _vp(ws), nbytes)
+        return dx, dg, du, None, None, None, None, None
+
+
+def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor = None, out_dtype=None) -> torch.Tensor:
+    """``ReLU(x W_gate^T) * (x W_up^T)`` over every row, Eq. (1) steps 1-3, in one
+    launch (``si_gated_linear``); ``w_up=None``: ``ReLU(x W_fc1^T)``.  ``x [..., n]``
+    and the weights ``[rows][n]`` in fp16 or bf16; returns ``[..., rows]`` in
+    ``out_dtype`` (``x``'s type).  Differentiable with respect to all; the backward
+    pass keeps both sums in ``x``'s type."""
+    x2, m, n, ld = _flat(x, "x", _HALF)
+    shape = _weight(w_gate, "w_gate", x)
+    rows = shape[0]
+    if shape[1] != n:
+        raise ValueError(f"w_gate {tuple(shape)} does not take rows of {n} values")
+    if w_up is not None:
+        _weight(w_up, "w_up", x, (rows, n))
+    out_dtype = _out_type(out_dtype, x)
+    if _wants_grad(x, w_gate, w_up):
+        h = _GatedLinear.apply(x2, w_gate, w_up, m, n, ld, rows, out_dtype)
+    else:
+        h = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, False)[0]
+    return h if x.dim() == 2 else h.view(*x.shape[:-1], rows)
+
+
+def mlp(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, out_dtype=None) -> torch.Tensor:
+    """The dense MLP of Eq. (1), ``(ReLU(x W_gate^T) * (x W_up^T)) W_down^T``, with
+    ``W_gate, W_up [k][d]`` and ``W_down [d][k]`` (``w_up=None``: the non-gated one):
+    ``gated_linear`` and ``linear``, differentiable with respect to all.  The hidden
+    values are rounded to ``x``'s type."""
+    return linear(gated_linear(x, w_gate, w_up), w_down, out_dtype=out_dtype)
+
+
+# ---- norms with their gradients -------------------------------------------------
+
+def _norm_forward(x2, tokens, d, ld, w, b, center, eps, keep):
+    """``(y, mean, rstd)``, the last two with ``keep``."""
+    index = _same_device(x2, w, b)
+    y = x2.new_empty((tokens, d))
+    mean = x2.new_empty((tokens,), dtype=torch.float32) if keep and center else None
+    rstd = x2.new_empty((tokens,), dtype=torch.float32) if keep else None
+    _call_on(index, "si_layer_norm", x2.data_ptr(), _DTYPE[x2.dtype], ld, w.data_ptr(), _vp(b), _DTYPE[w.dtype], center, eps,
+             y.data_ptr(), _vp(mean), _vp(rstd), tokens, d)
+    return y, mean, rstd
+
+
+class _Norm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x2, w, b, tokens, d, ld, center, eps):
+        y, mean, rstd = _norm_forward(x2, tokens, d, ld, w, b, center, eps, True)
+        ctx.save_for_backward(x2, w, mean, rstd)
+        ctx.args = (tokens, d, ld, center)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x2, w, mean, rstd = ctx.saved_tensors
+        tokens, d, ld, center = ctx.args
+        dy, ldd = _grad_rows(dy)
+        want_x, want_w, want_b = ctx.needs_input_grad[:3]
+        dx = x2.new_empty((tokens, d)) if want_x else None
+        dw = torch.empty_like(w) if want_w else None
+        db = torch.empty_like(w) if want_b else None
+        nbytes = 0
+        if want_w or want_b:
+            nbytes = _dense_workspace("si_layer_norm_backward_workspace_bytes", tokens, d)
+        ws = _scratch(x2, nbytes)
+        _call_on(_same_device(x2, dy, w), "si_layer_norm_backward", dy.data_ptr(), ldd, x2.data_ptr(), _DTYPE[x2.dtype], ld,
+                 w.data_ptr(), _DTYPE[w.dtype], center, _vp(mean), _vp(rstd), _vp(dx), _vp(dw), _vp(db), tokens, d, _vp(ws),
+                 nbytes)
+        return dx, dw, db, None, None, None, None, None
+
+
+_FLOATS = frozenset((torch.float16, torch.bfloat16, torch.float32))
+
+
+def _norm(x, w, b, eps, center):
+    x2, tokens, d, ld = _flat(x, "x", _FLOATS)
+    for t, name in ((w, "w"), (b, "b")):
+        if t is None and name == "b":
+            continue
+        _dev(t, name, _FLOATS, 1)
+        if t.shape[0] != d:
+            raise ValueError(f"{name} must be [{d}], got {list(t.shape)}")
+    if b is not None and b.dtype != w.dtype:
+        raise TypeError(f"b has dtype {b.dtype}, w {w.dtype}")
+    if _wants_grad(x, w, b):
+        y = _Norm.apply(x2, w, b, tokens, d, ld, center, float(eps))
+    else:
+        y = _norm_forward(x2, tokens, d, ld, w, b, center, float(eps), False)[0]
+    return y if x.dim() == 2 else y.view(x.shape)
+
+
+def layer_norm(x: torch.Tensor, w: torch.Tensor, b: torch.Tensor = None, eps: float = 1e-5) -> torch.Tensor:
+    """``(x - mean) / sqrt(var + eps) * w + b`` over the last dimension
+    (``si_layer_norm``), the norm in front of a non-gated MLP: ``x [..., d]`` in fp16,
+    bf16 or float32, ``w`` and ``b`` ``[d]`` of one of these types, in ``x``'s type.
+    Differentiable with respect to all."""
+    return _norm(x, w, b, eps, True)
+
+
+def rms_norm(x: torch.Tensor, w: torch.Tensor, eps: float = 1e-5) -> torch.Tensor:
+    """``x / sqrt(mean(x^2) + eps) * w`` over the last dimension (``si_layer_norm``),
+    differentiable; types as ``layer_norm``.  ``norm_residual`` is its form for
+    inference, with the residual."""
+    return _norm(x, w, None, eps, False)
+
+
+# ---- FP8 weights -----------------------------------------------------------------
+
+_E4M3 = torch.float8_e4m3fn
+
+
+def _quantize_fp8(name, w, arg, rows_per_scale):
+    rows, n, ld = _rows(w, arg, _ANY)
+    q = w.new_empty((rows, (n + 15) // 16 * 16), dtype=_E4M3)
+    scale = w.new_empty(((rows + rows_per_scale - 1) // rows_per_scale, (n + 127) // 128), dtype=torch.float32)
+    _call_on(w.get_device(), name, w.data_ptr(), _DTYPE[w.dtype], ld, rows, n, q.data_ptr(), scale.data_ptr())
+    return q, scale
+
+
+def quantize_rows_fp8(x: torch.Tensor):
+    """Tokens ``x [rows][n]`` (fp16, bf16 or float32, any row stride) to e4m3 with a
+    scale for each 128 values of a row (``si_quantize_rows_fp8``): returns the codes,
+    ``float8_e4m3fn [rows][n rounded up to 16]``, and scales, float32
+    ``[rows][ceil(n / 128)]``."""
+    return _quantize_fp8("si_quantize_rows_fp8", x, "x", 1)
+
+
+def quantize_blocks_fp8(w: torch.Tensor):
+    """Weights ``w [rows][n]`` to e4m3 with a scale for each 128 x 128 block
+    (``si_quantize_blocks_fp8``): the codes as ``quantize_rows_fp8``, the scales
+    float32 ``[ceil(rows / 128)][ceil(n / 128)]``."""
+    return _quantize_fp8("si_quantize_blocks_fp8", w, "w", 128)
+
+
+def _fp8(q, scale, name: str, rows_per_scale: int):
+    """Rows and stored values a row of FP8 rows or blocks."""
+    _dev(q, name, (_E4M3,), 2)
+    _dev(scale, f"{name}'s scales", (torch.float32,), 2)
+    rows, width = q.shape
+    if width % 16 or width == 0:
+        raise ValueError(f"{name} must hold rows of a multiple of 16 codes, got {width}")
+    want = ((rows + rows_per_scale - 1) // rows_per_scale, (width + 127) // 128)
+    if tuple(scale.shape) != want:
+        raise ValueError(f"{name}'s scales must be {list(want)}, got {list(scale.shape)}")
+    return rows, width
+
+
+def dequantize_fp8(q: torch.Tensor, scale: torch.Tensor, n: int, dtype=torch.float16) -> torch.Tensor:
+    """FP8 tokens (a scale row for each row) or weights (one for each 128) of ``n``
+    values as ``[rows][n]`` of ``dtype`` (``si_dequantize_fp8``)."""
+    per = 1 if isinstance(scale, torch.Tensor) and scale.dim() == 2 and scale.shape[0] == q.shape[0] else 128
+    rows, width = _fp8(q, scale, "q", per)
+    if width != (n + 15) // 16 * 16:
+        raise ValueError(f"q has rows of {width} codes, {n} values do not take that many")
+    if dtype not in _ANY:
+        raise TypeError(f"dtype {dtype}, expected one of {sorted(map(str, _ANY))}")
+    w = q.new_empty((rows, n), dtype=dtype)
+    _call_on(_same_device(q, scale), "si_dequantize_fp8", q.data_ptr(), scale.data_ptr(), per, rows, n, w.data_ptr(),
+             _DTYPE[dtype])
+    return w
+
+
+def _fp8_product(name, xq, x_scale, weights, out_dtype):
+    m, n = _fp8(xq, x_scale, "xq", 1)
+    gated = len(weights) == 4
+    rows, width = _fp8(weights[0], weights[1], "q_gate" if gated else "q", 128)
+    up = gated and weights[2] is not None
+    if up and _fp8(weights[2], weights[3], "q_up", 128) != (rows, width):
+        raise ValueError("q_up does not match q_gate")
+    if width != n:
+        raise ValueError(f"weights of {width} codes a row, tokens of {n}")
+    if out_dtype not in _ANY:
+        raise TypeError(f"out_dtype {out_dtype}, expected one of {sorted(map(str, _ANY))}")
+    index = _same_device(xq, x_scale, *weights)
+    y = xq.new_empty((m, rows), dtype=out_dtype)
+    nbytes = _dense_workspace("si_linear_fp8_workspace_bytes", m, rows, n, up)
+    ws = _scratch(xq, nbytes)
+    _call_on(index, name, xq.data_ptr(), x_scale.data_ptr(), m, n, *(_vp(t) for t in weights), rows, y.data_ptr(),
+             _DTYPE[out_dtype], _vp(ws), nbytes)
+    return y
+
+
+def linear_fp8(xq: torch.Tensor, x_scale: torch.Tensor, q: torch.Tensor, scale: torch.Tensor,
+               out_dtype=torch.float16) -> torch.Tensor:
+    """``x W^T`` of FP8 tokens (``quantize_rows_fp8``) and FP8 weights
+    (``quantize_blocks_fp8``, or a checkpoint's of that form) on the matrix cores
+    (``si_linear_fp8``): ``[m][rows]`` in ``out_dtype``."""
+    return _fp8_product("si_linear_fp8", xq, x_scale, (q, scale), out_dtype)
+
+
+def gated_linear_fp8(xq: torch.Tensor, x_scale: torch.Tensor, q_gate, s_gate, q_up=None, s_up=None,
+                     out_dtype=torch.float16) -> torch.Tensor:
+    """``gated_linear`` of FP8 tokens and weights (``si_gated_linear_fp8``);
+    ``q_up=None``: ``ReLU(x W_fc1^T)``."""
+    return _fp8_product("si_gated_linear_fp8", xq, x_scale, (q_gate, s_gate, q_up, s_up), out_dtype)
+
+
+class FP8MLPLayer:
+    """One layer's dense MLP with FP8 weights, made on the device at load from fp16,
+    bf16 or float32 ``W_gate``, ``W_up`` (``[k][d]``) and ``W_down`` (``[d][k]``), or
+    (``from_blocks``) from a checkpoint's codes and block scales.  ``w_up=None``: a
+    non-gated ReLU MLP."""
+
+    def __init__(self, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor):
+        self._set(quantize_blocks_fp8(w_gate), None if w_up is None else quantize_blocks_fp8(w_up),
+                  quantize_blocks_fp8(w_down))
+        self.d = w_gate.shape[1]
+
+    @classmethod
+    def from_blocks(cls, gate, up, down):
+        """From ``(codes, scales)`` pairs of the three matrices (``up=None``: non-gated)."""
+        layer = cls.__new__(cls)
+        layer._set(gate, up, down)
+        layer.d = layer.q_down.shape[0]
+        return layer
+
+    def _set(self, gate, up, down):
+        self.q_gate, self.s_gate = gate
+        self.q_up, self.s_up = up if up is not None else (None, None)
+        self.q_down, self.s_down = down
+        self.k, width = _fp8(self.q_gate, self.s_gate, "gate", 128)
+        if up is not None and _fp8(self.q_up, self.s_up, "up", 128) != (self.k, width):
+            raise ValueError("up does not match gate")
+        d, width_down = _fp8(self.q_down, self.s_down, "down", 128)
+        if (d + 15) // 16 * 16 != width or (self.k + 15) // 16 * 16 != width_down:
+            raise ValueError(f"down has {d} rows of {width_down} codes, gate {self.k} of {width}")
+
+    def prompt(self, x, out_dtype=None):
+        """The MLP of any number of tokens, ``x [m][d]`` fp16, bf16 or float32: tokens
+        to FP8, ``ReLU(x W_gate^T) * (x W_up^T)`` in ``x``'s type, that to FP8, the
+        product with ``W_down^T``; ``[m][d]`` in ``out_dtype`` (``x``'s type)."""
+        if x.shape[-1] != self.d:
+            raise ValueError(f"x has rows of {x.shape[-1]} values, the layer takes {self.d}")
+        h = gated_linear_fp8(*quantize_rows_fp8(x), self.q_gate, self.s_gate, self.q_up, self.s_up, out_dtype=x.dtype)
+        return linear_fp8(*quantize_rows_fp8(h), self.q_down, self.s_down, out_dtype or x.dtype)
+
+    def prompt_block(self, h, norm_w, eps: float, x_dtype=torch.bfloat16, post_norm_w=None, gate=None, scale: float = 1.0,
+                     next_norm_w=None, out: torch.Tensor = None):
+        """The MLP half of a decoder layer: ``norm_residual``, ``prompt``,
+        ``norm_residual`` (see ``MXFP4MLPLayer.prompt_block``)."""
+        _, x = norm_residual(h, pre_w=norm_w, eps=eps, x_dtype=x_dtype)
+        branch = self.prompt(x.view(-1, self.d))
         return norm_residual(h, branch.view(h.shape), post_w=post_norm_w, gate=gate, scale=scale, pre_w=next_norm_w,
                              eps=eps, x_dtype=x_dtype, out=out)

@@ -81,6 +81,27 @@ SIGNATURES = {
     "si_sparse_mlp_mxfp4": (_i, [_p, _p, _p, _p, _p, _p, _i, _i, _p, _i, _p, _p, _p, _sz, _u32, _p, _p]),
     "si_predict_sparse_mlp_mxfp4": (_i, [_p, _p, _p, _p, _p, _p, _p, _i, _i, _p, _i, _f, _p, _p, _p, _p, _p, _sz,
                                          _u32, _p, _p]),
+    "si_linear": (_i, [_p, _i, _sz, _i, _i, _p, _i, _i, _p, _i, _p, _sz, _p]),
+    "si_linear_workspace_bytes": (_sz, [_p, _sz, _i, _i, _p, _i, _i]),
+    "si_gated_linear": (_i, [_p, _i, _sz, _i, _i, _p, _p, _i, _p, _i, _p, _p, _p, _sz, _p]),
+    "si_gated_linear_workspace_bytes": (_sz, [_p, _sz, _i, _i, _p, _p, _i]),
+    "si_linear_backward": (_i, [_p, _i, _sz, _p, _i, _sz, _i, _i, _p, _i, _i, _p, _p, _p, _sz, _p]),
+    "si_linear_backward_workspace_bytes": (_sz, [_p, _i, _sz, _p, _sz, _i, _i, _p, _i, _i, _i, _i]),
+    "si_gated_linear_backward": (_i, [_p, _i, _sz, _p, _i, _p, _p, _i, _sz, _i, _i, _p, _p, _i, _p, _p, _p, _p, _sz,
+                                      _p]),
+    "si_gated_linear_backward_workspace_bytes": (_sz, [_p, _sz, _i, _i, _p, _p, _i, _i, _i]),
+    "si_fp8_codes_bytes": (_sz, [_i, _i]),
+    "si_fp8_scales_bytes": (_sz, [_i, _i]),
+    "si_fp8_block_scales_bytes": (_sz, [_i, _i]),
+    "si_quantize_rows_fp8": (_i, [_p, _i, _sz, _i, _i, _p, _p, _p]),
+    "si_quantize_blocks_fp8": (_i, [_p, _i, _sz, _i, _i, _p, _p, _p]),
+    "si_dequantize_fp8": (_i, [_p, _p, _i, _i, _i, _p, _i, _p]),
+    "si_linear_fp8": (_i, [_p, _p, _i, _i, _p, _p, _i, _p, _i, _p, _sz, _p]),
+    "si_gated_linear_fp8": (_i, [_p, _p, _i, _i, _p, _p, _p, _p, _i, _p, _i, _p, _sz, _p]),
+    "si_linear_fp8_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "si_layer_norm": (_i, [_p, _i, _sz, _p, _p, _i, _i, _f, _p, _p, _p, _i, _i, _p]),
+    "si_layer_norm_backward": (_i, [_p, _sz, _p, _i, _sz, _p, _i, _i, _p, _p, _p, _p, _p, _i, _i, _p, _sz, _p]),
+    "si_layer_norm_backward_workspace_bytes": (_sz, [_i, _i]),
     "si_norm_residual": (_i, [_p, _i, _sz, _p, _i, _sz, _p, _p, _i, _f, _p, _sz, _p, _p, _i, _sz, _i, _i, _f, _p]),
 }
 

@@ -1,0 +1,153 @@
+// The dense products' arguments and tiles, shared by their kernels (dense_tile.h),
+// the choice among them (dense.hip) and the C ABI (dense_api.hip).
+#pragma once
+
+#include "mx.h"
+#include "si_launch.h"
+
+namespace si {
+
+// C[n][m] = sum over the segments of sum_k A(m, k) B(n, k); see dense_tile.h.
+struct DenseArgs {
+  const void* a[2];  // W and W_up of a gated product; or by segment of k, or by batch
+  const void* b[2];  // by segment of k, or by batch
+  size_t lda, ldb;   // bytes from row to row
+  int M, N, K;       // K: of a segment
+  int segs;          // 1, or 2: the sum goes on over a[1], b[1]
+  void* c[2];        // [N][M] of c_dtype, by batch
+  int c_dtype;
+  int relu;          // one matrix: max(C, 0)
+  void* g;           // gated: the two sums themselves, of save_dtype, or NULL
+  void* u;
+  int save_dtype;
+  float* part;       // partial sums [split][parts_of][N][M], or NULL
+  int split, parts_of;
+  const float* sa[2];  // e4m3: scales of A's blocks [M / 128][blocks] ...
+  const float* sb;     // ... and of B's rows [N][blocks]
+  int blocks;
+  int m_tiles, n_tiles;
+};
+
+// Tiles by size: values along m (both matrices of a gated product) and n, planes of
+// a stage.  The first two are for few rows of B, which then lie along k.
+struct DenseShape {
+  int bm, bn, wk, threads;
+};
+constexpr DenseShape kDenseTiles[] = {{64, 16, 4, 512}, {64, 32, 4, 512}, {64, 64, 2, 512}, {128, 128, 1, 256}, {256, 256, 1, 512}};
+constexpr int kDenseTileCount = 5;
+
+// Instances (dense_*.hip): value type, layouts of A and B, matrices.
+hipError_t dense_rr(int type, const DenseArgs& a, int tile, hipStream_t s);                 // x W^T
+hipError_t dense_gated(int type, const DenseArgs& a, int tile, hipStream_t s);              // x W_gate^T, x W_up^T
+hipError_t dense_cr(int type, const DenseArgs& a, int tile, hipStream_t s);                 // dy W
+hipError_t dense_cc(int type, const DenseArgs& a, int tile, int batches, hipStream_t s);    // dy^T x
+hipError_t dense_fp8(const DenseArgs& a, int mats, int tile, hipStream_t s);
+
+// ---- calls (dense.hip), arguments validated by the caller ----------------------
+
+// A matrix of a call: rows of n values of type dtype, ld elements apart.
+struct DenseMat {
+  const void* p = nullptr;
+  int dtype = 0;
+  size_t ld = 0;
+};
+
+// y = x W^T, relu'd or gated: W [rows][n], or [n][rows] when transposed.
+struct DenseLinear {
+  DenseMat x, w, w_up;
+  int type = 0;  // kF16 or kBF16: the type of the products
+  bool transposed = false, relu = false;
+  int m = 0, rows = 0, n = 0;
+  void* y = nullptr;
+  int y_dtype = 0;
+  void* g = nullptr;
+  void* u = nullptr;
+  void* ws = nullptr;
+};
+size_t dense_linear_workspace(const DenseLinear& c);
+int dense_linear_tile(const DenseLinear& c);  // place of its tile; -1: more than one launch can hold
+hipError_t launch_dense_linear(const DenseLinear& c, hipStream_t s);
+
+// Gradients of DenseLinear.  gate NULL: of y = x W^T (dy); else of the ReLU'd or
+// gated product, whose gate values (one matrix: outputs) and up values were kept.
+struct DenseGrad {
+  DenseMat dy, x, w, w_up;
+  DenseMat gate, up;
+  int type = 0;
+  bool transposed = false;
+  int m = 0, rows = 0, n = 0;
+  void* dx = nullptr;
+  void* dw = nullptr;
+  void* dw_up = nullptr;
+  void* ws = nullptr;
+};
+size_t dense_grad_workspace(const DenseGrad& c);
+int dense_dx_tile(const DenseGrad& c);
+int dense_dw_tile(const DenseGrad& c);
+hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s);
+
+// Products of e4m3 values with block scales.
+struct DenseFp8 {
+  const uint8_t* xq = nullptr;
+  const float* xs = nullptr;
+  const uint8_t* q = nullptr;
+  const float* s = nullptr;
+  const uint8_t* q_up = nullptr;
+  const float* s_up = nullptr;
+  int m = 0, rows = 0, n = 0;
+  void* y = nullptr;
+  int y_dtype = 0;
+  bool relu = false;
+  void* ws = nullptr;
+};
+size_t dense_fp8_workspace(const DenseFp8& c);
+int dense_fp8_tile(const DenseFp8& c);
+hipError_t launch_dense_fp8(const DenseFp8& c, hipStream_t s);
+__host__ __device__ inline int fp8_padded(int n) { return (n + 15) / 16 * 16; }
+__host__ __device__ inline int fp8_blocks(int n) { return (n + 127) / 128; }
+
+// ---- e4m3 rows and blocks (fp8.hip) ------------------------------------------------
+hipError_t launch_quantize_rows_fp8(const void* x, int dtype, size_t ld, size_t rows, int n, uint8_t* q, float* scale,
+                                    hipStream_t s);
+hipError_t launch_quantize_blocks_fp8(const void* w, int dtype, size_t ld, int rows, int n, uint8_t* q, float* scale,
+                                      hipStream_t s);
+hipError_t launch_dequantize_fp8(const uint8_t* q, const float* scale, int rows_per_scale, size_t rows, int n, void* w,
+                                 int dtype, hipStream_t s);
+
+// ---- LayerNorm and RMSNorm (norm_train.hip) ------------------------------------------
+struct LayerNormArgs {
+  const void* x;
+  size_t ldx;
+  int dtype;          // of x, y, dy and dx
+  const void* w;
+  const void* b;
+  int w_dtype;        // of w, b and their gradients
+  void* y;            // [tokens][d]
+  float* mean;        // [tokens], or NULL
+  float* rstd;
+  size_t tokens;
+  int d, center;      // center: LayerNorm
+  float eps;
+};
+hipError_t launch_layer_norm(const LayerNormArgs& a, hipStream_t s);
+struct LayerNormGrad {
+  const void* dy;
+  size_t ldy;
+  const void* x;
+  size_t ldx;
+  int dtype;
+  const void* w;
+  int w_dtype;
+  const float* mean;
+  const float* rstd;
+  void* dx;           // [tokens][d], or NULL
+  void* dw;           // [d], or NULL
+  void* db;
+  size_t tokens;
+  int d, center;
+  float* part;        // workspace
+};
+size_t layer_norm_grad_workspace(size_t tokens, int d);
+hipError_t launch_layer_norm_grad(const LayerNormGrad& a, hipStream_t s);
+
+}  // namespace si

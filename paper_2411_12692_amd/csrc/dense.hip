@@ -1,0 +1,391 @@
+// The dense products of the MLP and their gradients, as calls of the tiles of
+// dense_tile.h:
+//   y  = x W^T          A = W (kRow), B = x (kRow); W_down^T [k][d]: A kCol
+//   g, u = x W_gate^T, x W_up^T in one launch, h = ReLU(g) * u in its epilogue
+//   dg = [g > 0] dh u,  du = dh ReLU(g)   (k_gated_grad)
+//   dx = dg W_gate + du W_up               one launch, its sum over both
+//   dW_gate = dg^T x,  dW_up = du^T x      one launch, a batch of two
+// Operands that cannot be read in 16-byte pieces (odd lengths, unaligned rows,
+// another type) are copied into the workspace first, rows padded with zeros.
+#include <algorithm>
+
+#include "dense.h"
+
+namespace si {
+
+// A copy of `rows` rows of n values with rows of whole 8, zeros behind the n-th, in
+// fp16 or bf16: 8 values a thread.
+__global__ __launch_bounds__(256) void k_dense_pad(const void* __restrict__ src, int dtype, size_t ld, size_t rows, int n,
+                                                   int np, int type, u32x4* __restrict__ out) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= rows * (size_t)(np / 8)) return;
+  const size_t r = i / (np / 8);
+  const int c = (int)(i - r * (np / 8)) * 8;
+  u32x4 v = {0, 0, 0, 0};
+  if (dtype == type && c + 8 <= n) {
+    v = *reinterpret_cast<const u32x4_e2*>(static_cast<const uint16_t*>(src) + r * ld + c);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (c + e < n) {
+        const float f = load_one(src, r * ld + c + e, dtype);
+        const uint32_t h = (type == kF16 ? pack_f2(f, 0.f) : pack_bf2(f, 0.f)) & 0xffffu;
+        v[e >> 1] |= h << (16 * (e & 1));
+      }
+  }
+  out[i] = v;
+}
+
+// dg and du of `rows` values a token, in rows of rp (zeros behind), 8 values a
+// thread.  UP: g and u are the two sums; else g is h = ReLU(g).  The gradient is 0
+// where g <= 0; a NaN of g lets it pass.
+template <bool UP>
+__global__ __launch_bounds__(256) void k_gated_grad(DenseMat dh, DenseMat gate, DenseMat up, size_t m, int rows, int rp,
+                                                    int type, u32x4* __restrict__ dg, u32x4* __restrict__ du) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= m * (size_t)(rp / 8)) return;
+  const size_t t = i / (rp / 8);
+  const int c = (int)(i - t * (rp / 8)) * 8;
+  float d[8], g[8], u[8];
+  auto load = [&](const DenseMat& a, float (&f)[8]) {
+    const bool half = a.dtype != kF32;
+    if (half && c + 8 <= rows) {
+      const u32x4 v = *reinterpret_cast<const u32x4_e2*>(static_cast<const uint16_t*>(a.p) + t * a.ld + c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t h = v[e >> 1] >> (16 * (e & 1));
+        f[e] = a.dtype == kF16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)h) : __builtin_bit_cast(float, h << 16);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = c + e < rows ? load_one(a.p, t * a.ld + c + e, a.dtype) : 0.f;
+    }
+  };
+  load(dh, d);
+  load(gate, g);
+  if constexpr (UP) load(up, u);
+  uint32_t a[4], b[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float x[2], y[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int k = 2 * e + j;
+      x[j] = g[k] <= 0.f ? 0.f : UP ? d[k] * u[k] : d[k];
+      y[j] = UP ? d[k] * (g[k] <= 0.f ? 0.f : g[k]) : 0.f;
+      if (c + k >= rows) x[j] = y[j] = 0.f;
+    }
+    a[e] = type == kF16 ? pack_f2(x[0], x[1]) : pack_bf2(x[0], x[1]);
+    if constexpr (UP) b[e] = type == kF16 ? pack_f2(y[0], y[1]) : pack_bf2(y[0], y[1]);
+  }
+  dg[i] = u32x4{a[0], a[1], a[2], a[3]};
+  if constexpr (UP) du[i] = u32x4{b[0], b[1], b[2], b[3]};
+}
+
+// The parts of a split sum, added in their order, 4 values a thread; `batches`
+// outputs one behind the other, or the two sums of a gated product.
+template <int MATS>
+__global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, size_t size) {
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= size) return;
+  const int batch = blockIdx.y, n = (int)min(size - i, (size_t)4);
+  float v[MATS][4];
+#pragma unroll
+  for (int w = 0; w < MATS; ++w)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[w][e] = 0.f;
+  for (int p = 0; p < a.split; ++p)
+#pragma unroll
+    for (int w = 0; w < MATS; ++w) {
+      const float* src = a.part + (size_t)(p * a.parts_of + batch + w) * size + i;
+      if (n == 4 && (size & 3) == 0) {
+        const f32x4 f = *reinterpret_cast<const f32x4*>(src);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[w][e] += f[e];
+      } else {
+        for (int e = 0; e < n; ++e) v[w][e] += src[e];
+      }
+    }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e >= n) break;
+    float y = v[0][e];
+    if constexpr (MATS == 2) {
+      if (a.g) {
+        uint16_t h = (uint16_t)(a.save_dtype == kBF16 ? pack_bf2(y, 0.f) : pack_f2(y, 0.f));
+        if (y > 0.f && h == 0) h = 1;  // as in the tiles
+        static_cast<uint16_t*>(a.g)[i + e] = h;
+        store_one(a.u, i + e, a.save_dtype, v[MATS - 1][e]);
+      }
+      y = (y > 0.f || y != y ? y : 0.f) * v[MATS - 1][e];
+    } else if (a.relu) {
+      y = y > 0.f || y != y ? y : 0.f;
+    }
+    store_one(a.c[batch], i + e, a.c_dtype, y);
+  }
+}
+
+namespace {
+
+constexpr long kBlocks = 256;  // compute units
+
+int pad8(int n) { return (n + 7) / 8 * 8; }
+
+bool needs_copy(const DenseMat& a, int type, int n) {
+  return a.dtype != type || n % 8 != 0 || a.ld % 8 != 0 || (reinterpret_cast<uintptr_t>(a.p) & 15u) != 0;
+}
+size_t copy_bytes(const DenseMat& a, int type, size_t rows, int n) {
+  return a.p && needs_copy(a, type, n) ? align256(rows * pad8(n) * 2) : 0;
+}
+
+// The matrix itself, or its copy at `ws`, which is moved behind it.
+hipError_t whole_rows(DenseMat& a, int type, size_t rows, int n, char*& ws, hipStream_t s) {
+  if (!a.p || !needs_copy(a, type, n)) return hipSuccess;
+  const int np = pad8(n);
+  const size_t all = rows * (np / 8);
+  k_dense_pad<<<(unsigned)((all + 255) / 256), 256, 0, s>>>(a.p, a.dtype, a.ld, rows, n, np, type,
+                                                            reinterpret_cast<u32x4*>(ws));
+  a = DenseMat{ws, type, (size_t)np};
+  ws += align256(all * 16);
+  return hipGetLastError();
+}
+
+struct Plan {
+  int tile, split;
+  size_t part_bytes;
+};
+
+// Which tile, and in how many parts the sum is taken, by an estimate of the time:
+// rounds of blocks over the compute units, each as long as its products or its
+// stages' bytes take, and the second launch that joins parts.
+Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows) {
+  Plan best = {-1, 1, 0};
+  double best_t = 1e30;
+  for (int i = b_rows ? 0 : 2; i < kDenseTileCount; ++i) {
+    const DenseShape& t = kDenseTiles[i];
+    const long blocks = (long)((M + t.bm / mats - 1) / (t.bm / mats)) * ((N + t.bn - 1) / t.bn) * batches;
+    const int kp = 128 / es * t.wk;
+    const long stages = (K + kp - 1) / kp;
+    const int resident = i == 3 ? 2 : 1;
+    const double rate = (i == 4 ? 5.0e12 : 4.2e12) * (es == 1 ? 1.8 : 1.0) / resident;  // flop/s of a block
+    for (int split = 1; split <= 16; split *= 2) {
+      if (split > 1 && stages < 4 * split) break;
+      if ((double)blocks * split * t.threads >= 4294967296.0) break;  // threads of a launch
+      const double rounds = (double)((blocks * split + kBlocks * resident - 1) / (kBlocks * resident));
+      const double k = (double)((stages + split - 1) / split) * kp;
+      const double mul = 2.0 * t.bm * t.bn * k / rate, move = (t.bm + t.bn) * k * es / (22e9 / resident * 1e0) * 1e0;
+      double us = rounds * (std::max(mul, move) * 1e6 + 2.0);
+      const double size = (double)M * N * mats * batches * 4;
+      if (split > 1) us += 3.0 + size * (2 * split + 1) / 4e6;
+      if (us < best_t) {
+        best_t = us;
+        best = {i, split, split > 1 ? align256((size_t)split * mats * batches * M * N * 4) : 0};
+      }
+    }
+  }
+  return best;
+}
+
+hipError_t join(const DenseArgs& a, int mats, int batches, hipStream_t s) {
+  if (!a.part) return hipSuccess;
+  const size_t size = (size_t)a.M * a.N;
+  const dim3 grid((unsigned)((size + 1023) / 1024), (unsigned)batches);
+  if (mats == 2)
+    k_dense_join<2><<<grid, 256, 0, s>>>(a, size);
+  else
+    k_dense_join<1><<<grid, 256, 0, s>>>(a, size);
+  return hipGetLastError();
+}
+
+Plan linear_plan(const DenseLinear& c) { return plan_of(c.rows, c.m, c.n, c.w_up.p ? 2 : 1, 1, 2, true); }
+Plan dx_plan(const DenseGrad& c) { return plan_of(c.n, c.m, (long)c.rows * (c.w_up.p ? 2 : 1), 1, 1, 2, true); }
+Plan dw_plan(const DenseGrad& c) {
+  return c.transposed ? plan_of(c.rows, c.n, c.m, 1, 1, 2, false)
+                      : plan_of(c.n, c.rows, c.m, 1, c.w_up.p ? 2 : 1, 2, false);
+}
+Plan fp8_plan(const DenseFp8& c) { return plan_of(c.rows, c.m, c.n, c.q_up ? 2 : 1, 1, 1, true); }
+
+size_t weight_copies(const DenseMat& w, const DenseMat& w_up, bool transposed, int type, int rows, int n) {
+  const int r = transposed ? n : rows, c = transposed ? rows : n;
+  return copy_bytes(w, type, r, c) + copy_bytes(w_up, type, r, c);
+}
+
+void set_plan(DenseArgs& a, const Plan& p, int parts_of, char* ws) {
+  a.split = p.split;
+  a.parts_of = parts_of;
+  a.part = p.part_bytes ? reinterpret_cast<float*>(ws) : nullptr;
+}
+
+}  // namespace
+
+#define TRY(e)                                     \
+  do {                                             \
+    if (hipError_t e_ = (e); e_ != hipSuccess) return e_; \
+  } while (0)
+
+size_t dense_linear_workspace(const DenseLinear& c) {
+  return copy_bytes(c.x, c.type, c.m, c.n) + weight_copies(c.w, c.w_up, c.transposed, c.type, c.rows, c.n) +
+         linear_plan(c).part_bytes;
+}
+
+hipError_t launch_dense_linear(const DenseLinear& c, hipStream_t s) {
+  char* ws = static_cast<char*>(c.ws);
+  DenseMat x = c.x, w = c.w, up = c.w_up;
+  const int wr = c.transposed ? c.n : c.rows, wc = c.transposed ? c.rows : c.n;
+  TRY(whole_rows(x, c.type, c.m, c.n, ws, s));
+  TRY(whole_rows(w, c.type, wr, wc, ws, s));
+  TRY(whole_rows(up, c.type, wr, wc, ws, s));
+  const Plan p = linear_plan(c);
+  const int mats = up.p ? 2 : 1;
+  DenseArgs a = {};
+  a.a[0] = w.p;
+  a.a[1] = up.p;
+  a.b[0] = x.p;
+  a.lda = w.ld * 2;
+  a.ldb = x.ld * 2;
+  a.M = c.rows;
+  a.N = c.m;
+  a.K = c.n;
+  a.segs = 1;
+  a.c[0] = c.y;
+  a.c_dtype = c.y_dtype;
+  a.relu = c.relu;
+  a.g = c.g;
+  a.u = c.u;
+  a.save_dtype = c.type;
+  set_plan(a, p, mats, ws);
+  const int type = c.type == kBF16 ? 1 : 0;
+  TRY(mats == 2 ? dense_gated(type, a, p.tile, s) : c.transposed ? dense_cr(type, a, p.tile, s)
+                                                                 : dense_rr(type, a, p.tile, s));
+  return join(a, mats, 1, s);
+}
+
+size_t dense_grad_workspace(const DenseGrad& c) {
+  size_t b = c.gate.p ? align256((size_t)c.m * pad8(c.rows) * 2) * (c.up.p ? 2 : 1) : copy_bytes(c.dy, c.type, c.m, c.rows);
+  if (c.dw || c.dw_up) b += copy_bytes(c.x, c.type, c.m, c.n);
+  size_t part = 0;
+  if (c.dx) {
+    b += weight_copies(c.w, c.w_up, c.transposed, c.type, c.rows, c.n);
+    part = dx_plan(c).part_bytes;
+  }
+  if (c.dw || c.dw_up) part = std::max(part, dw_plan(c).part_bytes);
+  return b + part;
+}
+
+hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
+  char* ws = static_cast<char*>(c.ws);
+  const int type = c.type == kBF16 ? 1 : 0;
+  DenseMat d = c.dy, du = {};
+  if (c.gate.p) {
+    const int rp = pad8(c.rows);
+    const size_t bytes = align256((size_t)c.m * rp * 2), all = (size_t)c.m * (rp / 8);
+    const unsigned grid = (unsigned)((all + 255) / 256);
+    u32x4* dg = reinterpret_cast<u32x4*>(ws);
+    ws += bytes;
+    d = DenseMat{dg, c.type, (size_t)rp};
+    if (c.up.p) {
+      du = DenseMat{ws, c.type, (size_t)rp};
+      k_gated_grad<true><<<grid, 256, 0, s>>>(c.dy, c.gate, c.up, c.m, c.rows, rp, c.type, dg,
+                                              reinterpret_cast<u32x4*>(ws));
+      ws += bytes;
+    } else {
+      k_gated_grad<false><<<grid, 256, 0, s>>>(c.dy, c.gate, c.up, c.m, c.rows, rp, c.type, dg, nullptr);
+    }
+    TRY(hipGetLastError());
+  } else {
+    TRY(whole_rows(d, c.type, c.m, c.rows, ws, s));
+  }
+  DenseMat x = c.x, w = c.w, up = c.w_up;
+  if (c.dw || c.dw_up) TRY(whole_rows(x, c.type, c.m, c.n, ws, s));
+  if (c.dx) {
+    const int wr = c.transposed ? c.n : c.rows, wc = c.transposed ? c.rows : c.n;
+    TRY(whole_rows(w, c.type, wr, wc, ws, s));
+    TRY(whole_rows(up, c.type, wr, wc, ws, s));
+    const Plan p = dx_plan(c);
+    DenseArgs a = {};
+    a.a[0] = w.p;
+    a.a[1] = up.p;
+    a.b[0] = d.p;
+    a.b[1] = du.p;
+    a.lda = w.ld * 2;
+    a.ldb = d.ld * 2;
+    a.M = c.n;
+    a.N = c.m;
+    a.K = c.rows;
+    a.segs = up.p ? 2 : 1;
+    a.c[0] = c.dx;
+    a.c_dtype = c.type;
+    set_plan(a, p, 1, ws);
+    TRY(c.transposed ? dense_rr(type, a, p.tile, s) : dense_cr(type, a, p.tile, s));
+    TRY(join(a, 1, 1, s));
+  }
+  if (c.dw || c.dw_up) {
+    const Plan p = dw_plan(c);
+    DenseArgs a = {};
+    a.K = c.m;
+    a.segs = 1;
+    a.c_dtype = c.type;
+    int batches = 1;
+    if (c.transposed) {
+      a.a[0] = d.p;
+      a.b[0] = x.p;
+      a.lda = d.ld * 2;
+      a.ldb = x.ld * 2;
+      a.M = c.rows;
+      a.N = c.n;
+      a.c[0] = c.dw;
+    } else {
+      // both matrices' gradients, or the one that is asked for
+      a.a[0] = a.a[1] = x.p;
+      a.lda = x.ld * 2;
+      a.ldb = d.ld * 2;
+      a.M = c.n;
+      a.N = c.rows;
+      const void* of[2] = {d.p, du.p};
+      void* to[2] = {c.dw, c.dw_up};
+      batches = 0;
+      for (int i = 0; i < 2; ++i)
+        if (to[i]) {
+          a.b[batches] = of[i];
+          a.c[batches++] = to[i];
+        }
+    }
+    set_plan(a, p, batches, ws);
+    TRY(dense_cc(type, a, p.tile, batches, s));
+    TRY(join(a, 1, batches, s));
+  }
+  return hipSuccess;
+}
+
+int dense_linear_tile(const DenseLinear& c) { return linear_plan(c).tile; }
+int dense_dx_tile(const DenseGrad& c) { return dx_plan(c).tile; }
+int dense_dw_tile(const DenseGrad& c) { return dw_plan(c).tile; }
+int dense_fp8_tile(const DenseFp8& c) { return fp8_plan(c).tile; }
+
+size_t dense_fp8_workspace(const DenseFp8& c) { return fp8_plan(c).part_bytes; }
+
+hipError_t launch_dense_fp8(const DenseFp8& c, hipStream_t s) {
+  const Plan p = fp8_plan(c);
+  const int mats = c.q_up ? 2 : 1;
+  DenseArgs a = {};
+  a.a[0] = c.q;
+  a.a[1] = c.q_up;
+  a.b[0] = c.xq;
+  a.lda = a.ldb = (size_t)fp8_padded(c.n);
+  a.M = c.rows;
+  a.N = c.m;
+  a.K = fp8_padded(c.n);
+  a.segs = 1;
+  a.c[0] = c.y;
+  a.c_dtype = c.y_dtype;
+  a.relu = c.relu;
+  a.sa[0] = c.s;
+  a.sa[1] = c.s_up;
+  a.sb = c.xs;
+  a.blocks = fp8_blocks(c.n);
+  set_plan(a, p, mats, static_cast<char*>(c.ws));
+  TRY(dense_fp8(a, mats, p.tile, s));
+  return join(a, mats, 1, s);
+}
+
+}  // namespace si

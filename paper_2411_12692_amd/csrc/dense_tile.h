@@ -1,0 +1,439 @@
+// Tiles of the dense products on the matrix cores, for 16-bit values (fp16, bf16)
+// and for e4m3 values with block scales:
+//     C[n][m] = sum_k A(m, k) B(n, k)
+// with fp32 accumulation.  The operands' names are those of the matrix instruction:
+// A's index runs along C's rows in memory, so that a lane ends with 4 consecutive
+// values of one row of C.
+//
+// An operand lies in memory in one of two ways: kRow, its rows hold consecutive k
+// (x and W of x W^T), or kCol, its rows are k and hold consecutive m or n (W of
+// dy W, both operands of dy^T x).  Both pass through LDS as they lie, in stages of
+// WK planes of 128 bytes of k (64 16-bit values, 128 of 8 bits), written by the
+// loads themselves; kCol tiles are turned around by the transposing LDS read.
+// Each plane of a stage belongs to one group of WM x WN waves; the groups' sums are
+// added at the end.
+//
+// Loads are buffer loads whose descriptor ends with the operand: what lies behind
+// its last row, or is addressed past it on purpose (the last pieces of k), arrives
+// as zeros, so sums need no tail.
+#pragma once
+
+#include <type_traits>
+
+#include "dense.h"
+#include "layer_common.h"
+
+namespace si {
+
+enum : int { kTypeF16 = 0, kTypeBF16 = 1, kTypeF8 = 2 };
+enum : int { kRow = 0, kCol = 1 };
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <int T>
+__device__ inline f32x4 dense_mfma(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x4 c) {
+  if constexpr (T == kTypeF8) {
+    const i32x8 a = {(int)a0.x, (int)a0.y, (int)a0.z, (int)a0.w, (int)a1.x, (int)a1.y, (int)a1.z, (int)a1.w};
+    const i32x8 b = {(int)b0.x, (int)b0.y, (int)b0.z, (int)b0.w, (int)b1.x, (int)b1.y, (int)b1.z, (int)b1.w};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+  } else if constexpr (T == kTypeBF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a0), __builtin_bit_cast(bf16x8, b0), c, 0,
+                                                   0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a0), __builtin_bit_cast(f16x8, b0), c, 0, 0,
+                                                  0);
+  }
+}
+
+// max(g, 0) where a NaN stays one
+__device__ inline float relu(float g) { return g > 0.f || g != g ? g : 0.f; }
+
+template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST>
+struct DenseTile {
+  static constexpr int NW = WM * WN * WK;
+  static constexpr int ES = T == kTypeF8 ? 1 : 2;     // bytes of a value
+  static constexpr int KP = 128 / ES;                 // values of k in a plane
+  static constexpr int R = BM / WM / 16, C = BN / WN / 16;  // 16 x 16 pieces of a wave
+  static constexpr int ABytes = BM * 128, BBytes = BN * 128, Plane = ABytes + BBytes, Bytes = WK * Plane;
+  static constexpr int IA = WK * ABytes / 1024, IB = WK * BBytes / 1024;  // wave requests of a stage
+  static constexpr int Requests = (IA + IB) / NW;
+  static_assert(IA % NW == 0 && IB % NW == 0, "whole requests a wave");
+  static_assert(R % MATS == 0 && (MATS == 1 || AL == kRow), "both matrices' pieces in each wave");
+  static_assert(T != kTypeF8 || (AL == kRow && BL == kRow && BM / MATS / WM <= 128), "a wave's rows share scales");
+  static_assert(Requests * (ST - 2) < 64, "what a wait can leave outstanding");
+  static_assert(ST * Bytes <= kMaxLds, "LDS of a compute unit");
+  static_assert((WK - 1) * BM * BN * 4 <= ST * Bytes, "the groups' sums");
+};
+
+// Where 16-byte piece p of row r of a plane lies in its row.
+// kRow, rows of 128 bytes: a read takes 16 rows' pieces g (lane group) of one half.
+// Sixteen lanes are served at a time, and those are not neighbours: rows 0-3 and
+// 12-15 of one lane group with rows 4-11 of the next, whose piece is one further.
+// kCol, rows of `pieces`: a transposing read takes, for each lane group, 4 rows'
+// 32 bytes, rows 8 apart; the 8 rows of half a wave get different 32 bytes of 256.
+template <int LAYOUT, int PIECES>
+__device__ inline int place(int r, int p) {
+  if constexpr (LAYOUT == kRow) return p ^ ((r >> 1) & 7) ^ (((r >> 2) ^ (r >> 3)) & 1);
+  else if constexpr (PIECES >= 16) return p ^ (((r & 3) | ((r >> 1) & 4)) << 1);
+  else return p ^ ((((r >> 1) & 1) | ((r >> 2) & 2)) << 1);
+}
+
+// Wait until at most N of the wave's vector memory requests and none of its LDS
+// reads are outstanding, then for the other waves.
+template <int N>
+__device__ inline void wait_stage() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | 0x0070 | ((N >> 4) << 14));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST>
+__global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__  // the buffer descriptors are types of the device alone
+  using P = DenseTile<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>;
+  constexpr int NW = P::NW, R = P::R, C = P::C, ES = P::ES, KP = P::KP;
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+  // XCD-aware order: blocks go to the XCDs in turn, so every XCD gets a run of
+  // neighbouring tiles; in a run 8 tiles along n share each tile along m
+  const int total = a.m_tiles * a.n_tiles;
+  int id = blockIdx.x % total;
+  const int rest = blockIdx.x / total, part = rest % a.split, batch = rest / a.split;
+  if (total % 8 == 0) id = (id & 7) * (total / 8) + (id >> 3);
+  const int grp = id / (8 * a.m_tiles), in = id - grp * 8 * a.m_tiles;
+  const int gw = min(8, a.n_tiles - grp * 8);
+  const int n0 = (grp * 8 + in % gw) * BN, m0 = (in / gw) * (BM / MATS);
+  // the stages of this part of the sum, over one or two segments of K each
+  const int per_seg = (a.K + KP * WK - 1) / (KP * WK), stages = per_seg * a.segs;
+  const int k_first = (int)((long long)stages * part / a.split);
+  const int k_last = (int)((long long)stages * (part + 1) / a.split);
+
+  // per-lane offsets of this wave's requests from the tile's first value
+  constexpr int NA = P::IA / NW, NB = P::IB / NW;
+  constexpr int PA = AL == kRow ? 8 : BM / 8, PB = BL == kRow ? 8 : BN / 8;  // 16-byte pieces of a row
+  constexpr int QA = P::ABytes / 1024, QB = P::BBytes / 1024;                // requests of a plane
+  uint32_t oa[NA], ob[NB];
+  int ka[NA], kb[NB];  // kRow: the first k of the lane's piece in the stage
+  bool second[NA];     // a request of W_up
+#pragma unroll
+  for (int i = 0; i < NA; ++i) {
+    const int q = wv + NW * i, plane = q / QA;
+    const int r = (q % QA) * (64 / PA) + lane / PA, p = place<AL, PA>(r, lane % PA);
+    second[i] = MATS == 2 && uniform(r >= BM / MATS);
+    const uint32_t row = AL == kRow ? r % (BM / MATS) : plane * KP + r;
+    ka[i] = plane * KP + p * (16 / ES);
+    oa[i] = row * (uint32_t)a.lda + p * 16 + (AL == kRow ? plane * 128 : 0);
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i) {
+    const int q = wv + NW * i, plane = q / QB;
+    const int r = (q % QB) * (64 / PB) + lane / PB, p = place<BL, PB>(r, lane % PB);
+    const uint32_t row = BL == kRow ? r : plane * KP + r;
+    kb[i] = plane * KP + p * (16 / ES);
+    ob[i] = row * (uint32_t)a.ldb + p * 16 + (BL == kRow ? plane * 128 : 0);
+  }
+  const int a_rows = min(BM / MATS, a.M - m0), b_rows = min(BN, a.N - n0);
+
+  // one stage's loads: the descriptors start at the stage's first value
+  auto request = [&](uint8_t* __restrict__ to, int stage) {
+    const int seg = stage >= per_seg, k = (stage - (seg ? per_seg : 0)) * (KP * WK);
+    const int left = a.K - k;
+    // operands' rows are whole 16-byte pieces (zeros where K, M or N are not)
+    auto whole = [](int n) { return (n + 16 / ES - 1) / (16 / ES) * (16 / ES); };
+    auto first = [&](const void* p, size_t ld, int layout, int at) {
+      return static_cast<const uint8_t*>(p) + (layout == kRow ? (size_t)at * ld + (size_t)k * ES
+                                                               : (size_t)k * ld + (size_t)at * ES);
+    };
+    auto bytes = [&](size_t ld, int layout, int rows, int cols) -> int {
+      return layout == kRow ? (rows - 1) * (int)ld + whole(left) * ES
+                            : (min(left, KP * WK) - 1) * (int)ld + whole(cols) * ES;
+    };
+    const int over = batch + seg;  // of two, the one or the other
+    const auto ra = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<uint8_t*>(first(a.a[MATS == 2 ? 0 : over], a.lda, AL, m0)), 0, bytes(a.lda, AL, a_rows, a.M - m0),
+        0x00020000);
+    const auto ra2 = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(first(a.a[1], a.lda, AL, m0)), 0,
+                                                       bytes(a.lda, AL, a_rows, a.M - m0), 0x00020000);
+    const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(first(a.b[over], a.ldb, BL, n0)), 0,
+                                                      bytes(a.ldb, BL, b_rows, a.N - n0), 0x00020000);
+    const bool tail = left < KP * WK;
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+      const int q = wv + NW * i;
+      uint8_t* dst = to + q / QA * P::Plane + q % QA * 1024;
+      uint32_t off = oa[i];
+      if (AL == kRow && tail && ka[i] >= left) off = 0x80000000u;
+      if (MATS == 2 && second[i])
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra2, (lds_u8*)dst, 16, off, 0, 0, 0);
+      else
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_u8*)dst, 16, off, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int q = wv + NW * i;
+      uint8_t* dst = to + q / QB * P::Plane + P::ABytes + q % QB * 1024;
+      uint32_t off = ob[i];
+      if (BL == kRow && tail && kb[i] >= left) off = 0x80000000u;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_u8*)dst, 16, off, 0, 0, 0);
+    }
+  };
+
+  const int wk = wv / (WM * WN), wm = wv / WN % WM, wn = wv % WN;
+  const int r = lane & 15, g = lane >> 4;
+  f32x4 acc[R][C];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int t = 0; t < C; ++t) acc[i][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // first row of the wave's 16-row piece i in the tile: with two matrices half of
+  // the pieces are W's rows and half the same rows of W_up
+  auto piece_row = [&](int i) {
+    if constexpr (MATS == 2)
+      return (i / (R / 2)) * (BM / 2) + wm * (BM / 2 / WM) + (i % (R / 2)) * 16;
+    else
+      return wm * (BM / WM) + i * 16;
+  };
+  // lane (r, g)'s 8 values (16 of 8 bits) of k for row or column c0 + r; step s of the plane's two
+  auto read = [&](auto layout, auto pieces, const uint8_t* tile, int c0, int s) -> u32x4 {
+    constexpr int L = decltype(layout)::value, PC = decltype(pieces)::value;
+    if constexpr (L == kRow) {
+      const int row = c0 + r;
+      return *reinterpret_cast<const u32x4*>(tile + row * 128 + 16 * place<kRow, 8>(row, 4 * s + g));
+    } else {
+      // lane 4 q + j of a group points at row q's values 4 j .. 4 j + 3 and receives
+      // its own column's values of the 4 rows
+      const int row = 32 * s + 8 * g + (r >> 2), p = c0 / 8 + ((r & 3) >> 1);
+      const uint8_t* lo = tile + row * (PC * 16) + 16 * place<kCol, PC>(row, p) + (r & 1) * 8;
+      const uint8_t* hi = tile + (row + 4) * (PC * 16) + 16 * place<kCol, PC>(row + 4, p) + (r & 1) * 8;
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)lo));
+      const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)hi));
+      return u32x4{x.x, x.y, y.x, y.y};
+    }
+  };
+  using LA = std::integral_constant<int, AL>;
+  using LB = std::integral_constant<int, BL>;
+  using CA = std::integral_constant<int, PA>;
+  using CB = std::integral_constant<int, PB>;
+
+  // e4m3: the scales of this wave's rows and tokens, a stage ahead
+  float sa[MATS], sb[C];
+  auto scales = [&](int stage) {
+    const int b = stage * WK + wk;
+    const bool on = b < a.blocks;
+    const int bc = on ? b : a.blocks - 1;
+#pragma unroll
+    for (int w = 0; w < MATS; ++w) {
+      const int row = min(m0 + wm * (BM / MATS / WM), a.M - 1) / 128;
+      sa[w] = a.sa[w][(size_t)row * a.blocks + bc];
+    }
+#pragma unroll
+    for (int t = 0; t < C; ++t) {
+      const int tok = min(n0 + wn * (BN / WN) + t * 16 + r, a.N - 1);
+      const float v = a.sb[(size_t)tok * a.blocks + bc];
+      sb[t] = v;
+    }
+    if (!on) {  // a plane behind the last block: its codes are zeros, its scales must not be NaN
+#pragma unroll
+      for (int t = 0; t < C; ++t) sb[t] = 0.f;
+#pragma unroll
+      for (int w = 0; w < MATS; ++w) sa[w] = 0.f;
+    }
+  };
+
+  auto compute = [&](const uint8_t* __restrict__ from, const float (&fa)[MATS], const float (&fb)[C]) {
+    const uint8_t* al = from + wk * P::Plane;
+    const uint8_t* bl = al + P::ABytes;
+    if constexpr (T == kTypeF8) {
+      u32x4 b[C][2];
+#pragma unroll
+      for (int t = 0; t < C; ++t)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) b[t][s] = read(LB{}, CB{}, bl, wn * (BN / WN) + t * 16, s);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int w = MATS == 2 ? i / (R / 2) : 0;
+        const u32x4 a0 = read(LA{}, CA{}, al, piece_row(i), 0), a1 = read(LA{}, CA{}, al, piece_row(i), 1);
+#pragma unroll
+        for (int t = 0; t < C; ++t) {
+          const f32x4 v = dense_mfma<T>(a0, a1, b[t][0], b[t][1], f32x4{0.f, 0.f, 0.f, 0.f});
+          const float f = fa[w] * fb[t];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(v[e], f, acc[i][t][e]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 b[C], v[R];
+#pragma unroll
+        for (int t = 0; t < C; ++t) b[t] = read(LB{}, CB{}, bl, wn * (BN / WN) + t * 16, s);
+#pragma unroll
+        for (int i = 0; i < R; ++i) v[i] = read(LA{}, CA{}, al, piece_row(i), s);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int t = 0; t < C; ++t) acc[i][t] = dense_mfma<T>(v[i], v[i], b[t], b[t], acc[i][t]);
+      }
+    }
+  };
+  // one stage computed while the requests of the next ST - 1 are in flight; the
+  // parts of LDS are told apart by the pointers' restrict, without which every
+  // read of LDS would wait for all requests
+  auto step = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from, int k) {
+    float fa[MATS], fb[C];
+    if constexpr (T == kTypeF8) {
+#pragma unroll
+      for (int w = 0; w < MATS; ++w) fa[w] = sa[w];
+#pragma unroll
+      for (int t = 0; t < C; ++t) fb[t] = sb[t];
+      if (k + 1 < k_last) scales(k + 1);
+    }
+    if (k + ST - 1 < k_last) request(to, k + ST - 1);
+    compute(from, fa, fb);
+  };
+
+  if constexpr (T == kTypeF8) scales(k_first);
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i)
+    if (k_first + i < k_last) request(lds + i * P::Bytes, k_first + i);
+  int cur = 0;
+  for (int k = k_first; k < k_last; ++k) {
+    // stage k is in LDS, and every wave has left the part that k + ST - 1 goes to
+    if (k + ST - 2 < k_last)
+      wait_stage<P::Requests * (ST - 2)>();
+    else
+      wait_stage<0>();
+    const int nxt = cur == 0 ? ST - 1 : cur - 1;
+    step(lds + nxt * P::Bytes, lds + cur * P::Bytes, k);
+    cur = cur == ST - 1 ? 0 : cur + 1;
+  }
+  if constexpr (WK > 1) {
+    // the groups' sums, added by the first one
+    __syncthreads();
+    f32x4* sums = reinterpret_cast<f32x4*>(lds) + (wv % (WM * WN)) * kWave + lane;
+#pragma unroll
+    for (int q = 1; q < WK; ++q)
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < C; ++t)
+          if (wk == q) sums[(((q - 1) * R + i) * C + t) * (WM * WN * kWave)] = acc[i][t];
+    __syncthreads();
+    if (wk != 0) return;
+#pragma unroll
+    for (int q = 1; q < WK; ++q)
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int t = 0; t < C; ++t) acc[i][t] += sums[(((q - 1) * R + i) * C + t) * (WM * WN * kWave)];
+  }
+
+  // a lane holds m = 4 g .. 4 g + 3 of each piece for n = r of each
+  auto put = [&](void* y, int dt, int i, int t, f32x4 v, bool keep_sign) {
+    const int m = m0 + piece_row(i) % (BM / MATS) + 4 * g;
+    const int n = n0 + wn * (BN / WN) + t * 16 + r;
+    if (n >= a.N || m >= a.M) return;
+    const size_t at = (size_t)n * a.M + m;
+    if (dt == kF32) {
+      float* p = static_cast<float*>(y) + at;
+      if ((a.M & 3) == 0) {
+        *reinterpret_cast<f32x4*>(p) = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (m + e < a.M) p[e] = v[e];
+      }
+      return;
+    }
+    uint16_t h[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      h[e] = (uint16_t)(dt == kBF16 ? pack_bf2(v[e], 0.f) : pack_f2(v[e], 0.f));
+      // what the derivative asks of it, whether it is above 0, survives the rounding
+      if (keep_sign && v[e] > 0.f && h[e] == 0) h[e] = 1;
+    }
+    uint16_t* p = static_cast<uint16_t*>(y) + at;
+    if ((a.M & 3) == 0) {
+      *reinterpret_cast<u32x2*>(p) = u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (m + e < a.M) p[e] = h[e];
+    }
+  };
+  if (a.part) {
+    const size_t size = (size_t)a.M * a.N;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int mat = MATS == 2 ? i / (R / 2) : batch;
+#pragma unroll
+      for (int t = 0; t < C; ++t) put(a.part + (size_t)(part * a.parts_of + mat) * size, kF32, i, t, acc[i][t], false);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < R / MATS; ++i)
+#pragma unroll
+    for (int t = 0; t < C; ++t) {
+      f32x4 v = acc[i][t];
+      if constexpr (MATS == 2) {
+        const f32x4 u = acc[i + R / 2][t];
+        if (a.g) {
+          put(a.g, a.save_dtype, i, t, v, true);
+          put(a.u, a.save_dtype, i, t, u, false);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = relu(v[e]) * u[e];
+      } else if (a.relu) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = relu(v[e]);
+      }
+      put(a.c[batch], a.c_dtype, i, t, v, false);
+    }
+#endif
+}
+
+// Launch of one tile shape over the whole product.
+template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST>
+hipError_t dense_tile_launch(DenseArgs a, int batches, hipStream_t s) {
+  using P = DenseTile<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>;
+  if (a.M < 1 || a.N < 1) return hipErrorInvalidValue;
+  static std::atomic<int> attr_set[kMaxDevices];
+  const int ok = per_device_once(attr_set, [](int) -> int {
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_dense<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, ST * P::Bytes) == hipSuccess ? 1 : -1;
+  });
+  if (ok != 1) return hipErrorInvalidConfiguration;
+  a.m_tiles = (a.M + BM / MATS - 1) / (BM / MATS);
+  a.n_tiles = (a.N + BN - 1) / BN;
+  k_dense<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>
+      <<<(unsigned)(a.m_tiles * a.n_tiles * a.split * batches), WM * WN * WK * kWave, ST * P::Bytes, s>>>(a);
+  return hipGetLastError();
+}
+
+// The tiles of kDenseTiles (dense.h), by their place there.
+template <int T, int AL, int BL, int MATS>
+hipError_t dense_launch(const DenseArgs& a, int tile, int batches, hipStream_t s) {
+#define SI_DENSE_TILE(I, WM, WN, WK, ST) \
+  case I:                                \
+    static_assert(WK == kDenseTiles[I].wk && WM * WN * WK * kWave == kDenseTiles[I].threads, "kDenseTiles"); \
+    return dense_tile_launch<T, AL, BL, MATS, kDenseTiles[I].bm, kDenseTiles[I].bn, WM, WN, WK, ST>(a, batches, s);
+  if constexpr (BL == kRow) {
+    switch (tile) {
+      SI_DENSE_TILE(0, 2, 1, 4, 3)
+      SI_DENSE_TILE(1, 2, 1, 4, 3)
+    }
+  }
+  switch (tile) {
+    SI_DENSE_TILE(2, 2, 2, 2, 3)
+    SI_DENSE_TILE(3, 2, 2, 1, 2)
+    SI_DENSE_TILE(4, 2, 4, 1, 2)
+  }
+#undef SI_DENSE_TILE
+  return hipErrorInvalidValue;
+}
+
+}  // namespace si
