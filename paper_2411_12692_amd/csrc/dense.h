@@ -33,7 +33,7 @@ struct DenseArgs {
 struct DenseShape {
   int bm, bn, wk, threads;
 };
-constexpr DenseShape kDenseTiles[] = {{64, 16, 4, 512}, {64, 32, 4, 512}, {64, 64, 2, 512}, {128, 128, 1, 256}, {256, 256, 1, 512}};
+constexpr DenseShape kDenseTiles[] = {{64, 16, 4, 512}, {64, 32, 4, 512}, {64, 64, 2, 512}, {128, 128, 1, 512}, {256, 256, 1, 512}};
 constexpr int kDenseTileCount = 5;
 
 // Instances (dense_*.hip): value type, layouts of A and B, matrices.

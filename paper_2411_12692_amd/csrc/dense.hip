@@ -167,7 +167,7 @@ Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows) {
     const int kp = 128 / es * t.wk;
     const long stages = (K + kp - 1) / kp;
     const int resident = i == 3 ? 2 : 1;
-    const double rate = (i == 4 ? 5.0e12 : 4.2e12) * (es == 1 ? 1.8 : 1.0) / resident;  // flop/s of a block
+    const double rate = (i == 4 ? 5.0e12 : i == 3 ? 4.1e12 : 3.0e12) * (es == 1 ? 1.8 : 1.0) / resident;  // flop/s of a block
     for (int split = 1; split <= 16; split *= 2) {
       if (split > 1 && stages < 4 * split) break;
       if ((double)blocks * split * t.threads >= 4294967296.0) break;  // threads of a launch

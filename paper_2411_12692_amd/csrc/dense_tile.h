@@ -59,10 +59,16 @@ struct DenseTile {
   static constexpr int ABytes = BM * 128, BBytes = BN * 128, Plane = ABytes + BBytes, Bytes = WK * Plane;
   static constexpr int IA = WK * ABytes / 1024, IB = WK * BBytes / 1024;  // wave requests of a stage
   static constexpr int Requests = (IA + IB) / NW;
+  // LDS reads of a step, and the products between two of them, or two requests
+  static constexpr int Reads = (AL == kRow ? R : 2 * R) + (BL == kRow ? C : 2 * C);
+  // products before a stage's barrier, between two requests behind it, and between two
+  // reads of the next stage
+  static constexpr int N1 = Reads < R * C ? Reads : R * C, M2 = 2 * Reads <= R * C ? 2 : 1;
+  static constexpr int M3 = 2 * R * C - N1 - M2 * Reads >= Requests ? (2 * R * C - N1 - M2 * Reads) / Requests : 1;
   static_assert(IA % NW == 0 && IB % NW == 0, "whole requests a wave");
   static_assert(R % MATS == 0 && (MATS == 1 || AL == kRow), "both matrices' pieces in each wave");
   static_assert(T != kTypeF8 || (AL == kRow && BL == kRow && BM / MATS / WM <= 128), "a wave's rows share scales");
-  static_assert(Requests * (ST - 2) < 64, "what a wait can leave outstanding");
+  static_assert(Requests * (ST - 1) < 64, "what a wait can leave outstanding");
   static_assert(ST * Bytes <= kMaxLds, "LDS of a compute unit");
   static_assert((WK - 1) * BM * BN * 4 <= ST * Bytes, "the groups' sums");
 };
@@ -116,7 +122,6 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
   constexpr int PA = AL == kRow ? 8 : BM / 8, PB = BL == kRow ? 8 : BN / 8;  // 16-byte pieces of a row
   constexpr int QA = P::ABytes / 1024, QB = P::BBytes / 1024;                // requests of a plane
   uint32_t oa[NA], ob[NB];
-  int ka[NA], kb[NB];  // kRow: the first k of the lane's piece in the stage
   bool second[NA];     // a request of W_up
 #pragma unroll
   for (int i = 0; i < NA; ++i) {
@@ -124,7 +129,6 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     const int r = (q % QA) * (64 / PA) + lane / PA, p = place<AL, PA>(r, lane % PA);
     second[i] = MATS == 2 && uniform(r >= BM / MATS);
     const uint32_t row = AL == kRow ? r % (BM / MATS) : plane * KP + r;
-    ka[i] = plane * KP + p * (16 / ES);
     oa[i] = row * (uint32_t)a.lda + p * 16 + (AL == kRow ? plane * 128 : 0);
   }
 #pragma unroll
@@ -132,40 +136,46 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     const int q = wv + NW * i, plane = q / QB;
     const int r = (q % QB) * (64 / PB) + lane / PB, p = place<BL, PB>(r, lane % PB);
     const uint32_t row = BL == kRow ? r : plane * KP + r;
-    kb[i] = plane * KP + p * (16 / ES);
     ob[i] = row * (uint32_t)a.ldb + p * 16 + (BL == kRow ? plane * 128 : 0);
   }
+  // kRow: the first k of the lane's piece in its plane, the same in all of the wave's
+  // requests (they are an even number of requests apart)
+  static_assert(NW % 2 == 0, "requests of a wave");
+  const int k_piece = place<kRow, 8>((wv & 1) * 8 + lane / 8, lane % 8) * (16 / ES);
   const int a_rows = min(BM / MATS, a.M - m0), b_rows = min(BN, a.N - n0);
 
-  // one stage's loads: the descriptors start at the stage's first value
-  auto request = [&](uint8_t* __restrict__ to, int stage) {
-    const int seg = stage >= per_seg, k = (stage - (seg ? per_seg : 0)) * (KP * WK);
-    const int left = a.K - k;
-    // operands' rows are whole 16-byte pieces (zeros where K, M or N are not)
-    auto whole = [](int n) { return (n + 16 / ES - 1) / (16 / ES) * (16 / ES); };
-    auto first = [&](const void* p, size_t ld, int layout, int at) {
-      return static_cast<const uint8_t*>(p) + (layout == kRow ? (size_t)at * ld + (size_t)k * ES
-                                                               : (size_t)k * ld + (size_t)at * ES);
-    };
-    auto bytes = [&](size_t ld, int layout, int rows, int cols) -> int {
-      return layout == kRow ? (rows - 1) * (int)ld + whole(left) * ES
-                            : (min(left, KP * WK) - 1) * (int)ld + whole(cols) * ES;
-    };
-    const int over = batch + seg;  // of two, the one or the other
-    const auto ra = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<uint8_t*>(first(a.a[MATS == 2 ? 0 : over], a.lda, AL, m0)), 0, bytes(a.lda, AL, a_rows, a.M - m0),
-        0x00020000);
-    const auto ra2 = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(first(a.a[1], a.lda, AL, m0)), 0,
-                                                       bytes(a.lda, AL, a_rows, a.M - m0), 0x00020000);
-    const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(first(a.b[over], a.ldb, BL, n0)), 0,
-                                                      bytes(a.ldb, BL, b_rows, a.N - n0), 0x00020000);
-    const bool tail = left < KP * WK;
+  // The stages' loads, one after another.  The descriptors start at the stage's
+  // first value; stages past the last have empty ones, so that the loop below needs no
+  // branch (and the compiler counts its requests).
+  constexpr size_t row_step = KP * WK * ES;
+  const size_t step_a = AL == kRow ? row_step : (size_t)(KP * WK) * a.lda;
+  const size_t step_b = BL == kRow ? row_step : (size_t)(KP * WK) * a.ldb;
+  const int seg0 = k_first >= per_seg;  // 0 or 1
+  int left = a.K - (k_first - (seg0 ? per_seg : 0)) * (KP * WK), more = k_last - k_first;
+  auto origin = [&](const void* p, size_t ld, int layout, int at) {
+    return reinterpret_cast<uintptr_t>(p) + (layout == kRow ? (size_t)at * ld : (size_t)at * ES);
+  };
+  const int over = batch + seg0;  // of two, the one or the other
+  uintptr_t pa = origin(MATS == 2 || over == 0 ? a.a[0] : a.a[1], a.lda, AL, m0) + (size_t)(a.K - left) / (KP * WK) * step_a;
+  uintptr_t pb = origin(over == 0 ? a.b[0] : a.b[1], a.ldb, BL, n0) + (size_t)(a.K - left) / (KP * WK) * step_b;
+  const uintptr_t up = MATS == 2 ? origin(a.a[1], a.lda, AL, m0) - origin(a.a[0], a.lda, AL, m0) : 0;
+  const uintptr_t pa_next = origin(a.a[1], a.lda, AL, m0), pb_next = origin(a.b[1], a.ldb, BL, n0);
+  // bytes of the tile's rows before the last one, and values of the last
+  const int rows_a = (a_rows - 1) * (int)a.lda, rows_b = (b_rows - 1) * (int)a.ldb;
+  auto whole = [](int n) { return (n + 16 / ES - 1) / (16 / ES) * 16; };  // in whole 16-byte pieces
+  const int cols_a = whole(a.M - m0), cols_b = whole(a.N - n0);
+  auto request = [&](uint8_t* __restrict__ to) {
+    const int rows = min(left, KP * WK) - 1;
+    const int bytes_a = more <= 0 ? 0 : AL == kRow ? rows_a + whole(left) : rows * (int)a.lda + cols_a;
+    const int bytes_b = more <= 0 ? 0 : BL == kRow ? rows_b + whole(left) : rows * (int)a.ldb + cols_b;
+    const auto ra = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pa), 0, bytes_a, 0x00020000);
+    const auto ra2 = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pa + up), 0, bytes_a, 0x00020000);
+    const auto rb = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pb), 0, bytes_b, 0x00020000);
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
       const int q = wv + NW * i;
       uint8_t* dst = to + q / QA * P::Plane + q % QA * 1024;
-      uint32_t off = oa[i];
-      if (AL == kRow && tail && ka[i] >= left) off = 0x80000000u;
+      const uint32_t off = AL == kRow && k_piece >= left - q / QA * KP ? 0x80000000u : oa[i];  // past every descriptor's end
       if (MATS == 2 && second[i])
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ra2, (lds_u8*)dst, 16, off, 0, 0, 0);
       else
@@ -175,9 +185,17 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     for (int i = 0; i < NB; ++i) {
       const int q = wv + NW * i;
       uint8_t* dst = to + q / QB * P::Plane + P::ABytes + q % QB * 1024;
-      uint32_t off = ob[i];
-      if (BL == kRow && tail && kb[i] >= left) off = 0x80000000u;
+      const uint32_t off = BL == kRow && k_piece >= left - q / QB * KP ? 0x80000000u : ob[i];
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_u8*)dst, 16, off, 0, 0, 0);
+    }
+    --more;
+    left -= KP * WK;
+    pa += step_a;
+    pb += step_b;
+    if (left <= 0) {  // the second segment
+      left = a.K;
+      pa = pa_next;
+      pb = pb_next;
     }
   };
 
@@ -243,10 +261,10 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     }
   };
 
-  auto compute = [&](const uint8_t* __restrict__ from, const float (&fa)[MATS], const float (&fb)[C]) {
-    const uint8_t* al = from + wk * P::Plane;
-    const uint8_t* bl = al + P::ABytes;
-    if constexpr (T == kTypeF8) {
+  if constexpr (T == kTypeF8) {
+    auto compute = [&](const uint8_t* __restrict__ from, const float (&fa)[MATS], const float (&fb)[C]) {
+      const uint8_t* al = from + wk * P::Plane;
+      const uint8_t* bl = al + P::ABytes;
       u32x4 b[C][2];
 #pragma unroll
       for (int t = 0; t < C; ++t)
@@ -264,51 +282,100 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
           for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(v[e], f, acc[i][t][e]);
         }
       }
-    } else {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        u32x4 b[C], v[R];
-#pragma unroll
-        for (int t = 0; t < C; ++t) b[t] = read(LB{}, CB{}, bl, wn * (BN / WN) + t * 16, s);
-#pragma unroll
-        for (int i = 0; i < R; ++i) v[i] = read(LA{}, CA{}, al, piece_row(i), s);
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-          for (int t = 0; t < C; ++t) acc[i][t] = dense_mfma<T>(v[i], v[i], b[t], b[t], acc[i][t]);
-      }
-    }
-  };
-  // one stage computed while the requests of the next ST - 1 are in flight; the
-  // parts of LDS are told apart by the pointers' restrict, without which every
-  // read of LDS would wait for all requests
-  auto step = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from, int k) {
-    float fa[MATS], fb[C];
-    if constexpr (T == kTypeF8) {
+    };
+    // one stage computed while the requests of the next ST - 1 are in flight; the
+    // parts of LDS are told apart by the pointers' restrict, without which every
+    // read of LDS would wait for all requests
+    auto step = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from, int k) {
+      float fa[MATS], fb[C];
 #pragma unroll
       for (int w = 0; w < MATS; ++w) fa[w] = sa[w];
 #pragma unroll
       for (int t = 0; t < C; ++t) fb[t] = sb[t];
-      if (k + 1 < k_last) scales(k + 1);
-    }
-    if (k + ST - 1 < k_last) request(to, k + ST - 1);
-    compute(from, fa, fb);
-  };
-
-  if constexpr (T == kTypeF8) scales(k_first);
+      scales(min(k + 1, k_last - 1));
+      request(to);
+      compute(from, fa, fb);
+    };
+    scales(k_first);
 #pragma unroll
-  for (int i = 0; i < ST - 1; ++i)
-    if (k_first + i < k_last) request(lds + i * P::Bytes, k_first + i);
-  int cur = 0;
-  for (int k = k_first; k < k_last; ++k) {
-    // stage k is in LDS, and every wave has left the part that k + ST - 1 goes to
-    if (k + ST - 2 < k_last)
+    for (int i = 0; i < ST - 1; ++i) request(lds + i * P::Bytes);
+    int cur = 0;
+    for (int k = k_first; k < k_last; ++k) {
+      // stage k is in LDS, and every wave has left the part that k + ST - 1 goes to
       wait_stage<P::Requests * (ST - 2)>();
-    else
-      wait_stage<0>();
-    const int nxt = cur == 0 ? ST - 1 : cur - 1;
-    step(lds + nxt * P::Bytes, lds + cur * P::Bytes, k);
-    cur = cur == ST - 1 ? 0 : cur + 1;
+      const int nxt = cur == 0 ? ST - 1 : cur - 1;
+      step(lds + nxt * P::Bytes, lds + cur * P::Bytes, k);
+      cur = cur == ST - 1 ? 0 : cur + 1;
+    }
+    wait_all_requests();  // none may arrive in LDS that is no longer this block's
+  } else {
+    // Two steps of K = 32 a plane.  Each step's operands are read while products of the
+    // other run, and the loads of stage k + ST are handed out between products too, as
+    // the address unit takes 16 cycles for each: nothing of it waits in a row.  One
+    // barrier a stage, where its second operands are read (its part of LDS is free) and
+    // the next stage has arrived.
+    struct Ops {
+      u32x4 a[R], b[C];
+    };
+    auto load = [&](const uint8_t* __restrict__ from, int s, Ops& o) {
+      const uint8_t* al = from + wk * P::Plane;
+      const uint8_t* bl = al + P::ABytes;
+#pragma unroll
+      for (int t = 0; t < C; ++t) o.b[t] = read(LB{}, CB{}, bl, wn * (BN / WN) + t * 16, s);
+#pragma unroll
+      for (int i = 0; i < R; ++i) o.a[i] = read(LA{}, CA{}, al, piece_row(i), s);
+    };
+    auto multiply = [&](const Ops& o, auto from, auto to) {
+#pragma unroll
+      for (int j = decltype(from)::value; j < decltype(to)::value; ++j) {
+        const int i = j / C, t = j % C;
+        acc[i][t] = dense_mfma<T>(o.a[i], o.a[i], o.b[t], o.b[t], acc[i][t]);
+      }
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, P::N1>;
+    using I2 = std::integral_constant<int, R * C>;
+    // requests and reads of different parts of LDS, told apart by restrict, without
+    // which every read would wait for all requests
+    auto second = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from, Ops& o0, const Ops& o1) {
+      request(to);
+      multiply(o0, I1{}, I2{});
+      load(from, 0, o0);
+      multiply(o1, I0{}, I2{});
+#pragma unroll
+      for (int i = 0; i < P::Requests; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, P::M3, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < P::Reads; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, P::M2, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    Ops o0, o1;
+#pragma unroll
+    for (int i = 0; i < ST; ++i) request(lds + i * P::Bytes);
+    wait_stage<P::Requests * (ST - 1)>();
+    load(lds, 0, o0);
+    int cur = 0;
+    for (int k = k_first; k < k_last; ++k) {
+      const int nxt = cur == ST - 1 ? 0 : cur + 1;
+      load(lds + cur * P::Bytes, 1, o1);
+      multiply(o0, I0{}, I1{});
+#pragma unroll
+      for (int i = 0; i < P::Reads; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // stage k + 1 is in LDS, and every wave has read all of stage k
+      wait_stage<P::Requests * (ST - 2)>();
+      second(lds + cur * P::Bytes, lds + nxt * P::Bytes, o0, o1);
+      cur = nxt;
+    }
+    wait_all_requests();  // none may arrive in LDS that is no longer this block's
   }
   if constexpr (WK > 1) {
     // the groups' sums, added by the first one
@@ -429,8 +496,12 @@ hipError_t dense_launch(const DenseArgs& a, int tile, int batches, hipStream_t s
   }
   switch (tile) {
     SI_DENSE_TILE(2, 2, 2, 2, 3)
-    SI_DENSE_TILE(3, 2, 2, 1, 2)
-    SI_DENSE_TILE(4, 2, 4, 1, 2)
+    SI_DENSE_TILE(3, 4, 2, 1, 2)
+  }
+  if constexpr (T == kTypeF8) {
+    if (tile == 4) return dense_tile_launch<T, AL, BL, MATS, kDenseTiles[4].bm, kDenseTiles[4].bn, 2, 4, 1, 2>(a, batches, s);
+  } else {
+    if (tile == 4) return dense_tile_launch<T, AL, BL, MATS, kDenseTiles[4].bm, kDenseTiles[4].bn, 4, 2, 1, 2>(a, batches, s);
   }
 #undef SI_DENSE_TILE
   return hipErrorInvalidValue;
