@@ -35,6 +35,8 @@ struct DenseShape {
 };
 constexpr DenseShape kDenseTiles[] = {{64, 16, 4, 512}, {64, 32, 4, 512}, {64, 64, 2, 512}, {128, 128, 1, 512}, {256, 256, 1, 512}};
 constexpr int kDenseTileCount = 5;
+constexpr int kDenseFew = 100;  // in place of a tile: the kernel for up to kFewTokens rows of B (dense_few.hip)
+constexpr int kFewTokens = 4;
 
 // Instances (dense_*.hip): value type, layouts of A and B, matrices.
 hipError_t dense_rr(int type, const DenseArgs& a, int tile, hipStream_t s);                 // x W^T
@@ -42,6 +44,7 @@ hipError_t dense_gated(int type, const DenseArgs& a, int tile, hipStream_t s);  
 hipError_t dense_cr(int type, const DenseArgs& a, int tile, hipStream_t s);                 // dy W
 hipError_t dense_cc(int type, const DenseArgs& a, int tile, int batches, hipStream_t s);    // dy^T x
 hipError_t dense_fp8(const DenseArgs& a, int mats, int tile, hipStream_t s);
+hipError_t dense_few(int type, int mats, const DenseArgs& a, hipStream_t s);                // x W^T, a few tokens; type 2: e4m3
 
 // ---- calls (dense.hip), arguments validated by the caller ----------------------
 

@@ -128,6 +128,7 @@ __global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, size_t size) {
 namespace {
 
 constexpr long kBlocks = 256;  // compute units
+constexpr int kTypeE4M3 = 2;   // dense_few's type of values
 
 int pad8(int n) { return (n + 7) / 8 * 8; }
 
@@ -156,9 +157,13 @@ struct Plan {
 };
 
 // Which tile, and in how many parts the sum is taken, by an estimate of the time:
-// rounds of blocks over the compute units, each as long as its products or its
-// stages' bytes take, and the second launch that joins parts.
-Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows) {
+// rounds of blocks over the compute units, each as long as its products or its loads
+// from L2 take, no less than the operands' bytes at the memory's rate, and the second
+// launch that joins parts.  The rates are those measured on large products (products of
+// 8192^3, TFLOP/s of the whole card: 256 x 256 tiles 1260-1320, 128 x 128 1040, e4m3
+// 1800-1950 and 1790).  Up to 4 tokens W's rows go through dense_few.hip.
+Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows, bool few) {
+  if (few && N <= kFewTokens && M < (1 << 24)) return {kDenseFew, 1, 0};
   Plan best = {-1, 1, 0};
   double best_t = 1e30;
   for (int i = b_rows ? 0 : 2; i < kDenseTileCount; ++i) {
@@ -167,15 +172,18 @@ Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows) {
     const int kp = 128 / es * t.wk;
     const long stages = (K + kp - 1) / kp;
     const int resident = i == 3 ? 2 : 1;
-    const double rate = (i == 4 ? 5.0e12 : i == 3 ? 4.1e12 : 3.0e12) * (es == 1 ? 1.8 : 1.0) / resident;  // flop/s of a block
+    // of a block, in 1e6 flop/us and bytes/us
+    const double rate = (es == 1 ? (i == 4 ? 7.4 : i == 3 ? 6.9 : 3.0) : (i == 4 ? 5.0 : i == 3 ? 4.1 : 2.5)) / resident;
+    const double l2 = 0.07e6 / resident, memory = 5.0e6;
+    const double bytes = ((double)M * mats + N) * (double)K * es * batches;
     for (int split = 1; split <= 16; split *= 2) {
       if (split > 1 && stages < 4 * split) break;
       if ((double)blocks * split * t.threads >= 4294967296.0) break;  // threads of a launch
       const double rounds = (double)((blocks * split + kBlocks * resident - 1) / (kBlocks * resident));
       const double k = (double)((stages + split - 1) / split) * kp;
-      const double mul = 2.0 * t.bm * t.bn * k / rate, move = (t.bm + t.bn) * k * es / (22e9 / resident * 1e0) * 1e0;
-      double us = rounds * (std::max(mul, move) * 1e6 + 2.0);
+      const double mul = 2e-6 * t.bm * t.bn * k / rate, move = (t.bm + t.bn) * k * es / l2;
       const double size = (double)M * N * mats * batches * 4;
+      double us = std::max(rounds * (std::max(mul, move) + 2.0), bytes / memory);
       if (split > 1) us += 3.0 + size * (2 * split + 1) / 4e6;
       if (us < best_t) {
         best_t = us;
@@ -197,13 +205,13 @@ hipError_t join(const DenseArgs& a, int mats, int batches, hipStream_t s) {
   return hipGetLastError();
 }
 
-Plan linear_plan(const DenseLinear& c) { return plan_of(c.rows, c.m, c.n, c.w_up.p ? 2 : 1, 1, 2, true); }
-Plan dx_plan(const DenseGrad& c) { return plan_of(c.n, c.m, (long)c.rows * (c.w_up.p ? 2 : 1), 1, 1, 2, true); }
+Plan linear_plan(const DenseLinear& c) { return plan_of(c.rows, c.m, c.n, c.w_up.p ? 2 : 1, 1, 2, true, !c.transposed); }
+Plan dx_plan(const DenseGrad& c) { return plan_of(c.n, c.m, (long)c.rows * (c.w_up.p ? 2 : 1), 1, 1, 2, true, c.transposed && !c.w_up.p); }
 Plan dw_plan(const DenseGrad& c) {
-  return c.transposed ? plan_of(c.rows, c.n, c.m, 1, 1, 2, false)
-                      : plan_of(c.n, c.rows, c.m, 1, c.w_up.p ? 2 : 1, 2, false);
+  return c.transposed ? plan_of(c.rows, c.n, c.m, 1, 1, 2, false, false)
+                      : plan_of(c.n, c.rows, c.m, 1, c.w_up.p ? 2 : 1, 2, false, false);
 }
-Plan fp8_plan(const DenseFp8& c) { return plan_of(c.rows, c.m, c.n, c.q_up ? 2 : 1, 1, 1, true); }
+Plan fp8_plan(const DenseFp8& c) { return plan_of(c.rows, c.m, c.n, c.q_up ? 2 : 1, 1, 1, true, true); }
 
 size_t weight_copies(const DenseMat& w, const DenseMat& w_up, bool transposed, int type, int rows, int n) {
   const int r = transposed ? n : rows, c = transposed ? rows : n;
@@ -255,6 +263,7 @@ hipError_t launch_dense_linear(const DenseLinear& c, hipStream_t s) {
   a.save_dtype = c.type;
   set_plan(a, p, mats, ws);
   const int type = c.type == kBF16 ? 1 : 0;
+  if (p.tile == kDenseFew) return dense_few(type, mats, a, s);
   TRY(mats == 2 ? dense_gated(type, a, p.tile, s) : c.transposed ? dense_cr(type, a, p.tile, s)
                                                                  : dense_rr(type, a, p.tile, s));
   return join(a, mats, 1, s);
@@ -316,7 +325,8 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
     a.c[0] = c.dx;
     a.c_dtype = c.type;
     set_plan(a, p, 1, ws);
-    TRY(c.transposed ? dense_rr(type, a, p.tile, s) : dense_cr(type, a, p.tile, s));
+    TRY(p.tile == kDenseFew ? dense_few(type, 1, a, s) : c.transposed ? dense_rr(type, a, p.tile, s)
+                                                                      : dense_cr(type, a, p.tile, s));
     TRY(join(a, 1, 1, s));
   }
   if (c.dw || c.dw_up) {
@@ -384,6 +394,7 @@ hipError_t launch_dense_fp8(const DenseFp8& c, hipStream_t s) {
   a.sb = c.xs;
   a.blocks = fp8_blocks(c.n);
   set_plan(a, p, mats, static_cast<char*>(c.ws));
+  if (p.tile == kDenseFew) return dense_few(kTypeE4M3, mats, a, s);
   TRY(dense_fp8(a, mats, p.tile, s));
   return join(a, mats, 1, s);
 }

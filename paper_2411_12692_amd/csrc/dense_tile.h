@@ -50,6 +50,8 @@ __device__ inline f32x4 dense_mfma(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x4
 // max(g, 0) where a NaN stays one
 __device__ inline float relu(float g) { return g > 0.f || g != g ? g : 0.f; }
 
+constexpr int kScaleStages = 8;
+
 template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST>
 struct DenseTile {
   static constexpr int NW = WM * WN * WK;
@@ -59,6 +61,11 @@ struct DenseTile {
   static constexpr int ABytes = BM * 128, BBytes = BN * 128, Plane = ABytes + BBytes, Bytes = WK * Plane;
   static constexpr int IA = WK * ABytes / 1024, IB = WK * BBytes / 1024;  // wave requests of a stage
   static constexpr int Requests = (IA + IB) / NW;
+  // e4m3, one plane a stage: the scales of all tokens of the tile and of two blocks of
+  // rows pass through LDS too, kScaleStages stages' at a time
+  static constexpr bool Chunked = T == kTypeF8 && WK == 1 && ST == 2;
+  static constexpr int ScaleB = BN * kScaleStages * 4, ScaleBytes = Chunked ? ScaleB + 256 : 0;
+  static constexpr int Lds = ST * Bytes + 2 * ScaleBytes;
   // LDS reads of a step, and the products between two of them, or two requests
   static constexpr int Reads = (AL == kRow ? R : 2 * R) + (BL == kRow ? C : 2 * C);
   // products before a stage's barrier, between two requests behind it, and between two
@@ -69,7 +76,8 @@ struct DenseTile {
   static_assert(R % MATS == 0 && (MATS == 1 || AL == kRow), "both matrices' pieces in each wave");
   static_assert(T != kTypeF8 || (AL == kRow && BL == kRow && BM / MATS / WM <= 128), "a wave's rows share scales");
   static_assert(Requests * (ST - 1) < 64, "what a wait can leave outstanding");
-  static_assert(ST * Bytes <= kMaxLds, "LDS of a compute unit");
+  static_assert(Lds <= kMaxLds, "LDS of a compute unit");
+  static_assert(!Chunked || (BN * kScaleStages / 64 % NW == 0 && BM / MATS <= 256), "the scales' loads");
   static_assert((WK - 1) * BM * BN * 4 <= ST * Bytes, "the groups' sums");
 };
 
@@ -261,7 +269,88 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     }
   };
 
-  if constexpr (T == kTypeF8) {
+  if constexpr (P::Chunked) {
+    // Stage k's scales lie in LDS, brought there a chunk of stages at a time: token
+    // after token, and behind them two rows of A's blocks (of each matrix, or two
+    // blocks of rows of one).  Past the last block and the last token they are zeros.
+    uint8_t* const scale_lds = lds + ST * P::Bytes;
+    auto request_scales = [&](int chunk) {
+      uint8_t* const to = scale_lds + (chunk & 1) * P::ScaleBytes;
+      const int b0 = chunk * kScaleStages, end = a.blocks - b0;
+      const auto r = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<float*>(a.sb + (size_t)n0 * a.blocks + b0), 0, max(((b_rows - 1) * a.blocks + end) * 4, 0), 0x00020000);
+#pragma unroll
+      for (int i = 0; i < BN * kScaleStages / 64 / NW; ++i) {
+        const int q = wv + NW * i, tok = q * 8 + lane / 8, b = (lane & 7) ^ ((q & 1) * 4);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u8*)(to + q * 256), 4,
+                                                 b < end ? (uint32_t)(tok * a.blocks + b) * 4 : 0x80000000u, 0, 0, 0);
+      }
+      if (wv == 0) {
+        // lanes 0-7 the first row of blocks, 8-15 the second
+        const int w = lane >> 3, b = lane & 7;
+        const float* p = MATS == 2 && w == 1 ? a.sa[1] : a.sa[0];
+        const int row = min(m0 / 128 + (MATS == 1 ? w : 0), (a.M - 1) / 128);
+        float v = 0.f;
+        if (w < 2 && b < end) v = p[(size_t)row * a.blocks + b0 + b];
+        if (lane < 16) *reinterpret_cast<float*>(to + P::ScaleB + lane * 4) = v;
+      }
+    };
+    // the scale of the products of piece (i's matrix, t) in stage k
+    const int row_slot = MATS == 1 ? wm * (BM / WM) / 128 : 0;
+    auto factor_a = [&](int k, int w) {
+      return *reinterpret_cast<const float*>(scale_lds + (k / kScaleStages & 1) * P::ScaleBytes + P::ScaleB +
+                                             ((MATS == 2 ? w : row_slot) * 8 + (k & 7)) * 4);
+    };
+    auto factor_b = [&](int k, int t) {
+      const int tok = wn * (BN / WN) + t * 16 + r;
+      return *reinterpret_cast<const float*>(scale_lds + (k / kScaleStages & 1) * P::ScaleBytes + tok * 32 +
+                                             (((k & 7) ^ ((tok >> 3 & 1) * 4)) * 4));
+    };
+    auto step = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from, int k) {
+      request(to);
+      u32x4 b[C][2];
+      float fa[MATS], fb[C];
+#pragma unroll
+      for (int w = 0; w < MATS; ++w) fa[w] = factor_a(k, w);
+#pragma unroll
+      for (int t = 0; t < C; ++t) {
+        fb[t] = factor_b(k, t);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) b[t][s] = read(LB{}, CB{}, from + P::ABytes, wn * (BN / WN) + t * 16, s);
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const u32x4 a0 = read(LA{}, CA{}, from, piece_row(i), 0), a1 = read(LA{}, CA{}, from, piece_row(i), 1);
+#pragma unroll
+        for (int t = 0; t < C; ++t) {
+          const f32x4 v = dense_mfma<T>(a0, a1, b[t][0], b[t][1], f32x4{0.f, 0.f, 0.f, 0.f});
+          const float f = fa[MATS == 2 ? i / (R / 2) : 0] * fb[t];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(v[e], f, acc[i][t][e]);
+        }
+      }
+      if constexpr (R * C >= 32) {
+        // a request, a product and a read in turn behind the first operands
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * C + 2 + C + MATS, 0);
+#pragma unroll
+        for (int i = 0; i < P::Requests; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+      }
+    };
+    request_scales(k_first / kScaleStages);
+    request_scales(k_first / kScaleStages + 1);
+    request(lds);
+    for (int k = k_first; k < k_last; ++k) {
+      const int cur = (k - k_first) & 1;
+      wait_stage<0>();  // stage k is in LDS, and every wave has left the other part
+      if ((k & (kScaleStages - 1)) == 0 && k > k_first) request_scales(k / kScaleStages + 1);
+      step(lds + (cur ^ 1) * P::Bytes, lds + cur * P::Bytes, k);
+    }
+    wait_all_requests();  // none may arrive in LDS that is no longer this block's
+  } else if constexpr (T == kTypeF8) {
     auto compute = [&](const uint8_t* __restrict__ from, const float (&fa)[MATS], const float (&fb)[C]) {
       const uint8_t* al = from + wk * P::Plane;
       const uint8_t* bl = al + P::ABytes;
@@ -471,13 +560,13 @@ hipError_t dense_tile_launch(DenseArgs a, int batches, hipStream_t s) {
   static std::atomic<int> attr_set[kMaxDevices];
   const int ok = per_device_once(attr_set, [](int) -> int {
     return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_dense<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, ST * P::Bytes) == hipSuccess ? 1 : -1;
+                               hipFuncAttributeMaxDynamicSharedMemorySize, P::Lds) == hipSuccess ? 1 : -1;
   });
   if (ok != 1) return hipErrorInvalidConfiguration;
   a.m_tiles = (a.M + BM / MATS - 1) / (BM / MATS);
   a.n_tiles = (a.N + BN - 1) / BN;
   k_dense<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>
-      <<<(unsigned)(a.m_tiles * a.n_tiles * a.split * batches), WM * WN * WK * kWave, ST * P::Bytes, s>>>(a);
+      <<<(unsigned)(a.m_tiles * a.n_tiles * a.split * batches), WM * WN * WK * kWave, P::Lds, s>>>(a);
   return hipGetLastError();
 }
 
@@ -497,11 +586,7 @@ hipError_t dense_launch(const DenseArgs& a, int tile, int batches, hipStream_t s
   switch (tile) {
     SI_DENSE_TILE(2, 2, 2, 2, 3)
     SI_DENSE_TILE(3, 4, 2, 1, 2)
-  }
-  if constexpr (T == kTypeF8) {
-    if (tile == 4) return dense_tile_launch<T, AL, BL, MATS, kDenseTiles[4].bm, kDenseTiles[4].bn, 2, 4, 1, 2>(a, batches, s);
-  } else {
-    if (tile == 4) return dense_tile_launch<T, AL, BL, MATS, kDenseTiles[4].bm, kDenseTiles[4].bn, 4, 2, 1, 2>(a, batches, s);
+    SI_DENSE_TILE(4, 4, 2, 1, 2)
   }
 #undef SI_DENSE_TILE
   return hipErrorInvalidValue;
