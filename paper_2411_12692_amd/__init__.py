@@ -852,6 +852,8 @@ def _grad_rows(dy):
     transposed are copied.  Returns ``(dy2, stride)``."""
     dy2 = dy if dy.dim() == 2 else dy.reshape(-1, dy.shape[-1])
     m, n = dy2.shape
+    if dy2.is_contiguous():
+        return dy2, n
     if (n > 1 and dy2.stride(1) != 1) or (m > 1 and not n <= dy2.stride(0) <= 1 << 21):
         dy2 = dy2.contiguous()
     return dy2, dy2.stride(0) if m > 1 else n
@@ -888,6 +890,17 @@ def _linear_forward(x2, m, n, ld, w, rows, transposed, out_dtype):
     return y
 
 
+def _first_order(backward):
+    """The gradients have none of their own: where a graph of the backward pass is
+    asked for, its use raises (``once_differentiable``); else that wrapper's time is
+    saved."""
+    guarded = torch.autograd.function.once_differentiable(backward)
+
+    def run(ctx, dy):
+        return guarded(ctx, dy) if torch.is_grad_enabled() else backward(ctx, dy)
+    return run
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x2, w, m, n, ld, rows, transposed, out_dtype):
@@ -896,7 +909,7 @@ class _Linear(torch.autograd.Function):
         return _linear_forward(x2, m, n, ld, w, rows, transposed, out_dtype)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_first_order
     def backward(ctx, dy):
         x2, w = ctx.saved_tensors
         m, n, ld, rows, transposed = ctx.args
@@ -954,7 +967,7 @@ class _GatedLinear(torch.autograd.Function):
         return h
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_first_order
     def backward(ctx, dh):
         x2, w_gate, w_up, g, u = ctx.saved_tensors
         m, n, ld, rows = ctx.args
@@ -1023,7 +1036,7 @@ class _Norm(torch.autograd.Function):
         return y
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_first_order
     def backward(ctx, dy):
         x2, w, mean, rstd = ctx.saved_tensors
         tokens, d, ld, center = ctx.args

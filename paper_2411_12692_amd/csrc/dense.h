@@ -31,10 +31,11 @@ struct DenseArgs {
 // Tiles by size: values along m (both matrices of a gated product) and n, planes of
 // a stage.  The first two are for few rows of B, which then lie along k.
 struct DenseShape {
-  int bm, bn, wk, threads;
+  int bm, bn, wk, threads, st;  // st: stages in LDS
 };
-constexpr DenseShape kDenseTiles[] = {{64, 16, 4, 512}, {64, 32, 4, 512}, {64, 64, 2, 512}, {128, 128, 1, 512}, {256, 256, 1, 512}};
-constexpr int kDenseTileCount = 5;
+constexpr DenseShape kDenseTiles[] = {{64, 16, 4, 512, 3},   {64, 32, 4, 512, 3},   {64, 64, 2, 512, 3},
+                                      {128, 128, 1, 512, 2}, {128, 256, 1, 512, 3}, {256, 256, 1, 512, 2}};
+constexpr int kDenseTileCount = 6;
 constexpr int kDenseFew = 100;  // in place of a tile: the kernel for up to kFewTokens rows of B (dense_few.hip)
 constexpr int kFewTokens = 4;
 

@@ -13,27 +13,38 @@
 
 namespace si {
 
-// A copy of `rows` rows of n values with rows of whole 8, zeros behind the n-th, in
-// fp16 or bf16: 8 values a thread.
-__global__ __launch_bounds__(256) void k_dense_pad(const void* __restrict__ src, int dtype, size_t ld, size_t rows, int n,
-                                                   int np, int type, u32x4* __restrict__ out) {
+// Copies of matrices, rows of n values, with rows of whole 8, zeros behind the n-th, in
+// fp16 or bf16: 8 values a thread, a matrix for each blockIdx.y.
+struct PadJob {
+  DenseMat src;
+  size_t rows;
+  int n, np;
+  u32x4* out;
+};
+struct PadJobs {
+  PadJob job[4];
+  int count, type;
+};
+
+__global__ __launch_bounds__(256) void k_dense_pad(PadJobs jobs) {
+  const PadJob& j = jobs.job[blockIdx.y];
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows * (size_t)(np / 8)) return;
-  const size_t r = i / (np / 8);
-  const int c = (int)(i - r * (np / 8)) * 8;
+  if (i >= j.rows * (size_t)(j.np / 8)) return;
+  const size_t r = i / (j.np / 8);
+  const int c = (int)(i - r * (j.np / 8)) * 8;
   u32x4 v = {0, 0, 0, 0};
-  if (dtype == type && c + 8 <= n) {
-    v = *reinterpret_cast<const u32x4_e2*>(static_cast<const uint16_t*>(src) + r * ld + c);
+  if (j.src.dtype == jobs.type && c + 8 <= j.n) {
+    v = *reinterpret_cast<const u32x4_e2*>(static_cast<const uint16_t*>(j.src.p) + r * j.src.ld + c);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (c + e < n) {
-        const float f = load_one(src, r * ld + c + e, dtype);
-        const uint32_t h = (type == kF16 ? pack_f2(f, 0.f) : pack_bf2(f, 0.f)) & 0xffffu;
+      if (c + e < j.n) {
+        const float f = load_one(j.src.p, r * j.src.ld + c + e, j.src.dtype);
+        const uint32_t h = (jobs.type == kF16 ? pack_f2(f, 0.f) : pack_bf2(f, 0.f)) & 0xffffu;
         v[e >> 1] |= h << (16 * (e & 1));
       }
   }
-  out[i] = v;
+  j.out[i] = v;
 }
 
 // dg and du of `rows` values a token, in rows of rp (zeros behind), 8 values a
@@ -139,17 +150,31 @@ size_t copy_bytes(const DenseMat& a, int type, size_t rows, int n) {
   return a.p && needs_copy(a, type, n) ? align256(rows * pad8(n) * 2) : 0;
 }
 
-// The matrix itself, or its copy at `ws`, which is moved behind it.
-hipError_t whole_rows(DenseMat& a, int type, size_t rows, int n, char*& ws, hipStream_t s) {
-  if (!a.p || !needs_copy(a, type, n)) return hipSuccess;
-  const int np = pad8(n);
-  const size_t all = rows * (np / 8);
-  k_dense_pad<<<(unsigned)((all + 255) / 256), 256, 0, s>>>(a.p, a.dtype, a.ld, rows, n, np, type,
-                                                            reinterpret_cast<u32x4*>(ws));
-  a = DenseMat{ws, type, (size_t)np};
-  ws += align256(all * 16);
-  return hipGetLastError();
-}
+// Replaces matrices that cannot be read in whole pieces by copies in the workspace,
+// all of a call's in one launch.
+class Copies {
+ public:
+  Copies(int type, char*& ws) : ws_(ws) { jobs_.type = type; }
+  void add(DenseMat& a, size_t rows, int n) {
+    if (!a.p || !needs_copy(a, jobs_.type, n)) return;
+    const int np = pad8(n);
+    jobs_.job[jobs_.count++] = PadJob{a, rows, n, np, reinterpret_cast<u32x4*>(ws_)};
+    a = DenseMat{ws_, jobs_.type, (size_t)np};
+    const size_t all = rows * (np / 8);
+    ws_ += align256(all * 16);
+    most_ = std::max(most_, all);
+  }
+  hipError_t launch(hipStream_t s) const {
+    if (jobs_.count == 0) return hipSuccess;
+    k_dense_pad<<<dim3((unsigned)((most_ + 255) / 256), (unsigned)jobs_.count), 256, 0, s>>>(jobs_);
+    return hipGetLastError();
+  }
+
+ private:
+  char*& ws_;
+  PadJobs jobs_ = {};
+  size_t most_ = 0;
+};
 
 struct Plan {
   int tile, split;
@@ -173,17 +198,20 @@ Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows, b
     const long stages = (K + kp - 1) / kp;
     const int resident = i == 3 ? 2 : 1;
     // of a block, in 1e6 flop/us and bytes/us
-    const double rate = (es == 1 ? (i == 4 ? 7.4 : i == 3 ? 6.9 : 3.0) : (i == 4 ? 5.0 : i == 3 ? 4.1 : 2.5)) / resident;
+    const double rate = (es == 1 ? (i == 5 ? 7.4 : i >= 3 ? 6.9 : 3.0) : (i == 5 ? 5.0 : i == 4 ? 4.3 : i == 3 ? 4.1 : 2.5)) / resident;
     const double l2 = 0.07e6 / resident, memory = 5.0e6;
+    // a stage's loads take this long to arrive: from memory where few tiles share W
+    const double latency = (((N + t.bn - 1) / t.bn) <= 2 ? 1.8 : 0.9) / (t.st - 1);
     const double bytes = ((double)M * mats + N) * (double)K * es * batches;
     for (int split = 1; split <= 16; split *= 2) {
       if (split > 1 && stages < 4 * split) break;
       if ((double)blocks * split * t.threads >= 4294967296.0) break;  // threads of a launch
       const double rounds = (double)((blocks * split + kBlocks * resident - 1) / (kBlocks * resident));
       const double k = (double)((stages + split - 1) / split) * kp;
+      const double wait = (double)((stages + split - 1) / split) * latency;
       const double mul = 2e-6 * t.bm * t.bn * k / rate, move = (t.bm + t.bn) * k * es / l2;
       const double size = (double)M * N * mats * batches * 4;
-      double us = std::max(rounds * (std::max(mul, move) + 2.0), bytes / memory);
+      double us = std::max(rounds * (std::max(std::max(mul, move), wait) + 2.0), bytes / memory);
       if (split > 1) us += 3.0 + size * (2 * split + 1) / 4e6;
       if (us < best_t) {
         best_t = us;
@@ -240,9 +268,11 @@ hipError_t launch_dense_linear(const DenseLinear& c, hipStream_t s) {
   char* ws = static_cast<char*>(c.ws);
   DenseMat x = c.x, w = c.w, up = c.w_up;
   const int wr = c.transposed ? c.n : c.rows, wc = c.transposed ? c.rows : c.n;
-  TRY(whole_rows(x, c.type, c.m, c.n, ws, s));
-  TRY(whole_rows(w, c.type, wr, wc, ws, s));
-  TRY(whole_rows(up, c.type, wr, wc, ws, s));
+  Copies copies(c.type, ws);
+  copies.add(x, c.m, c.n);
+  copies.add(w, wr, wc);
+  copies.add(up, wr, wc);
+  TRY(copies.launch(s));
   const Plan p = linear_plan(c);
   const int mats = up.p ? 2 : 1;
   DenseArgs a = {};
@@ -285,6 +315,9 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
   char* ws = static_cast<char*>(c.ws);
   const int type = c.type == kBF16 ? 1 : 0;
   DenseMat d = c.dy, du = {};
+  DenseMat x = c.x, w = c.w, up = c.w_up;
+  const bool want_w = c.dw || c.dw_up;
+  Copies copies(c.type, ws);
   if (c.gate.p) {
     const int rp = pad8(c.rows);
     const size_t bytes = align256((size_t)c.m * rp * 2), all = (size_t)c.m * (rp / 8);
@@ -302,14 +335,16 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
     }
     TRY(hipGetLastError());
   } else {
-    TRY(whole_rows(d, c.type, c.m, c.rows, ws, s));
+    copies.add(d, c.m, c.rows);
   }
-  DenseMat x = c.x, w = c.w, up = c.w_up;
-  if (c.dw || c.dw_up) TRY(whole_rows(x, c.type, c.m, c.n, ws, s));
+  if (want_w) copies.add(x, c.m, c.n);
   if (c.dx) {
     const int wr = c.transposed ? c.n : c.rows, wc = c.transposed ? c.rows : c.n;
-    TRY(whole_rows(w, c.type, wr, wc, ws, s));
-    TRY(whole_rows(up, c.type, wr, wc, ws, s));
+    copies.add(w, wr, wc);
+    copies.add(up, wr, wc);
+  }
+  TRY(copies.launch(s));
+  if (c.dx) {
     const Plan p = dx_plan(c);
     DenseArgs a = {};
     a.a[0] = w.p;
@@ -329,7 +364,7 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
                                                                       : dense_cr(type, a, p.tile, s));
     TRY(join(a, 1, 1, s));
   }
-  if (c.dw || c.dw_up) {
+  if (want_w) {
     const Plan p = dw_plan(c);
     DenseArgs a = {};
     a.K = c.m;

@@ -50,7 +50,7 @@ __device__ inline f32x4 dense_mfma(u32x4 a0, u32x4 a1, u32x4 b0, u32x4 b1, f32x4
 // max(g, 0) where a NaN stays one
 __device__ inline float relu(float g) { return g > 0.f || g != g ? g : 0.f; }
 
-constexpr int kScaleStages = 8;
+constexpr int kScaleStages = 4;
 
 template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST>
 struct DenseTile {
@@ -63,8 +63,8 @@ struct DenseTile {
   static constexpr int Requests = (IA + IB) / NW;
   // e4m3, one plane a stage: the scales of all tokens of the tile and of two blocks of
   // rows pass through LDS too, kScaleStages stages' at a time
-  static constexpr bool Chunked = T == kTypeF8 && WK == 1 && ST == 2;
-  static constexpr int ScaleB = BN * kScaleStages * 4, ScaleBytes = Chunked ? ScaleB + 256 : 0;
+  static constexpr bool Chunked = T == kTypeF8 && WK == 1;
+  static constexpr int ScaleB = BN * kScaleStages * 4, ScaleBytes = Chunked ? ScaleB + 32 : 0;
   static constexpr int Lds = ST * Bytes + 2 * ScaleBytes;
   // LDS reads of a step, and the products between two of them, or two requests
   static constexpr int Reads = (AL == kRow ? R : 2 * R) + (BL == kRow ? C : 2 * C);
@@ -281,30 +281,29 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
           const_cast<float*>(a.sb + (size_t)n0 * a.blocks + b0), 0, max(((b_rows - 1) * a.blocks + end) * 4, 0), 0x00020000);
 #pragma unroll
       for (int i = 0; i < BN * kScaleStages / 64 / NW; ++i) {
-        const int q = wv + NW * i, tok = q * 8 + lane / 8, b = (lane & 7) ^ ((q & 1) * 4);
+        const int q = wv + NW * i, tok = q * 16 + lane / 4, b = lane & 3;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u8*)(to + q * 256), 4,
                                                  b < end ? (uint32_t)(tok * a.blocks + b) * 4 : 0x80000000u, 0, 0, 0);
       }
       if (wv == 0) {
-        // lanes 0-7 the first row of blocks, 8-15 the second
-        const int w = lane >> 3, b = lane & 7;
+        // lanes 0-3 the first row of blocks, 4-7 the second
+        const int w = lane >> 2, b = lane & 3;
         const float* p = MATS == 2 && w == 1 ? a.sa[1] : a.sa[0];
         const int row = min(m0 / 128 + (MATS == 1 ? w : 0), (a.M - 1) / 128);
         float v = 0.f;
         if (w < 2 && b < end) v = p[(size_t)row * a.blocks + b0 + b];
-        if (lane < 16) *reinterpret_cast<float*>(to + P::ScaleB + lane * 4) = v;
+        if (lane < 8) *reinterpret_cast<float*>(to + P::ScaleB + lane * 4) = v;
       }
     };
     // the scale of the products of piece (i's matrix, t) in stage k
     const int row_slot = MATS == 1 ? wm * (BM / WM) / 128 : 0;
     auto factor_a = [&](int k, int w) {
       return *reinterpret_cast<const float*>(scale_lds + (k / kScaleStages & 1) * P::ScaleBytes + P::ScaleB +
-                                             ((MATS == 2 ? w : row_slot) * 8 + (k & 7)) * 4);
+                                             ((MATS == 2 ? w : row_slot) * kScaleStages + k % kScaleStages) * 4);
     };
     auto factor_b = [&](int k, int t) {
       const int tok = wn * (BN / WN) + t * 16 + r;
-      return *reinterpret_cast<const float*>(scale_lds + (k / kScaleStages & 1) * P::ScaleBytes + tok * 32 +
-                                             (((k & 7) ^ ((tok >> 3 & 1) * 4)) * 4));
+      return *reinterpret_cast<const float*>(scale_lds + (k / kScaleStages & 1) * P::ScaleBytes + (tok * kScaleStages + k % kScaleStages) * 4);
     };
     auto step = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from, int k) {
       request(to);
@@ -342,12 +341,18 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     };
     request_scales(k_first / kScaleStages);
     request_scales(k_first / kScaleStages + 1);
-    request(lds);
+#pragma unroll
+    for (int i = 0; i < ST - 1; ++i) request(lds + i * P::Bytes);
+    int cur = 0;
     for (int k = k_first; k < k_last; ++k) {
-      const int cur = (k - k_first) & 1;
-      wait_stage<0>();  // stage k is in LDS, and every wave has left the other part
-      if ((k & (kScaleStages - 1)) == 0 && k > k_first) request_scales(k / kScaleStages + 1);
-      step(lds + (cur ^ 1) * P::Bytes, lds + cur * P::Bytes, k);
+      // stage k and its scales are in LDS (the scales' loads, between the stages', make
+      // the wait longer, never shorter), and every wave has left the part that stage
+      // k + ST - 1 goes to
+      wait_stage<P::Requests * (ST - 2)>();
+      if (k % kScaleStages == 0 && k > k_first) request_scales(k / kScaleStages + 1);
+      const int nxt = cur == 0 ? ST - 1 : cur - 1;
+      step(lds + nxt * P::Bytes, lds + cur * P::Bytes, k);
+      cur = cur == ST - 1 ? 0 : cur + 1;
     }
     wait_all_requests();  // none may arrive in LDS that is no longer this block's
   } else if constexpr (T == kTypeF8) {
@@ -575,7 +580,7 @@ template <int T, int AL, int BL, int MATS>
 hipError_t dense_launch(const DenseArgs& a, int tile, int batches, hipStream_t s) {
 #define SI_DENSE_TILE(I, WM, WN, WK, ST) \
   case I:                                \
-    static_assert(WK == kDenseTiles[I].wk && WM * WN * WK * kWave == kDenseTiles[I].threads, "kDenseTiles"); \
+    static_assert(WK == kDenseTiles[I].wk && WM * WN * WK * kWave == kDenseTiles[I].threads && ST == kDenseTiles[I].st, "kDenseTiles"); \
     return dense_tile_launch<T, AL, BL, MATS, kDenseTiles[I].bm, kDenseTiles[I].bn, WM, WN, WK, ST>(a, batches, s);
   if constexpr (BL == kRow) {
     switch (tile) {
@@ -586,7 +591,8 @@ hipError_t dense_launch(const DenseArgs& a, int tile, int batches, hipStream_t s
   switch (tile) {
     SI_DENSE_TILE(2, 2, 2, 2, 3)
     SI_DENSE_TILE(3, 4, 2, 1, 2)
-    SI_DENSE_TILE(4, 4, 2, 1, 2)
+    SI_DENSE_TILE(4, 2, 4, 1, 3)
+    SI_DENSE_TILE(5, 4, 2, 1, 2)
   }
 #undef SI_DENSE_TILE
   return hipErrorInvalidValue;

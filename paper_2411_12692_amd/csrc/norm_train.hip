@@ -72,26 +72,28 @@ __global__ __launch_bounds__(WAVE ? 256 : kLnThreads) void k_layer_norm(LayerNor
   }
 }
 
-// Sums of two values over the threads of a row.
-template <bool WAVE>
-__device__ inline void row_sums(float& p, float& q, float (*part)[2]) {
-  p = wave_total(p);
-  q = wave_total(q);
+// Sums of N values over the threads of a row.
+template <bool WAVE, int N>
+__device__ inline void row_sums(float (&v)[N], float (*part)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = wave_total(v[i]);
   if constexpr (!WAVE) {
     __syncthreads();  // the last sums' readers are done
     if ((threadIdx.x & (kWave - 1)) == 0) {
-      part[threadIdx.x / kWave][0] = p;
-      part[threadIdx.x / kWave][1] = q;
+#pragma unroll
+      for (int i = 0; i < N; ++i) part[threadIdx.x / kWave][i] = v[i];
     }
     __syncthreads();
-    p = q = 0.f;
-    for (int w = 0; w < (int)(blockDim.x / kWave); ++w) {
-      p += part[w][0];
-      q += part[w][1];
-    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    for (int w = 0; w < (int)(blockDim.x / kWave); ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += part[w][i];
   }
 }
 
+// A row at a time, the requests of the block's next row in flight meanwhile.  (Two rows
+// ahead, or two at a time with shared barriers: no faster.)
 template <bool VEC, bool WAVE, int U>
 __global__ __launch_bounds__(WAVE ? 256 : kLnThreads) void k_layer_norm_grad(LayerNormGrad a) {
   __shared__ float part[kLnThreads / kWave][2];
@@ -108,25 +110,27 @@ __global__ __launch_bounds__(WAVE ? 256 : kLnThreads) void k_layer_norm_grad(Lay
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[u][e] = db[u][e] = 0.f;
   }
-  Raw8 xr[U], gr[U];
-  float mean = 0.f, r = 0.f;
-  auto load = [&](size_t row) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      xr[u] = load_raw<VEC>(a.x, row * a.ldx, a.dtype, t, gt, u, d);
-      gr[u] = load_raw<VEC>(a.dy, row * a.ldy, a.dtype, t, gt, u, d);
-    }
-    if (a.center) mean = a.mean[row];
-    r = a.rstd[row];
+  struct Row {
+    Raw8 x[U], g[U];
+    float mean, r;
   };
-  if (first < a.tokens) load(first);
-  for (size_t row = first; row < a.tokens; row += stride) {
-    float n[U][8], g[U][8], se = 0.f, sn = 0.f;
-    const float rr = r;
+  auto load = [&](size_t row, Row& q) {
+    if (row >= a.tokens) return;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      to_floats(xr[u], a.dtype, n[u]);
-      to_floats(gr[u], a.dtype, g[u]);
+      q.x[u] = load_raw<VEC>(a.x, row * a.ldx, a.dtype, t, gt, u, d);
+      q.g[u] = load_raw<VEC>(a.dy, row * a.ldy, a.dtype, t, gt, u, d);
+    }
+    q.mean = a.center ? a.mean[row] : 0.f;
+    q.r = a.rstd[row];
+  };
+  auto take = [&](size_t row, Row& q) {
+    float n[U][8], g[U][8], sums[2] = {0.f, 0.f};
+    const float mean = q.mean, r = q.r;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      to_floats(q.x[u], a.dtype, n[u]);
+      to_floats(q.g[u], a.dtype, g[u]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         n[u][e] = (n[u][e] - mean) * r;
@@ -134,23 +138,25 @@ __global__ __launch_bounds__(WAVE ? 256 : kLnThreads) void k_layer_norm_grad(Lay
         db[u][e] += g[u][e];
         g[u][e] *= w[u][e];
         if (index_of<VEC>(t, gt, u, e) < d) {
-          se += g[u][e];
-          sn = fmaf(g[u][e], n[u][e], sn);
+          sums[0] += g[u][e];
+          sums[1] = fmaf(g[u][e], n[u][e], sums[1]);
         }
       }
     }
-    if (row + stride < a.tokens) load(row + stride);
-    if (a.dx) {
-      row_sums<WAVE>(se, sn, part);
-      const float me = a.center ? se / (float)d : 0.f, mn = sn / (float)d;
+    load(row + stride, q);
+    if (!a.dx) return;
+    row_sums<WAVE>(sums, part);
+    const float me = a.center ? sums[0] / (float)d : 0.f, mn = sums[1] / (float)d;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[u][e] = (g[u][e] - me - n[u][e] * mn) * rr;
-        store8<VEC>(a.dx, row * (size_t)d, a.dtype, t, gt, u, d, g[u]);
-      }
+      for (int e = 0; e < 8; ++e) g[u][e] = (g[u][e] - me - n[u][e] * mn) * r;
+      store8<VEC>(a.dx, row * (size_t)d, a.dtype, t, gt, u, d, g[u]);
     }
-  }
+  };
+  Row q;
+  load(first, q);
+  for (size_t row = first; row < a.tokens; row += stride) take(row, q);
   if (!a.part) return;
   // [block][dw, db][d]
   float* out = a.part + (size_t)blockIdx.x * 2 * d;
@@ -185,8 +191,18 @@ __global__ __launch_bounds__(1024) void k_norm_columns(const float* __restrict__
   if (!out) return;
   const int c = blockIdx.x * 64 + lane;
   float v = 0.f;
-  if (c < d)
-    for (int b = wv; b < blocks; b += 16) v += part[((size_t)b * 2 + k) * d + c];
+  if (c < d) {
+    const float* p = part + (size_t)k * d + c;
+    int b = wv;
+    for (; b + 7 * 16 < blocks; b += 8 * 16) {  // eight requests at once
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = p[(size_t)(b + 16 * e) * 2 * d];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v += f[e];
+    }
+    for (; b < blocks; b += 16) v += p[(size_t)b * 2 * d];
+  }
   s[wv][lane] = v;
   __syncthreads();
   if (wv == 0 && c < d) {
@@ -217,7 +233,8 @@ bool whole(const void* p, size_t ld, int dt) {
 }
 
 // Blocks of the backward pass: two a compute unit, so that the blocks' sums, 8 d
-// bytes each, stay few; no more than rows.
+// bytes each, stay few (4096 x 5120 bf16, both kernels: 45 us with 512 blocks, 49 with
+// 768, 54 with 1024); no more than rows.
 unsigned grad_blocks(size_t tokens, int d) {
   const size_t rows = shape_of(d).wave ? 4 : 1;
   return (unsigned)std::min<size_t>((tokens + rows - 1) / rows, 512);
