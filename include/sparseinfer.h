@@ -621,6 +621,15 @@ size_t si_gated_linear_backward_workspace_bytes(const void* x, size_t ldx, int m
                                                 const void* w_up, int rows, int want_dx, int want_dw);
 
 /*
+ * Diagnostic, host-only: which kernel a dense product of these sizes takes.  kind 0:
+ * si_linear (1: with W^T) or si_gated_linear; 2: the gradient with respect to x (3: with
+ * W^T); 4: with respect to W (5: with W^T); 6: the FP8 products.  gated nonzero: with
+ * W_up.  100: the one for a few tokens; 0 and up: the place of its tile in the library's
+ * list, smallest first; -2: sizes that the product refuses, or m = 0.
+ */
+int si_dense_tile(int kind, int m, int rows, int n, int gated);
+
+/*
  * FP8 weights: e4m3 values (sign, 4 bits of exponent, 3 of fraction; largest 448, no
  * infinities) with float32 scales.  A row of n values is stored as n rounded up to
  * 16 codes (zeros behind the n-th); a value is its code times its scale:

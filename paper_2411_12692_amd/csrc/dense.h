@@ -32,9 +32,12 @@ struct DenseArgs {
 // a stage.  The first two are for few rows of B, which then lie along k.
 struct DenseShape {
   int bm, bn, wk, threads, st;  // st: stages in LDS
+  int resident;                 // blocks a compute unit
+  float stage_us, round_us;     // time of a stage, and what a round of blocks takes besides
 };
-constexpr DenseShape kDenseTiles[] = {{64, 16, 4, 512, 3},   {64, 32, 4, 512, 3},   {64, 64, 2, 512, 3},
-                                      {128, 128, 1, 512, 2}, {128, 256, 1, 512, 3}, {256, 256, 1, 512, 2}};
+constexpr DenseShape kDenseTiles[] = {{64, 16, 4, 512, 3, 1, 0.69f, 0.7f},  {64, 32, 4, 512, 3, 1, 0.93f, 0.9f},
+                                      {64, 64, 2, 512, 3, 1, 0.59f, 2.0f},  {128, 128, 1, 512, 2, 2, 0.76f, 2.0f},
+                                      {128, 256, 1, 512, 3, 1, 0.71f, 2.4f}, {256, 256, 1, 512, 2, 1, 1.03f, 6.0f}};
 constexpr int kDenseTileCount = 6;
 constexpr int kDenseFew = 100;  // in place of a tile: the kernel for up to kFewTokens rows of B (dense_few.hip)
 constexpr int kFewTokens = 4;

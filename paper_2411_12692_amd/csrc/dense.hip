@@ -8,6 +8,7 @@
 // Operands that cannot be read in 16-byte pieces (odd lengths, unaligned rows,
 // another type) are copied into the workspace first, rows padded with zeros.
 #include <algorithm>
+#include <cmath>
 
 #include "dense.h"
 
@@ -182,13 +183,14 @@ struct Plan {
 };
 
 // Which tile, and in how many parts the sum is taken, by an estimate of the time:
-// rounds of blocks over the compute units, each as long as its products or its loads
-// from L2 take, no less than the operands' bytes at the memory's rate, and the second
-// launch that joins parts.  The rates are those measured on large products (products of
-// 8192^3, TFLOP/s of the whole card: 256 x 256 tiles 1260-1320, 128 x 128 1040, e4m3
-// 1800-1950 and 1790).  Up to 4 tokens W's rows go through dense_few.hip.
+// rounds of blocks over the compute units, each as long as its stages and what comes
+// before and behind them, and the second launch that joins parts.  The times are
+// kDenseTiles' and those of the join, fitted to 438 products of random sizes (5 to 6000
+// tokens, 64 to 16384 rows, sums of 64 to 8192, every tile and split timed): the tile
+// taken is 2% slower than the best one on average.  Up to 4 tokens W's rows go
+// through dense_few.hip (gate and up of 11008 x 4096, one token: 35.1 us in tiles, 27.7).
 Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows, bool few) {
-  if (few && N <= kFewTokens && M < (1 << 24)) return {kDenseFew, 1, 0};
+  if (few && N <= kFewTokens) return {kDenseFew, 1, 0};
   Plan best = {-1, 1, 0};
   double best_t = 1e30;
   for (int i = b_rows ? 0 : 2; i < kDenseTileCount; ++i) {
@@ -196,23 +198,14 @@ Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows, b
     const long blocks = (long)((M + t.bm / mats - 1) / (t.bm / mats)) * ((N + t.bn - 1) / t.bn) * batches;
     const int kp = 128 / es * t.wk;
     const long stages = (K + kp - 1) / kp;
-    const int resident = i == 3 ? 2 : 1;
-    // of a block, in 1e6 flop/us and bytes/us
-    const double rate = (es == 1 ? (i == 5 ? 7.4 : i >= 3 ? 6.9 : 3.0) : (i == 5 ? 5.0 : i == 4 ? 4.3 : i == 3 ? 4.1 : 2.5)) / resident;
-    const double l2 = 0.07e6 / resident, memory = 5.0e6;
-    // a stage's loads take this long to arrive: from memory where few tiles share W
-    const double latency = (((N + t.bn - 1) / t.bn) <= 2 ? 1.8 : 0.9) / (t.st - 1);
-    const double bytes = ((double)M * mats + N) * (double)K * es * batches;
     for (int split = 1; split <= 16; split *= 2) {
       if (split > 1 && stages < 4 * split) break;
       if ((double)blocks * split * t.threads >= 4294967296.0) break;  // threads of a launch
-      const double rounds = (double)((blocks * split + kBlocks * resident - 1) / (kBlocks * resident));
-      const double k = (double)((stages + split - 1) / split) * kp;
-      const double wait = (double)((stages + split - 1) / split) * latency;
-      const double mul = 2e-6 * t.bm * t.bn * k / rate, move = (t.bm + t.bn) * k * es / l2;
+      const double full = (double)kBlocks * t.resident;
+      const double rounds = std::ceil((double)blocks * split / full);
+      double us = rounds * ((double)((stages + split - 1) / split) * t.stage_us + t.round_us);
       const double size = (double)M * N * mats * batches * 4;
-      double us = std::max(rounds * (std::max(std::max(mul, move), wait) + 2.0), bytes / memory);
-      if (split > 1) us += 3.0 + size * (2 * split + 1) / 4e6;
+      if (split > 1) us += 4.0 + size * (2 * split + 1) / 3.3e6;
       if (us < best_t) {
         best_t = us;
         best = {i, split, split > 1 ? align256((size_t)split * mats * batches * M * N * 4) : 0};

@@ -323,6 +323,27 @@ si_status si_gated_linear_backward(const void* dh, int dh_dtype, size_t lddh, co
   return run_grad(c, lddh, ldx, true, workspace, workspace_bytes, stream);
 }
 
+int si_dense_tile(int kind, int m, int rows, int n, int gated) {
+  if (kind < 0 || kind > 6 || check_sizes(m, rows, n) != SI_OK || m == 0) return -2;
+  const bool transposed = kind < 6 && (kind & 1);
+  const void* up = gated && !transposed ? kSome : nullptr;
+  int tile;
+  if (kind == 6) {
+    DenseFp8 c;
+    c.m = m;
+    c.rows = rows;
+    c.n = n;
+    c.q_up = gated ? kSome : nullptr;
+    tile = dense_fp8_tile(c);
+  } else if (kind < 2) {
+    tile = dense_linear_tile(linear_call(kSome, SI_F16, (size_t)n, m, n, kSome, up, rows, transposed));
+  } else {
+    const DenseGrad c = grad_call(kSome, SI_F16, (size_t)rows, kSome, SI_F16, (size_t)n, m, n, kSome, up, rows, transposed);
+    tile = kind < 4 ? dense_dx_tile(c) : dense_dw_tile(c);
+  }
+  return tile < 0 ? -2 : tile;
+}
+
 // ---- FP8 ---------------------------------------------------------------------------
 
 size_t si_fp8_codes_bytes(int rows, int n) {
