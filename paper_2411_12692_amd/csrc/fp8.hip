@@ -123,6 +123,7 @@ __global__ __launch_bounds__(256) void k_dequantize_fp8(const uint8_t* __restric
   if (i >= rows * (size_t)pieces) return;
   const size_t r = i / pieces;
   const int c = (int)(i - r * pieces) * 8;
+  if (c >= n) return;  // a row's codes behind its values
   const u32x2 v = *reinterpret_cast<const u32x2*>(q + r * np + c);
   const float s = scale[r / per * fp8_blocks(n) + c / 128];
   float f[8];
