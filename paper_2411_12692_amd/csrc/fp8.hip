@@ -1,7 +1,9 @@
 // Rows and blocks of 8-bit floating point values (e4m3: 4 bits of exponent, 3 of
 // fraction, largest value 448, no infinities) with float32 scales:
-//     scale = max |v| / 448 over a block,  code = the nearest e4m3 of v / scale
-// with correctly rounded float32 quotients, ties to the even code.  Tokens have a
+//     scale = max |v| * (1 / 448) over a block,  code = the nearest e4m3 of v / scale
+// with 1 / 448, the product and the quotient rounded to float32 each, ties to the even
+// code (the product, as PyTorch divides a tensor by a number on the GPU: a scale that is
+// one step off puts values at the border between two codes on the other side).  Tokens have a
 // scale for each 128 values of a row, weights one for each 128 x 128 block.  Rows
 // are stored as n rounded up to 16 codes (zeros behind the n-th), so that a row's
 // codes are whole 16-byte pieces.  A block of zeros has scale 0 and codes 0; one
@@ -46,7 +48,7 @@ __device__ inline uint32_t top_bits(const float (&f)[8], uint32_t top) {
 }
 
 __device__ inline float scale_of(uint32_t top) {
-  return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __fdiv_rn(__uint_as_float(top), 448.f);
+  return top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : __uint_as_float(top) * (1.f / 448.f);
 }
 
 __device__ inline u32x2 codes_of(const float (&f)[8], float scale) {

@@ -95,7 +95,7 @@ def quantize(v, rows_per_scale):
     p = torch.nn.functional.pad(v, (0, -n % 128, 0, -rows % rows_per_scale))
     b = p.view(p.shape[0] // rows_per_scale, rows_per_scale, p.shape[1] // 128, 128)
     top = torch.where(b.isnan(), torch.inf, b.abs()).amax(dim=(1, 3), keepdim=True)
-    scale = torch.where(torch.isinf(top), torch.nan, top / 448.0)
+    scale = torch.where(torch.isinf(top), torch.nan, top * (torch.ones(()) / 448))
     ok = scale > 0
     q = torch.where(ok, e4m3_code(torch.where(ok, b / scale, torch.zeros(()))), 0)
     codes = q.reshape(p.shape)[:rows, : (n + 15) // 16 * 16]
