@@ -568,9 +568,8 @@ si_status si_norm_residual(const void* h, int h_dtype, size_t ldh, const void* b
  *   w   : [rows][n], at any address that fits an element; with w_transposed nonzero
  *         W^T, [n][rows] (what si_transpose_down makes of W_down: y = h W_down^T).
  *   y, h: [m][rows] of type y_dtype / h_dtype, written.
- *   g, u: both or neither: the two sums themselves, [m][rows] of type dtype, kept for
- *         the backward pass.  A positive g that the type rounds to 0 is kept as the
- *         type's smallest value, so that its sign survives.  With w_up only.
+ *   g, u: both or neither: the two sums themselves, [m][rows] in float32, for the
+ *         backward pass.  With w_up only.
  *   m 0 to 2^24 (0 does nothing), rows and n 1 to 2^20, m times rows or n below 2^35
  *         and few enough blocks for one launch (else SI_ERR_SHAPE).
  *   workspace: the ..._workspace_bytes() of the call: scratch for split sums and for
@@ -583,7 +582,7 @@ si_status si_norm_residual(const void* h, int h_dtype, size_t ldh, const void* b
 si_status si_linear(const void* x, int dtype, size_t ldx, int m, int n, const void* w, int rows, int w_transposed,
                     void* y, int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
 si_status si_gated_linear(const void* x, int dtype, size_t ldx, int m, int n, const void* w_gate, const void* w_up,
-                          int rows, void* h, int h_dtype, void* g, void* u, void* workspace, size_t workspace_bytes,
+                          int rows, void* h, int h_dtype, float* g, float* u, void* workspace, size_t workspace_bytes,
                           void* stream);
 
 /*
@@ -592,24 +591,33 @@ si_status si_gated_linear(const void* x, int dtype, size_t ldx, int m, int n, co
  *   si_gated_linear_backward : dg = dh u where g > 0, else 0;  du = dh max(g, 0);
  *                              dx = dg W_gate + du W_up,  dw_gate = dg^T x,
  *                              dw_up = du^T x
+ *   si_mlp_backward          : of the whole MLP, y = h W_down^T with W_down [d][k]: dh =
+ *                              dy W_down (float32, not stored), dw_down = dy^T h, and the
+ *                              gradients of si_gated_linear for n = d and rows = k
  *   dy  : m rows of type dtype or float32, lddy elements from row to row; dh of any
  *         type.  dy (as an operand of the products), dg and du are rounded to dtype.
- *   g, u: as si_gated_linear kept them.  w_up NULL: u NULL, and g is its output h,
- *         [m][rows] of type g_dtype.
- *   dx, dw, dw_gate, dw_up: [m][n] and the weights' shapes, of type dtype, written;
- *         each may be NULL.  With m = 0 the weights' gradients are zeros.
- *   workspace: ..._workspace_bytes() of the call; want_dx and want_dw say which of the
- *         gradients are not NULL.
+ *   g, u: as si_gated_linear kept them (g_dtype SI_F32).  w_up NULL: u NULL, and g is its
+ *         output h, [m][rows] of type g_dtype (si_mlp_backward: g NULL).
+ *   h   : [m][k] of type dtype, si_gated_linear's output.
+ *   g, u and h on 16 bytes.
+ *   dx, dw, dw_gate, dw_up, dw_down: [m][n] and the weights' shapes, of type dtype,
+ *         written; each may be NULL.  With m = 0 the weights' gradients are zeros.
+ *   workspace: ..._workspace_bytes() of the call; want_dx, want_dw (of either of w_gate
+ *         and w_up) and want_dw_down say which of the gradients are not NULL.
  */
 si_status si_linear_backward(const void* dy, int dy_dtype, size_t lddy, const void* x, int dtype, size_t ldx, int m, int n,
                              const void* w, int rows, int w_transposed, void* dx, void* dw, void* workspace,
                              size_t workspace_bytes, void* stream);
-si_status si_gated_linear_backward(const void* dh, int dh_dtype, size_t lddh, const void* g, int g_dtype, const void* u,
+si_status si_gated_linear_backward(const void* dh, int dh_dtype, size_t lddh, const void* g, int g_dtype, const float* u,
                                    const void* x, int dtype, size_t ldx, int m, int n, const void* w_gate,
                                    const void* w_up, int rows, void* dx, void* dw_gate, void* dw_up, void* workspace,
                                    size_t workspace_bytes, void* stream);
+si_status si_mlp_backward(const void* dy, int dy_dtype, size_t lddy, const void* x, int dtype, size_t ldx, int m, int d,
+                          const void* w_gate, const void* w_up, const void* w_down, int k, const void* h, const float* g,
+                          const float* u, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
-/* Bytes of workspace of the four calls above (0 for unsupported shapes and where none
+/* Bytes of workspace of the five calls above (0 for unsupported shapes and where none
  * is needed).  Of the operands only alignment, and of w_up the presence, counts.
  * Host-only. */
 size_t si_linear_workspace_bytes(const void* x, size_t ldx, int m, int n, const void* w, int rows, int w_transposed);
@@ -619,6 +627,9 @@ size_t si_linear_backward_workspace_bytes(const void* dy, int dy_dtype, size_t l
                                           int n, const void* w, int rows, int w_transposed, int want_dx, int want_dw);
 size_t si_gated_linear_backward_workspace_bytes(const void* x, size_t ldx, int m, int n, const void* w_gate,
                                                 const void* w_up, int rows, int want_dx, int want_dw);
+size_t si_mlp_backward_workspace_bytes(const void* dy, int dy_dtype, size_t lddy, const void* x, size_t ldx, int m, int d,
+                                       const void* w_gate, const void* w_up, const void* w_down, int k, int want_dx,
+                                       int want_dw, int want_dw_down);
 
 /*
  * Diagnostic, host-only: which kernel a dense product of these sizes takes.  kind 0:
@@ -645,9 +656,9 @@ size_t si_fp8_block_scales_bytes(int rows, int n);
 
 /*
  * Rows (tokens) and blocks (weights, once at load) to FP8.  With m the largest |v| of
- * a block: scale = m / 448, the code of v is the e4m3 value nearest to v / scale, ties
- * to the even code; both quotients are correctly rounded float32 ones.  A scale of 0
- * (m = 0, or so small that the quotient is 0) has codes 0; a block with an infinity or
+ * a block: scale = m * (1 / 448), the code of v is the e4m3 value nearest to v / scale,
+ * ties to the even code; 1 / 448, the product and the quotient are each rounded to
+ * float32.  A scale of 0 (m = 0, or so small that the product is 0) has codes 0; a block with an infinity or
  * a NaN the scale NaN and codes 0, so that it reads back as NaN.
  *   x (w) : rows of n values of type x_dtype, ldx elements from row to row (n to 2^32
  *           where rows > 1), at any address that fits an element.

@@ -945,12 +945,12 @@ def linear(x: torch.Tensor, w: torch.Tensor, transposed: bool = False, out_dtype
 
 
 def _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, keep):
-    """``(h, g, u)``; g and u (with ``keep`` and ``w_up``) in ``x``'s type."""
+    """``(h, g, u)``; g and u (with ``keep`` and ``w_up``) the two sums, float32."""
     index = _same_device(x2, w_gate, w_up)
     h = x2.new_empty((m, rows), dtype=out_dtype)
     g = u = None
     if keep and w_up is not None:
-        g, u = x2.new_empty((m, rows)), x2.new_empty((m, rows))
+        g, u = x2.new_empty((m, rows), dtype=torch.float32), x2.new_empty((m, rows), dtype=torch.float32)
     nbytes = _dense_workspace("si_gated_linear_workspace_bytes", _like(x2), ld, m, n, _like(w_gate), _like(w_up), rows)
     ws = _scratch(x2, nbytes)
     _call_on(index, "si_gated_linear", x2.data_ptr(), _DTYPE[x2.dtype], ld, m, n, w_gate.data_ptr(), _vp(w_up), rows,
@@ -989,8 +989,8 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor = Non
     """``ReLU(x W_gate^T) * (x W_up^T)`` over every row, Eq. (1) steps 1-3, in one
     launch (``si_gated_linear``); ``w_up=None``: ``ReLU(x W_fc1^T)``.  ``x [..., n]``
     and the weights ``[rows][n]`` in fp16 or bf16; returns ``[..., rows]`` in
-    ``out_dtype`` (``x``'s type).  Differentiable with respect to all; the backward
-    pass keeps both sums in ``x``'s type."""
+    ``out_dtype`` (``x``'s type).  Differentiable with respect to all; both sums
+    are kept for the backward pass in float32."""
     x2, m, n, ld = _flat(x, "x", _HALF)
     shape = _weight(w_gate, "w_gate", x)
     rows = shape[0]
@@ -1006,12 +1006,56 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor = Non
     return h if x.dim() == 2 else h.view(*x.shape[:-1], rows)
 
 
+class _MLP(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x2, w_gate, w_up, w_down, m, n, ld, rows, out_dtype):
+        h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, x2.dtype, True)
+        ctx.save_for_backward(x2, w_gate, w_up, w_down, h, g, u)
+        ctx.args = (m, n, ld, rows)
+        return _linear_forward(h, m, rows, rows, w_down, n, False, out_dtype)
+
+    @staticmethod
+    @_first_order
+    def backward(ctx, dy):
+        x2, w_gate, w_up, w_down, h, g, u = ctx.saved_tensors
+        m, n, ld, rows = ctx.args
+        if _DTYPE[dy.dtype] not in (_DTYPE[x2.dtype], _lib.SI_F32):
+            dy = dy.float()
+        dy, ldd = _grad_rows(dy)
+        want_x, want_g, want_u, want_d = ctx.needs_input_grad[:4]
+        dx = x2.new_empty((m, n)) if want_x else None
+        dg = torch.empty_like(w_gate) if want_g else None
+        du = torch.empty_like(w_up) if want_u else None
+        dd = torch.empty_like(w_down) if want_d else None
+        nbytes = _dense_workspace("si_mlp_backward_workspace_bytes", _like(dy), _DTYPE[dy.dtype], ldd, _like(x2), ld, m, n,
+                                  _like(w_gate), _like(w_up), _like(w_down), rows, want_x, want_g or want_u, want_d)
+        ws = _scratch(x2, nbytes)
+        _call_on(_same_device(x2, dy, w_gate, w_up, w_down), "si_mlp_backward", dy.data_ptr(), _DTYPE[dy.dtype], ldd,
+                 x2.data_ptr(), _DTYPE[x2.dtype], ld, m, n, w_gate.data_ptr(), _vp(w_up), w_down.data_ptr(), rows,
+                 h.data_ptr(), _vp(g), _vp(u), _vp(dx), _vp(dg), _vp(du), _vp(dd), _vp(ws), nbytes)
+        return dx, dg, du, dd, None, None, None, None, None
+
+
 def mlp(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, out_dtype=None) -> torch.Tensor:
     """The dense MLP of Eq. (1), ``(ReLU(x W_gate^T) * (x W_up^T)) W_down^T``, with
     ``W_gate, W_up [k][d]`` and ``W_down [d][k]`` (``w_up=None``: the non-gated one):
-    ``gated_linear`` and ``linear``, differentiable with respect to all.  The hidden
-    values are rounded to ``x``'s type."""
-    return linear(gated_linear(x, w_gate, w_up), w_down, out_dtype=out_dtype)
+    ``gated_linear`` and ``linear``, differentiable with respect to all; the backward
+    pass is one call (``si_mlp_backward``).  The hidden values are rounded to ``x``'s
+    type; where gradients are asked for they and both sums (float32) are kept."""
+    x2, m, n, ld = _flat(x, "x", _HALF)
+    rows = _weight(w_gate, "w_gate", x)[0]
+    if w_gate.shape[1] != n:
+        raise ValueError(f"w_gate {tuple(w_gate.shape)} does not take rows of {n} values")
+    if w_up is not None:
+        _weight(w_up, "w_up", x, (rows, n))
+    _weight(w_down, "w_down", x, (n, rows))
+    out_dtype = _out_type(out_dtype, x)
+    if _wants_grad(x, w_gate, w_up, w_down):
+        y = _MLP.apply(x2, w_gate, w_up, w_down, m, n, ld, rows, out_dtype)
+    else:
+        h = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, x2.dtype, False)[0]
+        y = _linear_forward(h, m, rows, rows, w_down, n, False, out_dtype)
+    return y if x.dim() == 2 else y.view(x.shape)
 
 
 # ---- norms with their gradients -------------------------------------------------

@@ -90,6 +90,8 @@ SIGNATURES = {
     "si_gated_linear_backward": (_i, [_p, _i, _sz, _p, _i, _p, _p, _i, _sz, _i, _i, _p, _p, _i, _p, _p, _p, _p, _sz,
                                       _p]),
     "si_gated_linear_backward_workspace_bytes": (_sz, [_p, _sz, _i, _i, _p, _p, _i, _i, _i]),
+    "si_mlp_backward": (_i, [_p, _i, _sz, _p, _i, _sz, _i, _i, _p, _p, _p, _i, _p, _p, _p, _p, _p, _p, _p, _p, _sz, _p]),
+    "si_mlp_backward_workspace_bytes": (_sz, [_p, _i, _sz, _p, _sz, _i, _i, _p, _p, _p, _i, _i, _i, _i]),
     "si_dense_tile": (_i, [_i, _i, _i, _i, _i]),
     "si_fp8_codes_bytes": (_sz, [_i, _i]),
     "si_fp8_scales_bytes": (_sz, [_i, _i]),

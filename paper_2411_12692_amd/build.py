@@ -23,8 +23,8 @@ TRACE_LIB = os.path.join(PKG, "libsparseinfer_trace.so")
 TRACED = "owned.hip"  # the source compiled with -DSI_TRACE in the trace variant
 SOURCES = ["api.hip", "pack.hip", "predict.hip", "mlp.hip", "owned.hip", "diag.hip",
            "mx_quant.hip", "mx_linear.hip", "mx_sparse.hip", "mx_api.hip", "norm.hip",
-           "dense.hip", "dense_rr.hip", "dense_gated.hip", "dense_cr.hip", "dense_cc.hip", "dense_fp8.hip", "dense_few.hip",
-           "fp8.hip", "norm_train.hip", "dense_api.hip"]
+           "dense.hip", "dense_rr.hip", "dense_gated.hip", "dense_cr.hip", "dense_dh.hip", "dense_cc.hip", "dense_fp8.hip",
+           "dense_few.hip", "fp8.hip", "norm_train.hip", "dense_api.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc" if os.path.exists("/opt/rocm/bin/hipcc") else "hipcc")

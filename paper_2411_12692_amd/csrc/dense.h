@@ -17,9 +17,15 @@ struct DenseArgs {
   void* c[2];        // [N][M] of c_dtype, by batch
   int c_dtype;
   int relu;          // one matrix: max(C, 0)
-  void* g;           // gated: the two sums themselves, of save_dtype, or NULL
-  void* u;
-  int save_dtype;
+  float* g;          // gated: the two sums themselves, or NULL
+  float* u;
+  // The product is dh, the gradient of h = relu(gate) * up (both float32) or, up NULL, of
+  // h = relu(..) (gate is h, of c_dtype): c[0] is written with dg and du with du, rows of
+  // ldc values (a multiple of 8), zeros behind the M-th.
+  const void* gate;
+  const float* up;
+  void* du;
+  int ldc;
   float* part;       // partial sums [split][parts_of][N][M], or NULL
   int split, parts_of;
   const float* sa[2];  // e4m3: scales of A's blocks [M / 128][blocks] ...
@@ -46,9 +52,66 @@ constexpr int kFewTokens = 4;
 hipError_t dense_rr(int type, const DenseArgs& a, int tile, hipStream_t s);                 // x W^T
 hipError_t dense_gated(int type, const DenseArgs& a, int tile, hipStream_t s);              // x W_gate^T, x W_up^T
 hipError_t dense_cr(int type, const DenseArgs& a, int tile, hipStream_t s);                 // dy W
+hipError_t dense_dh(int type, const DenseArgs& a, int tile, hipStream_t s);                 // the same, to dg and du
 hipError_t dense_cc(int type, const DenseArgs& a, int tile, int batches, hipStream_t s);    // dy^T x
 hipError_t dense_fp8(const DenseArgs& a, int mats, int tile, hipStream_t s);
 hipError_t dense_few(int type, int mats, const DenseArgs& a, hipStream_t s);                // x W^T, a few tokens; type 2: e4m3
+
+// dg and du of one value: the gradient is 0 where the gate is <= 0; a NaN gate lets it
+// pass.
+__device__ inline void gated_grad(float dh, float gate, float up, float& dg, float& du) {
+  dg = gate <= 0.f ? 0.f : dh * up;
+  du = dh * (gate <= 0.f ? 0.f : gate);
+}
+
+// What dg and du of four values, row n from m on (a multiple of 4), ask for.  UP: both
+// sums are kept; else gate is h.  WHOLE: M is a multiple of 4.  Zeros behind the M-th.
+struct GatedPiece {
+  f32x4 g, u;
+};
+template <bool UP, bool WHOLE>
+__device__ inline GatedPiece gated_piece(const DenseArgs& a, int n, int m) {
+  const size_t at = (size_t)n * a.M + m;
+  GatedPiece p = {{0.f, 0.f, 0.f, 0.f}, {1.f, 1.f, 1.f, 1.f}};
+  if constexpr (WHOLE) {
+    if (m >= a.M) return p;
+    if constexpr (UP) {
+      p.g = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.gate) + at);
+      p.u = *reinterpret_cast<const f32x4*>(a.up + at);
+    } else {
+      const u32x2 h = *reinterpret_cast<const u32x2*>(static_cast<const uint16_t*>(a.gate) + at);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t v = h[e >> 1] >> (16 * (e & 1));
+        p.g[e] = a.c_dtype == kBF16 ? bf16_lo(v) : (float)__builtin_bit_cast(_Float16, (uint16_t)v);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (m + e < a.M) {
+        p.g[e] = load_one(a.gate, at + e, UP ? kF32 : a.c_dtype);
+        if constexpr (UP) p.u[e] = a.up[at + e];
+      }
+  }
+  return p;
+}
+
+// dg and du in their place, zeros behind the M-th.
+template <bool UP>
+__device__ inline void put_gated_grad(const DenseArgs& a, int n, int m, f32x4 dh, const GatedPiece& p) {
+  const size_t at = (size_t)n * a.ldc + m;
+  float x[4], y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    gated_grad(dh[e], p.g[e], p.u[e], x[e], y[e]);
+    if (m + e >= a.M) x[e] = y[e] = 0.f;
+  }
+  auto pack = [&](float v, float w) { return a.c_dtype == kBF16 ? pack_bf2(v, w) : pack_f2(v, w); };
+  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.c[0]) + at) = u32x2{pack(x[0], x[1]), pack(x[2], x[3])};
+  if constexpr (UP)
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.du) + at) = u32x2{pack(y[0], y[1]), pack(y[2], y[3])};
+}
 
 // ---- calls (dense.hip), arguments validated by the caller ----------------------
 
@@ -67,8 +130,8 @@ struct DenseLinear {
   int m = 0, rows = 0, n = 0;
   void* y = nullptr;
   int y_dtype = 0;
-  void* g = nullptr;
-  void* u = nullptr;
+  float* g = nullptr;
+  float* u = nullptr;
   void* ws = nullptr;
 };
 size_t dense_linear_workspace(const DenseLinear& c);
@@ -76,20 +139,25 @@ int dense_linear_tile(const DenseLinear& c);  // place of its tile; -1: more tha
 hipError_t launch_dense_linear(const DenseLinear& c, hipStream_t s);
 
 // Gradients of DenseLinear.  gate NULL: of y = x W^T (dy); else of the ReLU'd or
-// gated product, whose gate values (one matrix: outputs) and up values were kept.
+// gated product, whose sums (one matrix: outputs) were kept.  down given: of the whole
+// MLP, whose hidden values h were kept; dy is then that of y = h W_down^T, [m][n].
 struct DenseGrad {
   DenseMat dy, x, w, w_up;
   DenseMat gate, up;
+  DenseMat down, h;  // W_down [n][rows], h [m][rows]
   int type = 0;
   bool transposed = false;
   int m = 0, rows = 0, n = 0;
   void* dx = nullptr;
   void* dw = nullptr;
   void* dw_up = nullptr;
+  void* dw_down = nullptr;
   void* ws = nullptr;
 };
 size_t dense_grad_workspace(const DenseGrad& c);
 int dense_dx_tile(const DenseGrad& c);
+int dense_dh_tile(const DenseGrad& c);
+int dense_dw_down_tile(const DenseGrad& c);
 int dense_dw_tile(const DenseGrad& c);
 hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s);
 

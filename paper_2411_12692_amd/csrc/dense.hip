@@ -2,7 +2,8 @@
 // dense_tile.h:
 //   y  = x W^T          A = W (kRow), B = x (kRow); W_down^T [k][d]: A kCol
 //   g, u = x W_gate^T, x W_up^T in one launch, h = ReLU(g) * u in its epilogue
-//   dg = [g > 0] dh u,  du = dh ReLU(g)   (k_gated_grad)
+//   dg = [g > 0] dh u,  du = dh ReLU(g)   (k_gated_grad; of the whole MLP in the epilogue
+//                                          of dh = dy W_down)
 //   dx = dg W_gate + du W_up               one launch, its sum over both
 //   dW_gate = dg^T x,  dW_up = du^T x      one launch, a batch of two
 // Operands that cannot be read in 16-byte pieces (odd lengths, unaligned rows,
@@ -23,7 +24,7 @@ struct PadJob {
   u32x4* out;
 };
 struct PadJobs {
-  PadJob job[4];
+  PadJob job[6];
   int count, type;
 };
 
@@ -49,8 +50,7 @@ __global__ __launch_bounds__(256) void k_dense_pad(PadJobs jobs) {
 }
 
 // dg and du of `rows` values a token, in rows of rp (zeros behind), 8 values a
-// thread.  UP: g and u are the two sums; else g is h = ReLU(g).  The gradient is 0
-// where g <= 0; a NaN of g lets it pass.
+// thread.  UP: g and u are the two sums; else g is h = ReLU(g).
 template <bool UP>
 __global__ __launch_bounds__(256) void k_gated_grad(DenseMat dh, DenseMat gate, DenseMat up, size_t m, int rows, int rp,
                                                     int type, u32x4* __restrict__ dg, u32x4* __restrict__ du) {
@@ -60,8 +60,15 @@ __global__ __launch_bounds__(256) void k_gated_grad(DenseMat dh, DenseMat gate, 
   const int c = (int)(i - t * (rp / 8)) * 8;
   float d[8], g[8], u[8];
   auto load = [&](const DenseMat& a, float (&f)[8]) {
-    const bool half = a.dtype != kF32;
-    if (half && c + 8 <= rows) {
+    if (a.dtype == kF32 && c + 8 <= rows) {
+      const float* p = static_cast<const float*>(a.p) + t * a.ld + c;
+      const u32x4 lo = *reinterpret_cast<const u32x4_e4*>(p), hi = *reinterpret_cast<const u32x4_e4*>(p + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[e] = __uint_as_float(lo[e]);
+        f[4 + e] = __uint_as_float(hi[e]);
+      }
+    } else if (a.dtype != kF32 && c + 8 <= rows) {
       const u32x4 v = *reinterpret_cast<const u32x4_e2*>(static_cast<const uint16_t*>(a.p) + t * a.ld + c);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -83,8 +90,7 @@ __global__ __launch_bounds__(256) void k_gated_grad(DenseMat dh, DenseMat gate, 
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int k = 2 * e + j;
-      x[j] = g[k] <= 0.f ? 0.f : UP ? d[k] * u[k] : d[k];
-      y[j] = UP ? d[k] * (g[k] <= 0.f ? 0.f : g[k]) : 0.f;
+      gated_grad(d[k], g[k], UP ? u[k] : 1.f, x[j], y[j]);
       if (c + k >= rows) x[j] = y[j] = 0.f;
     }
     a[e] = type == kF16 ? pack_f2(x[0], x[1]) : pack_bf2(x[0], x[1]);
@@ -124,10 +130,8 @@ __global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, size_t size) {
     float y = v[0][e];
     if constexpr (MATS == 2) {
       if (a.g) {
-        uint16_t h = (uint16_t)(a.save_dtype == kBF16 ? pack_bf2(y, 0.f) : pack_f2(y, 0.f));
-        if (y > 0.f && h == 0) h = 1;  // as in the tiles
-        static_cast<uint16_t*>(a.g)[i + e] = h;
-        store_one(a.u, i + e, a.save_dtype, v[MATS - 1][e]);
+        a.g[i + e] = y;
+        a.u[i + e] = v[MATS - 1][e];
       }
       y = (y > 0.f || y != y ? y : 0.f) * v[MATS - 1][e];
     } else if (a.relu) {
@@ -135,6 +139,22 @@ __global__ __launch_bounds__(256) void k_dense_join(DenseArgs a, size_t size) {
     }
     store_one(a.c[batch], i + e, a.c_dtype, y);
   }
+}
+
+// The same for dh: dg and du, 4 values a thread of rows of ldc.
+template <bool UP>
+__global__ __launch_bounds__(256) void k_dense_join_grad(DenseArgs a) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int pieces = a.ldc / 4;
+  if (i >= (size_t)a.N * pieces) return;
+  const int n = (int)(i / pieces), m = (int)(i - (size_t)n * pieces) * 4;
+  const size_t size = (size_t)a.M * a.N, in = (size_t)n * a.M + m;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  for (int p = 0; p < a.split; ++p)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (m + e < a.M) v[e] += a.part[(size_t)p * size + in + e];
+  put_gated_grad<UP>(a, n, m, v, gated_piece<UP, false>(a, n, m));
 }
 
 namespace {
@@ -232,6 +252,9 @@ Plan dw_plan(const DenseGrad& c) {
   return c.transposed ? plan_of(c.rows, c.n, c.m, 1, 1, 2, false, false)
                       : plan_of(c.n, c.rows, c.m, 1, c.w_up.p ? 2 : 1, 2, false, false);
 }
+// of the whole MLP: dh = dy W_down, dW_down = dy^T h
+Plan dh_plan(const DenseGrad& c) { return plan_of(c.rows, c.m, c.n, 1, 1, 2, true, false); }
+Plan dw_down_plan(const DenseGrad& c) { return plan_of(c.rows, c.n, c.m, 1, 1, 2, false, false); }
 Plan fp8_plan(const DenseFp8& c) { return plan_of(c.rows, c.m, c.n, c.q_up ? 2 : 1, 1, 1, true, true); }
 
 size_t weight_copies(const DenseMat& w, const DenseMat& w_up, bool transposed, int type, int rows, int n) {
@@ -283,7 +306,6 @@ hipError_t launch_dense_linear(const DenseLinear& c, hipStream_t s) {
   a.relu = c.relu;
   a.g = c.g;
   a.u = c.u;
-  a.save_dtype = c.type;
   set_plan(a, p, mats, ws);
   const int type = c.type == kBF16 ? 1 : 0;
   if (p.tile == kDenseFew) return dense_few(type, mats, a, s);
@@ -293,14 +315,28 @@ hipError_t launch_dense_linear(const DenseLinear& c, hipStream_t s) {
 }
 
 size_t dense_grad_workspace(const DenseGrad& c) {
-  size_t b = c.gate.p ? align256((size_t)c.m * pad8(c.rows) * 2) * (c.up.p ? 2 : 1) : copy_bytes(c.dy, c.type, c.m, c.rows);
-  if (c.dw || c.dw_up) b += copy_bytes(c.x, c.type, c.m, c.n);
-  size_t part = 0;
+  const size_t one = align256((size_t)c.m * pad8(c.rows) * 2) * (c.up.p ? 2 : 1);
+  const bool want_w = c.dw || c.dw_up, through = c.dx || want_w;  // dg and du are asked for
+  size_t b = 0, part = 0;
+  if (c.down.p) {
+    b += copy_bytes(c.dy, c.type, c.m, c.n);
+    if (through) {
+      b += copy_bytes(c.down, c.type, c.n, c.rows) + one;
+      part = dh_plan(c).part_bytes;
+    }
+    if (c.dw_down) {
+      b += copy_bytes(c.h, c.type, c.m, c.rows);
+      part = std::max(part, dw_down_plan(c).part_bytes);
+    }
+  } else {
+    b += c.gate.p ? one : copy_bytes(c.dy, c.type, c.m, c.rows);
+  }
+  if (want_w) b += copy_bytes(c.x, c.type, c.m, c.n);
   if (c.dx) {
     b += weight_copies(c.w, c.w_up, c.transposed, c.type, c.rows, c.n);
-    part = dx_plan(c).part_bytes;
+    part = std::max(part, dx_plan(c).part_bytes);
   }
-  if (c.dw || c.dw_up) part = std::max(part, dw_plan(c).part_bytes);
+  if (want_w) part = std::max(part, dw_plan(c).part_bytes);
   return b + part;
 }
 
@@ -308,25 +344,30 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
   char* ws = static_cast<char*>(c.ws);
   const int type = c.type == kBF16 ? 1 : 0;
   DenseMat d = c.dy, du = {};
-  DenseMat x = c.x, w = c.w, up = c.w_up;
-  const bool want_w = c.dw || c.dw_up;
+  DenseMat x = c.x, w = c.w, up = c.w_up, down = c.down, h = c.h;
+  const bool want_w = c.dw || c.dw_up, through = c.dx || want_w;
   Copies copies(c.type, ws);
-  if (c.gate.p) {
-    const int rp = pad8(c.rows);
-    const size_t bytes = align256((size_t)c.m * rp * 2), all = (size_t)c.m * (rp / 8);
-    const unsigned grid = (unsigned)((all + 255) / 256);
-    u32x4* dg = reinterpret_cast<u32x4*>(ws);
+  const int rp = pad8(c.rows);
+  const size_t bytes = align256((size_t)c.m * rp * 2);
+  u32x4 *dg = nullptr, *dg_up = nullptr;
+  auto take = [&] {  // room for dg and du
+    dg = reinterpret_cast<u32x4*>(ws);
     ws += bytes;
-    d = DenseMat{dg, c.type, (size_t)rp};
     if (c.up.p) {
-      du = DenseMat{ws, c.type, (size_t)rp};
-      k_gated_grad<true><<<grid, 256, 0, s>>>(c.dy, c.gate, c.up, c.m, c.rows, rp, c.type, dg,
-                                              reinterpret_cast<u32x4*>(ws));
+      dg_up = reinterpret_cast<u32x4*>(ws);
       ws += bytes;
-    } else {
-      k_gated_grad<false><<<grid, 256, 0, s>>>(c.dy, c.gate, c.up, c.m, c.rows, rp, c.type, dg, nullptr);
     }
-    TRY(hipGetLastError());
+  };
+  DenseMat dy = c.dy;
+  if (c.down.p) {
+    copies.add(dy, c.m, c.n);
+    if (through) {
+      copies.add(down, c.n, c.rows);
+      take();
+    }
+    if (c.dw_down) copies.add(h, c.m, c.rows);
+  } else if (c.gate.p) {
+    take();
   } else {
     copies.add(d, c.m, c.rows);
   }
@@ -337,6 +378,63 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
     copies.add(up, wr, wc);
   }
   TRY(copies.launch(s));
+  if (c.down.p && through && c.m > 0) {
+    const Plan p = dh_plan(c);
+    DenseArgs a = {};
+    a.a[0] = down.p;
+    a.b[0] = dy.p;
+    a.lda = down.ld * 2;
+    a.ldb = dy.ld * 2;
+    a.M = c.rows;
+    a.N = c.m;
+    a.K = c.n;
+    a.segs = 1;
+    a.c[0] = dg;
+    a.c_dtype = c.type;
+    a.gate = c.gate.p;
+    a.up = static_cast<const float*>(c.up.p);
+    a.du = dg_up;
+    a.ldc = rp;
+    set_plan(a, p, 1, ws);
+    TRY(dense_dh(type, a, p.tile, s));
+    if (a.part) {
+      const size_t all = (size_t)a.N * (rp / 4);
+      const unsigned grid = (unsigned)((all + 255) / 256);
+      if (a.up)
+        k_dense_join_grad<true><<<grid, 256, 0, s>>>(a);
+      else
+        k_dense_join_grad<false><<<grid, 256, 0, s>>>(a);
+      TRY(hipGetLastError());
+    }
+  } else if (!c.down.p && c.gate.p && c.m > 0) {
+    const unsigned grid = (unsigned)(((size_t)c.m * (rp / 8) + 255) / 256);
+    if (c.up.p)
+      k_gated_grad<true><<<grid, 256, 0, s>>>(c.dy, c.gate, c.up, c.m, c.rows, rp, c.type, dg, dg_up);
+    else
+      k_gated_grad<false><<<grid, 256, 0, s>>>(c.dy, c.gate, c.up, c.m, c.rows, rp, c.type, dg, nullptr);
+    TRY(hipGetLastError());
+  }
+  if (c.gate.p) {
+    d = DenseMat{dg, c.type, (size_t)rp};
+    du = DenseMat{dg_up, c.type, (size_t)rp};
+  }
+  if (c.dw_down) {
+    const Plan p = dw_down_plan(c);
+    DenseArgs a = {};
+    a.a[0] = h.p;
+    a.b[0] = dy.p;
+    a.lda = h.ld * 2;
+    a.ldb = dy.ld * 2;
+    a.M = c.rows;
+    a.N = c.n;
+    a.K = c.m;
+    a.segs = 1;
+    a.c[0] = c.dw_down;
+    a.c_dtype = c.type;
+    set_plan(a, p, 1, ws);
+    TRY(dense_cc(type, a, p.tile, 1, s));
+    TRY(join(a, 1, 1, s));
+  }
   if (c.dx) {
     const Plan p = dx_plan(c);
     DenseArgs a = {};
@@ -398,6 +496,8 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
 int dense_linear_tile(const DenseLinear& c) { return linear_plan(c).tile; }
 int dense_dx_tile(const DenseGrad& c) { return dx_plan(c).tile; }
 int dense_dw_tile(const DenseGrad& c) { return dw_plan(c).tile; }
+int dense_dh_tile(const DenseGrad& c) { return dh_plan(c).tile; }
+int dense_dw_down_tile(const DenseGrad& c) { return dw_down_plan(c).tile; }
 int dense_fp8_tile(const DenseFp8& c) { return fp8_plan(c).tile; }
 
 size_t dense_fp8_workspace(const DenseFp8& c) { return fp8_plan(c).part_bytes; }

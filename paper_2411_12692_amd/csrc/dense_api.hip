@@ -85,7 +85,7 @@ si_status run_linear(DenseLinear c, size_t ldx, void* workspace, size_t workspac
   if (g && !w_up) return fail(SI_ERR_ARG, "g and u are those of a gated product");
   if (si_status s = fits(dense_linear_tile(c), c.m, c.rows, c.n)) return s;
   const size_t size = (size_t)c.m * c.rows, wb = (size_t)c.rows * c.n * 2;
-  const Rows out[3] = {flat(y, size * dtype_bytes(c.y_dtype)), flat(g, size * 2), flat(u, size * 2)};
+  const Rows out[3] = {flat(y, size * dtype_bytes(c.y_dtype)), flat(g, size * 4), flat(u, size * 4)};
   const Rows in[3] = {rows_of(c.x, c.m, c.n), flat(w, wb), flat(w_up, wb)};
   for (int i = 0; i < 3; ++i) {
     for (const Rows& r : in)
@@ -121,48 +121,78 @@ si_status run_grad(DenseGrad c, size_t lddy, size_t ldx, bool gated, void* works
   REQUIRE_DTYPE(dy_dtype);
   REQUIRE_DTYPE(g_dtype);
   if (si_status s = check_sizes(c.m, c.rows, c.n)) return s;
-  if (si_status s = check_ld("lddy", lddy, c.rows, c.m, kMaxLd)) return s;
+  const int dy_n = c.down.p ? c.n : c.rows;
+  if (si_status s = check_ld("lddy", lddy, dy_n, c.m, kMaxLd)) return s;
   if (si_status s = check_ld("ldx", ldx, c.n, c.m, kMaxLd)) return s;
-  const void *dy = c.dy.p, *x = c.x.p, *w = c.w.p, *w_up = c.w_up.p, *g = c.gate.p, *u = c.up.p, *dx = c.dx, *dw = c.dw,
-             *dw_up = c.dw_up;
-  if (!dx && !dw && !dw_up) return fail(SI_ERR_NULL, "none of the gradients is asked for");
-  if (c.m > 0) {
-    REQUIRE_PTR(dy);
-    if (gated) REQUIRE_PTR(g);
-    if (w_up) REQUIRE_PTR(u);
-    if (dw || dw_up) REQUIRE_PTR(x);
-  }
-  if (dx || c.m > 0) REQUIRE_PTR(w);
+  const void *dy = c.dy.p, *x = c.x.p, *w = c.w.p, *w_up = c.w_up.p, *w_down = c.down.p, *g = c.gate.p, *u = c.up.p,
+             *h = c.h.p, *dx = c.dx, *dw = c.dw, *dw_up = c.dw_up, *dw_down = c.dw_down;
+  if (!dx && !dw && !dw_up && !dw_down) return fail(SI_ERR_NULL, "none of the gradients is asked for");
   if (dw_up && !w_up) return fail(SI_ERR_ARG, "dw_up without w_up");
   if (u && !w_up) return fail(SI_ERR_ARG, "u without w_up");
+  const bool through = dx || dw || dw_up;
+  if (c.m > 0) {
+    REQUIRE_PTR(dy);
+    if (gated && through) REQUIRE_PTR(g);
+    if (w_up && through) REQUIRE_PTR(u);
+    if (dw || dw_up) REQUIRE_PTR(x);
+    if (dw_down) REQUIRE_PTR(h);
+  }
+  if (dx || c.m > 0) REQUIRE_PTR(w);
   REQUIRE_ELEMENT_ALIGNED(dy, dy_dtype);
   REQUIRE_ELEMENT_ALIGNED(x, c.type);
   REQUIRE_ELEMENT_ALIGNED(w, c.type);
   REQUIRE_ELEMENT_ALIGNED(w_up, c.type);
-  REQUIRE_ELEMENT_ALIGNED(g, g_dtype);
-  REQUIRE_ELEMENT_ALIGNED(u, c.type);
+  REQUIRE_ELEMENT_ALIGNED(w_down, c.type);
+  REQUIRE_ALIGNED(g);
+  REQUIRE_ALIGNED(u);
+  REQUIRE_ALIGNED(h);
   REQUIRE_ALIGNED(dx);
   REQUIRE_ALIGNED(dw);
   REQUIRE_ALIGNED(dw_up);
+  REQUIRE_ALIGNED(dw_down);
+  if (w_down && through && c.m > 0)
+    if (si_status s = fits(dense_dh_tile(c), c.m, c.rows, c.n)) return s;
   if (dx && c.m > 0)
     if (si_status s = fits(dense_dx_tile(c), c.m, c.rows, c.n)) return s;
   if (dw || dw_up)
     if (si_status s = fits(dense_dw_tile(c), c.m, c.rows, c.n)) return s;
+  if (dw_down)
+    if (si_status s = fits(dense_dw_down_tile(c), c.m, c.rows, c.n)) return s;
   const size_t wb = (size_t)c.rows * c.n * 2;
-  const Rows out[3] = {flat(dx, (size_t)c.m * c.n * 2), flat(dw, wb), flat(dw_up, wb)};
-  const Rows in[6] = {rows_of(c.dy, c.m, c.rows), rows_of(c.x, c.m, c.n),       flat(w, wb),
-                      flat(w_up, wb),             rows_of(c.gate, c.m, c.rows), rows_of(c.up, c.m, c.rows)};
-  for (int i = 0; i < 3; ++i) {
+  const Rows out[4] = {flat(dx, (size_t)c.m * c.n * 2), flat(dw, wb), flat(dw_up, wb), flat(dw_down, wb)};
+  const Rows in[8] = {rows_of(c.dy, c.m, dy_n),     rows_of(c.x, c.m, c.n),     flat(w, wb),     flat(w_up, wb),
+                      rows_of(c.gate, c.m, c.rows), rows_of(c.up, c.m, c.rows), flat(w_down, wb), rows_of(c.h, c.m, c.rows)};
+  for (int i = 0; i < 4; ++i) {
     for (const Rows& r : in)
       if (overlap(out[i], r)) return fail(SI_ERR_ARG, "a gradient overlaps an input");
     for (int j = 0; j < i; ++j)
       if (overlap(out[i], out[j])) return fail(SI_ERR_ARG, "two gradients overlap");
   }
   if (c.m == 0) c.dx = nullptr;
-  if (!c.dx && !c.dw && !c.dw_up) return SI_OK;
+  if (!c.dx && !c.dw && !c.dw_up && !c.dw_down) return SI_OK;
   if (si_status s = check_workspace(workspace, workspace_bytes, dense_grad_workspace(c))) return s;
   c.ws = workspace;
   return hip_status(launch_dense_grad(c, (hipStream_t)stream), "dense gradient launch");
+}
+
+// The gate's values of a gated product are its sums, float32; else its output.
+void set_gate(DenseGrad& c, const void* g, int g_dtype, const float* u) {
+  c.gate = DenseMat{g, c.w_up.p ? SI_F32 : g_dtype, (size_t)c.rows};
+  c.up = DenseMat{u, SI_F32, (size_t)c.rows};
+}
+
+DenseGrad mlp_call(const void* dy, int dy_dtype, size_t lddy, const void* x, int dtype, size_t ldx, int m, int d,
+                   const void* w_gate, const void* w_up, const void* w_down, int k, const void* h, const float* g,
+                   const float* u) {
+  DenseGrad c = grad_call(dy, dy_dtype, lddy, x, dtype, ldx, m, d, w_gate, w_up, k, false);
+  c.dy.ld = stride(lddy, m, d);
+  c.down = DenseMat{w_down, dtype, (size_t)k};
+  c.h = DenseMat{h, dtype, (size_t)k};
+  if (w_up)
+    set_gate(c, g, SI_F32, u);
+  else
+    set_gate(c, h, dtype, u);
+  return c;
 }
 
 alignas(16) const uint8_t kSome[16] = {};  // stands for operands of which only the presence counts
@@ -267,7 +297,7 @@ size_t si_gated_linear_workspace_bytes(const void* x, size_t ldx, int m, int n, 
 }
 
 si_status si_gated_linear(const void* x, int dtype, size_t ldx, int m, int n, const void* w_gate, const void* w_up,
-                          int rows, void* h, int h_dtype, void* g, void* u, void* workspace, size_t workspace_bytes,
+                          int rows, void* h, int h_dtype, float* g, float* u, void* workspace, size_t workspace_bytes,
                           void* stream) {
   DenseLinear c = linear_call(x, dtype, ldx, m, n, w_gate, w_up, rows, false);
   c.relu = !w_up;
@@ -303,24 +333,52 @@ size_t si_gated_linear_backward_workspace_bytes(const void* x, size_t ldx, int m
                                                 const void* w_up, int rows, int want_dx, int want_dw) {
   if (check_sizes(m, rows, n) != SI_OK || m == 0) return 0;
   DenseGrad c = grad_call(kSome, SI_F16, (size_t)rows, x, SI_F16, ldx, m, n, w_gate, w_up, rows, false);
-  c.gate = DenseMat{kSome, SI_F16, (size_t)rows};
-  if (w_up) c.up = c.gate;
+  set_gate(c, kSome, SI_F16, w_up ? reinterpret_cast<const float*>(kSome) : nullptr);
   c.dx = want_dx ? const_cast<uint8_t*>(kSome) : nullptr;
   c.dw = want_dw ? const_cast<uint8_t*>(kSome) : nullptr;
   return dense_grad_workspace(c);
 }
 
-si_status si_gated_linear_backward(const void* dh, int dh_dtype, size_t lddh, const void* g, int g_dtype, const void* u,
+si_status si_gated_linear_backward(const void* dh, int dh_dtype, size_t lddh, const void* g, int g_dtype, const float* u,
                                    const void* x, int dtype, size_t ldx, int m, int n, const void* w_gate,
                                    const void* w_up, int rows, void* dx, void* dw_gate, void* dw_up, void* workspace,
                                    size_t workspace_bytes, void* stream) {
   DenseGrad c = grad_call(dh, dh_dtype, lddh, x, dtype, ldx, m, n, w_gate, w_up, rows, false);
-  c.gate = DenseMat{g, g_dtype, (size_t)rows};
-  c.up = DenseMat{u, dtype, (size_t)rows};
+  if (w_up && g_dtype != SI_F32) return fail(SI_ERR_ARG, "g_dtype=%d: the sums of a gated product are float32", g_dtype);
+  set_gate(c, g, g_dtype, u);
   c.dx = dx;
   c.dw = dw_gate;
   c.dw_up = dw_up;
   return run_grad(c, lddh, ldx, true, workspace, workspace_bytes, stream);
+}
+
+size_t si_mlp_backward_workspace_bytes(const void* dy, int dy_dtype, size_t lddy, const void* x, size_t ldx, int m, int d,
+                                       const void* w_gate, const void* w_up, const void* w_down, int k, int want_dx,
+                                       int want_dw, int want_dw_down) {
+  if (check_sizes(m, k, d) != SI_OK || m == 0) return 0;
+  const float* sums = reinterpret_cast<const float*>(kSome);
+  DenseGrad c = mlp_call(dy, dy_dtype == SI_F32 ? SI_F32 : SI_F16, lddy, x, SI_F16, ldx, m, d, w_gate, w_up, w_down, k, kSome,
+                         sums, w_up ? sums : nullptr);
+  c.dx = want_dx ? const_cast<uint8_t*>(kSome) : nullptr;
+  c.dw = want_dw ? const_cast<uint8_t*>(kSome) : nullptr;
+  c.dw_down = want_dw_down ? const_cast<uint8_t*>(kSome) : nullptr;
+  return dense_grad_workspace(c);
+}
+
+si_status si_mlp_backward(const void* dy, int dy_dtype, size_t lddy, const void* x, int dtype, size_t ldx, int m, int d,
+                          const void* w_gate, const void* w_up, const void* w_down, int k, const void* h, const float* g,
+                          const float* u, void* dx, void* dw_gate, void* dw_up, void* dw_down, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  if (dy_dtype != dtype && dy_dtype != SI_F32) return fail(SI_ERR_ARG, "dy_dtype=%d: the products' type or float32", dy_dtype);
+  if (g && !w_up) return fail(SI_ERR_ARG, "g without w_up");
+  REQUIRE_PTR(w_down);
+  if (m > 0 && !w_up) REQUIRE_PTR(h);
+  DenseGrad c = mlp_call(dy, dy_dtype, lddy, x, dtype, ldx, m, d, w_gate, w_up, w_down, k, h, g, u);
+  c.dx = dx;
+  c.dw = dw_gate;
+  c.dw_up = dw_up;
+  c.dw_down = dw_down;
+  return run_grad(c, lddy, ldx, true, workspace, workspace_bytes, stream);
 }
 
 int si_dense_tile(int kind, int m, int rows, int n, int gated) {

@@ -136,10 +136,8 @@ __global__ __launch_bounds__(256) void k_dense_few(DenseArgs a) {
       float v = acc[0][i][t];
       if constexpr (MATS == 2) {
         if (a.g) {
-          uint16_t h = (uint16_t)(a.save_dtype == kBF16 ? pack_bf2(v, 0.f) : pack_f2(v, 0.f));
-          if (v > 0.f && h == 0) h = 1;  // as in the tiles
-          static_cast<uint16_t*>(a.g)[at] = h;
-          store_one(a.u, at, a.save_dtype, acc[1][i][t]);
+          a.g[at] = v;
+          a.u[at] = acc[MATS - 1][i][t];
         }
         v = (v > 0.f || v != v ? v : 0.f) * acc[MATS - 1][i][t];
       } else if (a.relu) {

@@ -104,7 +104,7 @@ __device__ inline void wait_stage() {
   asm volatile("" ::: "memory");
 }
 
-template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST>
+template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST, int GRAD>
 __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__  // the buffer descriptors are types of the device alone
   using P = DenseTile<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>;
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
   }
 
   // a lane holds m = 4 g .. 4 g + 3 of each piece for n = r of each
-  auto put = [&](void* y, int dt, int i, int t, f32x4 v, bool keep_sign) {
+  auto put = [&](void* y, int dt, int i, int t, f32x4 v) {
     const int m = m0 + piece_row(i) % (BM / MATS) + 4 * g;
     const int n = n0 + wn * (BN / WN) + t * 16 + r;
     if (n >= a.N || m >= a.M) return;
@@ -511,11 +511,7 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     }
     uint16_t h[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      h[e] = (uint16_t)(dt == kBF16 ? pack_bf2(v[e], 0.f) : pack_f2(v[e], 0.f));
-      // what the derivative asks of it, whether it is above 0, survives the rounding
-      if (keep_sign && v[e] > 0.f && h[e] == 0) h[e] = 1;
-    }
+    for (int e = 0; e < 4; ++e) h[e] = (uint16_t)(dt == kBF16 ? pack_bf2(v[e], 0.f) : pack_f2(v[e], 0.f));
     uint16_t* p = static_cast<uint16_t*>(y) + at;
     if ((a.M & 3) == 0) {
       *reinterpret_cast<u32x2*>(p) = u32x2{h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16};
@@ -531,20 +527,53 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     for (int i = 0; i < R; ++i) {
       const int mat = MATS == 2 ? i / (R / 2) : batch;
 #pragma unroll
-      for (int t = 0; t < C; ++t) put(a.part + (size_t)(part * a.parts_of + mat) * size, kF32, i, t, acc[i][t], false);
+      for (int t = 0; t < C; ++t) put(a.part + (size_t)(part * a.parts_of + mat) * size, kF32, i, t, acc[i][t]);
     }
     return;
   }
+  if constexpr (GRAD != 0) {
+    // dh: what is written is dg and du.  What they ask for is read B pieces ahead of the
+    // stores.
+    auto grads = [&](auto whole) {
+      constexpr bool UP = GRAD == 2, WHOLE = decltype(whole)::value;
+      constexpr int P = R * C, B = WHOLE && P >= 4 ? 4 : 1;
+      static_assert(P % B == 0);
+      const auto m_of = [&](int p) { return m0 + piece_row(p % R) + 4 * g; };
+      const auto n_of = [&](int p) { return n0 + wn * (BN / WN) + p / R * 16 + r; };
+      GatedPiece now[B], next[B];
+      auto read = [&](int p0, GatedPiece(&to)[B]) {
 #pragma unroll
-  for (int i = 0; i < R / MATS; ++i)
+        for (int j = 0; j < B; ++j)
+          if (n_of(p0 + j) < a.N) to[j] = gated_piece<UP, WHOLE>(a, n_of(p0 + j), m_of(p0 + j));
+      };
+      read(0, now);
 #pragma unroll
-    for (int t = 0; t < C; ++t) {
+      for (int p = 0; p < P; p += B) {
+        if (p + B < P) read(p + B, next);
+#pragma unroll
+        for (int j = 0; j < B; ++j) {
+          const int n = n_of(p + j), m = m_of(p + j);
+          if (n < a.N && m < a.ldc) put_gated_grad<UP>(a, n, m, acc[(p + j) % R][(p + j) / R], now[j]);
+          now[j] = next[j];
+        }
+      }
+    };
+    if ((a.M & 3) == 0)
+      grads(std::true_type{});
+    else
+      grads(std::false_type{});
+    return;
+  }
+#pragma unroll
+  for (int t = 0; t < C; ++t)
+#pragma unroll
+    for (int i = 0; i < R / MATS; ++i) {  // i inside: a row's pieces lie side by side
       f32x4 v = acc[i][t];
       if constexpr (MATS == 2) {
         const f32x4 u = acc[i + R / 2][t];
         if (a.g) {
-          put(a.g, a.save_dtype, i, t, v, true);
-          put(a.u, a.save_dtype, i, t, u, false);
+          put(a.g, kF32, i, t, v);
+          put(a.u, kF32, i, t, u);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = relu(v[e]) * u[e];
@@ -552,36 +581,36 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = relu(v[e]);
       }
-      put(a.c[batch], a.c_dtype, i, t, v, false);
+      put(a.c[batch], a.c_dtype, i, t, v);
     }
 #endif
 }
 
 // Launch of one tile shape over the whole product.
-template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST>
+template <int T, int AL, int BL, int MATS, int BM, int BN, int WM, int WN, int WK, int ST, int GRAD>
 hipError_t dense_tile_launch(DenseArgs a, int batches, hipStream_t s) {
   using P = DenseTile<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>;
   if (a.M < 1 || a.N < 1) return hipErrorInvalidValue;
   static std::atomic<int> attr_set[kMaxDevices];
   const int ok = per_device_once(attr_set, [](int) -> int {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_dense<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>),
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_dense<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST, GRAD>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, P::Lds) == hipSuccess ? 1 : -1;
   });
   if (ok != 1) return hipErrorInvalidConfiguration;
   a.m_tiles = (a.M + BM / MATS - 1) / (BM / MATS);
   a.n_tiles = (a.N + BN - 1) / BN;
-  k_dense<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST>
+  k_dense<T, AL, BL, MATS, BM, BN, WM, WN, WK, ST, GRAD>
       <<<(unsigned)(a.m_tiles * a.n_tiles * a.split * batches), WM * WN * WK * kWave, P::Lds, s>>>(a);
   return hipGetLastError();
 }
 
 // The tiles of kDenseTiles (dense.h), by their place there.
-template <int T, int AL, int BL, int MATS>
+template <int T, int AL, int BL, int MATS, int GRAD = 0>
 hipError_t dense_launch(const DenseArgs& a, int tile, int batches, hipStream_t s) {
 #define SI_DENSE_TILE(I, WM, WN, WK, ST) \
   case I:                                \
     static_assert(WK == kDenseTiles[I].wk && WM * WN * WK * kWave == kDenseTiles[I].threads && ST == kDenseTiles[I].st, "kDenseTiles"); \
-    return dense_tile_launch<T, AL, BL, MATS, kDenseTiles[I].bm, kDenseTiles[I].bn, WM, WN, WK, ST>(a, batches, s);
+    return dense_tile_launch<T, AL, BL, MATS, kDenseTiles[I].bm, kDenseTiles[I].bn, WM, WN, WK, ST, GRAD>(a, batches, s);
   if constexpr (BL == kRow) {
     switch (tile) {
       SI_DENSE_TILE(0, 2, 1, 4, 3)

@@ -12,7 +12,7 @@ import paper_2411_12692_amd as si
 from paper_2411_12692_amd import _lib
 
 A = 1 << 40  # a fake 16-byte-aligned address: validation fails before it is used
-B, C, D, E, F, G, H, I, J, K = (A + (i << 36) for i in range(1, 11))  # far apart: no overlap
+B, C, D, E, F, G, H, I, J, K, L, M = (A + (i << 36) for i in range(1, 13))  # far apart: no overlap
 F16, BF16, F32 = _lib.SI_F16, _lib.SI_BF16, _lib.SI_F32
 BIG = 1 << 50
 
@@ -116,6 +116,12 @@ def test_workspace_sizes(lib):
     gb = lib.si_gated_linear_backward_workspace_bytes
     assert gb(A, 128, 3, 128, B, C, 63, 1, 1) >= 2 * 3 * 64 * 2          # dg and du
     assert gb(A, 128, 0, 128, B, C, 63, 1, 1) == 0
+    mb = lib.si_mlp_backward_workspace_bytes
+    assert mb(A, F16, 128, B, 128, 3, 128, C, D, E, 64, 0, 0, 1) == 0    # dw_down alone: operands as they are
+    assert mb(A, F32, 128, B, 128, 3, 128, C, D, E, 64, 0, 0, 1) >= 3 * 128 * 2
+    assert mb(A, F16, 128, B, 128, 3, 128, C, D, E, 64, 1, 0, 0) >= 2 * 3 * 64 * 2
+    assert mb(A, F16, 128, B, 128, 3, 128, C, D, E + 2, 64, 1, 0, 0) >= 2 * 3 * 64 * 2 + 128 * 64 * 2
+    assert mb(A, F16, 128, B, 128, 0, 128, C, D, E, 64, 1, 1, 1) == 0
     assert lib.si_layer_norm_backward_workspace_bytes(5, 100) == 2 * 2 * 100 * 4  # two blocks of four rows
     assert lib.si_layer_norm_backward_workspace_bytes(0, 100) == 0
     assert lib.si_layer_norm_backward_workspace_bytes(5, 16385) == 0
@@ -159,13 +165,43 @@ def backward(dy=A, dy_dtype=F16, lddy=64, x=B, dtype=F16, ldx=128, m=3, n=128, w
     return "si_linear_backward", dy, dy_dtype, lddy, x, dtype, ldx, m, n, w, rows, t, dx, dw, ws, wb, None
 
 
-def gated_backward(dh=A, dh_dtype=F16, lddh=64, g=B, g_dtype=F16, u=C, x=D, dtype=F16, ldx=128, m=3, n=128, wg=E, wu=F,
+def gated_backward(dh=A, dh_dtype=F16, lddh=64, g=B, g_dtype=F32, u=C, x=D, dtype=F16, ldx=128, m=3, n=128, wg=E, wu=F,
                    rows=64, dx=G, dwg=H, dwu=I, ws=J, wb=BIG):
     return ("si_gated_linear_backward", dh, dh_dtype, lddh, g, g_dtype, u, x, dtype, ldx, m, n, wg, wu, rows, dx, dwg, dwu,
             ws, wb, None)
 
 
+def mlp_backward(dy=A, dy_dtype=F16, lddy=128, x=B, dtype=F16, ldx=128, m=3, d=128, wg=C, wu=D, wd=E, k=64, h=F, g=G, u=H,
+                 dx=I, dwg=J, dwu=K, dwd=L, ws=M, wb=BIG):
+    return ("si_mlp_backward", dy, dy_dtype, lddy, x, dtype, ldx, m, d, wg, wu, wd, k, h, g, u, dx, dwg, dwu, dwd, ws, wb, None)
+
+
 @pytest.mark.parametrize("status,call", [
+    (_lib.SI_ERR_ARG, mlp_backward(dtype=F32, dy_dtype=F32)), (_lib.SI_ERR_ARG, mlp_backward(dy_dtype=BF16)),
+    (_lib.SI_ERR_SHAPE, mlp_backward(m=-1)), (_lib.SI_ERR_SHAPE, mlp_backward(lddy=127)),
+    (_lib.SI_ERR_SHAPE, mlp_backward(ldx=127)), (_lib.SI_ERR_SHAPE, mlp_backward(k=0)),
+    (_lib.SI_ERR_SHAPE, mlp_backward(d=(1 << 20) + 1)), (_lib.SI_ERR_SHAPE, mlp_backward(m=1 << 24, k=1 << 20)),
+    (_lib.SI_ERR_NULL, mlp_backward(dx=None, dwg=None, dwu=None, dwd=None)), (_lib.SI_ERR_NULL, mlp_backward(dy=None)),
+    (_lib.SI_ERR_NULL, mlp_backward(x=None)), (_lib.SI_ERR_NULL, mlp_backward(wg=None)),
+    (_lib.SI_ERR_NULL, mlp_backward(wd=None)), (_lib.SI_ERR_NULL, mlp_backward(h=None)),
+    (_lib.SI_ERR_NULL, mlp_backward(g=None)), (_lib.SI_ERR_NULL, mlp_backward(u=None)),
+    (_lib.SI_ERR_NULL, mlp_backward(wu=None, dwu=None, g=None, u=None, h=None)),
+    (_lib.SI_ERR_ARG, mlp_backward(wu=None, dwu=None)), (_lib.SI_ERR_ARG, mlp_backward(wu=None, dwu=None, g=None)),
+    (_lib.SI_ERR_ARG, mlp_backward(wu=None, g=None, u=None)),
+    (_lib.SI_ERR_ALIGN, mlp_backward(dy=A + 1)), (_lib.SI_ERR_ALIGN, mlp_backward(wd=E + 1)),
+    (_lib.SI_ERR_ALIGN, mlp_backward(h=F + 8)), (_lib.SI_ERR_ALIGN, mlp_backward(g=G + 4)),
+    (_lib.SI_ERR_ALIGN, mlp_backward(u=H + 8)), (_lib.SI_ERR_ALIGN, mlp_backward(dwd=L + 2)),
+    (_lib.SI_ERR_ARG, mlp_backward(dwd=A)), (_lib.SI_ERR_ARG, mlp_backward(dx=F)), (_lib.SI_ERR_ARG, mlp_backward(dwd=G + 752)),
+    (_lib.SI_ERR_ARG, mlp_backward(dwu=L)), (_lib.SI_ERR_ARG, mlp_backward(dwg=E + 1024)),
+    (_lib.SI_ERR_NULL, mlp_backward(ws=None)), (_lib.SI_ERR_WORKSPACE, mlp_backward(wb=2 * 3 * 64 * 2 - 1)),
+    (_lib.SI_ERR_ALIGN, mlp_backward(ws=M + 4)),
+])
+def test_mlp_gradients_refuse(status, call):
+    refused(status, *call)
+
+
+@pytest.mark.parametrize("status,call", [
+    (_lib.SI_ERR_ARG, gated_backward(g_dtype=F16)), (_lib.SI_ERR_ALIGN, gated_backward(g=B + 4)),
     (_lib.SI_ERR_ARG, backward(dtype=F32, dy_dtype=F32)), (_lib.SI_ERR_ARG, backward(dy_dtype=BF16)),
     (_lib.SI_ERR_SHAPE, backward(m=-1)), (_lib.SI_ERR_SHAPE, backward(lddy=63)), (_lib.SI_ERR_SHAPE, backward(ldx=127)),
     (_lib.SI_ERR_SHAPE, backward(lddy=(1 << 21) + 1)), (_lib.SI_ERR_NULL, backward(dx=None, dw=None)),
@@ -248,7 +284,7 @@ def test_nothing_to_do():
     """No tokens: accepted without a launch (the weights' gradients, which are zeros
     then, are asked for on the GPU)."""
     for call in (linear(m=0, x=None), gated(m=0, x=None), quant(rows=0), fp8(m=0), norm(tokens=0, x=None),
-                 backward(m=0, dw=None), norm_backward(tokens=0, dw=None, db=None)):
+                 backward(m=0, dw=None), mlp_backward(m=0, dwg=None, dwu=None, dwd=None), norm_backward(tokens=0, dw=None, db=None)):
         assert _lib.status(*call) == _lib.SI_OK, (call[0], _lib.last_error())
 
 

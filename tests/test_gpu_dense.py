@@ -118,6 +118,36 @@ def test_gated_linear_backward(dtype, m, rows, n, up):
         same(got, w, dtype)
 
 
+@pytest.mark.parametrize("up", [True, False])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("m,rows,n", sorted(set(ref.shapes("transposed") + ref.shapes("dw transposed")) |
+                                            {(33, 37, 29), (2, 1, 1), (5, 9, 200), (300, 204, 1000), (7, 63, 8200)}))
+def test_mlp_backward(dtype, m, rows, n, up):
+    """All four gradients of the whole MLP, and each alone, exact: dh = dy W_down goes
+    into dg and du without a rounding."""
+    g = gen(21, m, rows, n)
+    few = min(1.0, 4.0 / n)  # of W_down's values are other than 0: dh stays small
+    x, wg, dy = sparse(g, m, n), sparse(g, rows, n), ref.whole(g, -1, 1, m, n)
+    wu = sparse(g, rows, n) if up else None
+    wd = ref.whole(g, -1, 1, n, rows) * (torch.rand(n, rows, generator=g) < few)
+    dh = sums(dy, wd.t())
+    dx, dwg, dwu = exact_gradients(x, wg, wu, dh, dtype)
+    pg, pu, h = gated_values(x, wg, wu, dtype)
+    want = [t for t in (dx, dwg, dwu, sums(dy.t(), h.t())) if t is not None]
+    leaves = [t.to(dtype).to(DEV).requires_grad_() if t is not None else None for t in (x, wg, wu, wd)]
+    y, leaves = si.mlp(*leaves), [t for t in leaves if t is not None]
+    dev = dy.to(dtype).to(DEV)
+    got = torch.autograd.grad(y, leaves, dev, retain_graph=True)
+    for a, w in zip(got, want):
+        same(a, w, dtype)
+    assert all(torch.equal(t, got[0]) for t in torch.autograd.grad(si.mlp(*(leaves if up else [*leaves[:2], None, leaves[2]]),
+                                                                          out_dtype=F32), leaves[0], dev.float()))
+    for i in range(len(leaves)):
+        part = [t.detach().requires_grad_(i == j) for j, t in enumerate(leaves)]
+        y = si.mlp(*(part if up else [*part[:2], None, part[2]]))
+        assert torch.equal(torch.autograd.grad(y, part[i], dev)[0], got[i])
+
+
 @pytest.mark.parametrize("transposed", [False, True])
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("m,rows,n", sorted(set(ref.shapes("dx") + ref.shapes("dw") + ref.shapes("dx transposed") +
@@ -146,7 +176,7 @@ def bound(k, size, dtype, roundings=1):
 @pytest.mark.parametrize("m,rows,n", [(1, 200, 4096), (3, 64, 11008), (37, 500, 1371), (333, 1371, 509)])
 def test_gaussian_values(dtype, m, rows, n):
     """A whole MLP forward and backward against float64, with the roundings on the way:
-    h; u, g, dh and dg, du (dx and the weights' gradients sum values of three of them)."""
+    h; dg and du."""
     g = gen(5, m, rows, n)
     x, wg, wu = (torch.randn(s, generator=g).mul(f).to(dtype).to(DEV).requires_grad_()
                  for s, f in (((m, n), 1.0), ((rows, n), n ** -0.5), ((rows, n), n ** -0.5)))
@@ -161,13 +191,12 @@ def test_gaussian_values(dtype, m, rows, n):
     eh = eg * pu.abs() + pg.abs() * eu + eg * eu + 2.0 ** -23 * h.abs() + HALF_STEP[dtype] * 1.01 * h.abs() + SMALLEST[dtype]
     size = h.abs() @ W.abs().t()
     assert ((y.detach().double() - h @ W.t()).abs() <= eh @ W.abs().t() + bound(rows, size + eh @ W.abs().t(), dtype)).all()
-    # gradients: h's own error does not enter; g and u are the stored ones
+    # gradients: h's own error enters dW_down alone; the sums and dh stay in float32
     near = pg.abs() <= eg  # the sign of a sum that cancels is not decided
     dh = DY @ W
-    edh = bound(n, DY.abs() @ W.abs(), dtype)
+    edh = bound(n, DY.abs() @ W.abs(), F32)
     on = (pg > 0).double()
     dg, du = dh * pu * on, dh * torch.relu(pg)
-    eu, eg = eu + HALF_STEP[dtype] * 1.01 * pu.abs() + SMALLEST[dtype], eg + HALF_STEP[dtype] * 1.01 * pg.abs() + SMALLEST[dtype]
     edg = edh * (pu.abs() + eu) + dh.abs() * eu
     edg = edg + HALF_STEP[dtype] * 1.01 * (dg.abs() + edg) + SMALLEST[dtype]
     edu = edh * (pg.abs() + eg) + dh.abs() * eg
@@ -244,8 +273,9 @@ def test_no_tokens():
     w = torch.ones(40, 64, dtype=F16, device=DEV).requires_grad_()
     for x in (torch.zeros(0, 64, dtype=F16, device=DEV), torch.zeros(2, 0, 64, dtype=F16, device=DEV)):
         x.requires_grad_()
-        for y in (si.linear(x, w), si.gated_linear(x, w, w), si.gated_linear(x, w)):
-            assert y.shape == (*x.shape[:-1], 40)
+        wd = torch.ones(64, 40, dtype=F16, device=DEV).requires_grad_()
+        for y in (si.linear(x, w), si.gated_linear(x, w, w), si.gated_linear(x, w), si.mlp(x, w, w, wd), si.mlp(x, w, None, wd)):
+            assert y.shape[:-1] == x.shape[:-1]
             dx, dw = torch.autograd.grad(y, (x, w), torch.zeros_like(y))
             assert dx.shape == x.shape and torch.equal(dw, torch.zeros_like(dw))
 
