@@ -64,7 +64,7 @@ struct DenseTile {
   // e4m3, one plane a stage: the scales of all tokens of the tile and of two blocks of
   // rows pass through LDS too, kScaleStages stages' at a time
   static constexpr bool Chunked = T == kTypeF8 && WK == 1;
-  static constexpr int ScaleB = BN * kScaleStages * 4, ScaleBytes = Chunked ? ScaleB + 32 : 0;
+  static constexpr int ScaleB = BN * kScaleStages * 4, ScaleBytes = Chunked ? ScaleB + 512 : 0;
   static constexpr int Lds = ST * Bytes + 2 * ScaleBytes;
   // LDS reads of a step, and the products between two of them, or two requests
   static constexpr int Reads = (AL == kRow ? R : 2 * R) + (BL == kRow ? C : 2 * C);
@@ -172,15 +172,9 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
   const int rows_a = (a_rows - 1) * (int)a.lda, rows_b = (b_rows - 1) * (int)a.ldb;
   auto whole = [](int n) { return (n + 16 / ES - 1) / (16 / ES) * 16; };  // in whole 16-byte pieces
   const int cols_a = whole(a.M - m0), cols_b = whole(a.N - n0);
-  auto request = [&](uint8_t* __restrict__ to) {
-    const int rows = min(left, KP * WK) - 1;
-    const int bytes_a = more <= 0 ? 0 : AL == kRow ? rows_a + whole(left) : rows * (int)a.lda + cols_a;
-    const int bytes_b = more <= 0 ? 0 : BL == kRow ? rows_b + whole(left) : rows * (int)a.ldb + cols_b;
-    const auto ra = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pa), 0, bytes_a, 0x00020000);
-    const auto ra2 = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pa + up), 0, bytes_a, 0x00020000);
-    const auto rb = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pb), 0, bytes_b, 0x00020000);
-#pragma unroll
-    for (int i = 0; i < NA; ++i) {
+  // request i of a stage of which `left` values of k are left
+  auto issue = [&](auto ra, auto ra2, auto rb, int left, uint8_t* __restrict__ to, int i) {
+    if (i < NA) {
       const int q = wv + NW * i;
       uint8_t* dst = to + q / QA * P::Plane + q % QA * 1024;
       const uint32_t off = AL == kRow && k_piece >= left - q / QA * KP ? 0x80000000u : oa[i];  // past every descriptor's end
@@ -188,14 +182,21 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ra2, (lds_u8*)dst, 16, off, 0, 0, 0);
       else
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_u8*)dst, 16, off, 0, 0, 0);
-    }
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int q = wv + NW * i;
+    } else {
+      const int q = wv + NW * (i - NA);
       uint8_t* dst = to + q / QB * P::Plane + P::ABytes + q % QB * 1024;
-      const uint32_t off = BL == kRow && k_piece >= left - q / QB * KP ? 0x80000000u : ob[i];
+      const uint32_t off = BL == kRow && k_piece >= left - q / QB * KP ? 0x80000000u : ob[i - NA];
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_u8*)dst, 16, off, 0, 0, 0);
     }
+  };
+  // the next stage's requests; between(i) stands in front of request i and behind the last
+  auto request_with = [&](uint8_t* __restrict__ to, auto between) {
+    const int now = left, rows = min(left, KP * WK) - 1;
+    const int bytes_a = more <= 0 ? 0 : AL == kRow ? rows_a + whole(left) : rows * (int)a.lda + cols_a;
+    const int bytes_b = more <= 0 ? 0 : BL == kRow ? rows_b + whole(left) : rows * (int)a.ldb + cols_b;
+    const auto ra = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pa), 0, bytes_a, 0x00020000);
+    const auto ra2 = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pa + up), 0, bytes_a, 0x00020000);
+    const auto rb = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(pb), 0, bytes_b, 0x00020000);
     --more;
     left -= KP * WK;
     pa += step_a;
@@ -205,7 +206,14 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
       pa = pa_next;
       pb = pb_next;
     }
+#pragma unroll
+    for (int i = 0; i < NA + NB; ++i) {
+      between(i);
+      issue(ra, ra2, rb, now, to, i);
+    }
+    between(NA + NB);
   };
+  auto request = [&](uint8_t* __restrict__ to) { request_with(to, [](int) {}); };
 
   const int wk = wv / (WM * WN), wm = wv / WN % WM, wn = wv % WN;
   const int r = lane & 15, g = lane >> 4;
@@ -271,88 +279,127 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
 
   if constexpr (P::Chunked) {
     // Stage k's scales lie in LDS, brought there a chunk of stages at a time: token
-    // after token, and behind them two rows of A's blocks (of each matrix, or two
-    // blocks of rows of one).  Past the last block and the last token they are zeros.
+    // after token, and behind them, 256 bytes apart, two rows of A's blocks (of each
+    // matrix, or two blocks of rows of one).  Past the last block and the last token
+    // they are zeros.
     uint8_t* const scale_lds = lds + ST * P::Bytes;
     auto request_scales = [&](int chunk) {
       uint8_t* const to = scale_lds + (chunk & 1) * P::ScaleBytes;
-      const int b0 = chunk * kScaleStages, end = a.blocks - b0;
+      const int b0 = chunk * kScaleStages, end = a.blocks - b0, b = lane & 3;
       const auto r = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<float*>(a.sb + (size_t)n0 * a.blocks + b0), 0, max(((b_rows - 1) * a.blocks + end) * 4, 0), 0x00020000);
 #pragma unroll
       for (int i = 0; i < BN * kScaleStages / 64 / NW; ++i) {
-        const int q = wv + NW * i, tok = q * 16 + lane / 4, b = lane & 3;
+        const int q = wv + NW * i, tok = q * 16 + lane / 4;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u8*)(to + q * 256), 4,
                                                  b < end ? (uint32_t)(tok * a.blocks + b) * 4 : 0x80000000u, 0, 0, 0);
       }
-      if (wv == 0) {
-        // lanes 0-3 the first row of blocks, 4-7 the second
-        const int w = lane >> 2, b = lane & 3;
-        const float* p = MATS == 2 && w == 1 ? a.sa[1] : a.sa[0];
-        const int row = min(m0 / 128 + (MATS == 1 ? w : 0), (a.M - 1) / 128);
-        float v = 0.f;
-        if (w < 2 && b < end) v = p[(size_t)row * a.blocks + b0 + b];
-        if (lane < 8) *reinterpret_cast<float*>(to + P::ScaleB + lane * 4) = v;
+      if (wv < 2) {
+        const int row = min(m0 / 128 + (MATS == 1 ? wv : 0), (a.M - 1) / 128);
+        const float* p = (MATS == 2 && wv == 1 ? a.sa[1] : a.sa[0]) + (size_t)row * a.blocks + b0;
+        const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), 0, max(min(end, kScaleStages) * 4, 0), 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_u8*)(to + P::ScaleB + wv * 256), 4, lane * 4, 0, 0, 0);
       }
     };
-    // the scale of the products of piece (i's matrix, t) in stage k
+    // the scales of stage k: of the rows of matrix w, of the tokens of piece t
     const int row_slot = MATS == 1 ? wm * (BM / WM) / 128 : 0;
-    auto factor_a = [&](int k, int w) {
-      return *reinterpret_cast<const float*>(scale_lds + (k / kScaleStages & 1) * P::ScaleBytes + P::ScaleB +
-                                             ((MATS == 2 ? w : row_slot) * kScaleStages + k % kScaleStages) * 4);
+    float fa[MATS], fb[C];
+    auto load_scales = [&](int k) {
+      const uint8_t* from = scale_lds + (k / kScaleStages & 1) * P::ScaleBytes + k % kScaleStages * 4;
+#pragma unroll
+      for (int w = 0; w < MATS; ++w)
+        fa[w] = *reinterpret_cast<const float*>(from + P::ScaleB + (MATS == 2 ? w : row_slot) * 256);
+#pragma unroll
+      for (int t = 0; t < C; ++t)
+        fb[t] = *reinterpret_cast<const float*>(from + (wn * (BN / WN) + t * 16 + r) * (kScaleStages * 4));
     };
-    auto factor_b = [&](int k, int t) {
-      const int tok = wn * (BN / WN) + t * 16 + r;
-      return *reinterpret_cast<const float*>(scale_lds + (k / kScaleStages & 1) * P::ScaleBytes + (tok * kScaleStages + k % kScaleStages) * 4);
+    // A stage is one step of K = 128 of each product.  A's pieces are read a row ahead;
+    // B's of the next stage while the last row's products let go of this one's, so that
+    // a wave keeps one set of B alone.  One barrier a stage, before that last row: all
+    // of the stage is read then (its part of LDS is free) and the next one has arrived.
+    u32x4 av[2][2], bv[C][2];
+    auto load_a = [&](const uint8_t* from, int i) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) av[i & 1][s] = read(LA{}, CA{}, from, piece_row(i), s);
     };
-    auto step = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from, int k) {
-      request(to);
-      u32x4 b[C][2];
-      float fa[MATS], fb[C];
+    auto load_b = [&](const uint8_t* from, int t) {
 #pragma unroll
-      for (int w = 0; w < MATS; ++w) fa[w] = factor_a(k, w);
-#pragma unroll
-      for (int t = 0; t < C; ++t) {
-        fb[t] = factor_b(k, t);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) b[t][s] = read(LB{}, CB{}, from + P::ABytes, wn * (BN / WN) + t * 16, s);
-      }
-#pragma unroll
-      for (int i = 0; i < R; ++i) {
-        const u32x4 a0 = read(LA{}, CA{}, from, piece_row(i), 0), a1 = read(LA{}, CA{}, from, piece_row(i), 1);
-#pragma unroll
-        for (int t = 0; t < C; ++t) {
-          const f32x4 v = dense_mfma<T>(a0, a1, b[t][0], b[t][1], f32x4{0.f, 0.f, 0.f, 0.f});
-          const float f = fa[MATS == 2 ? i / (R / 2) : 0] * fb[t];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(v[e], f, acc[i][t][e]);
-        }
-      }
-      if constexpr (R * C >= 32) {
-        // a request, a product and a read in turn behind the first operands
-        __builtin_amdgcn_sched_group_barrier(0x100, 2 * C + 2 + C + MATS, 0);
-#pragma unroll
-        for (int i = 0; i < P::Requests; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        }
-      }
+      for (int s = 0; s < 2; ++s) bv[t][s] = read(LB{}, CB{}, from + P::ABytes, wn * (BN / WN) + t * 16, s);
     };
+    // product j of the stage, and of an earlier one the sum: the matrix unit's result can
+    // be read 12 instructions later at the earliest, so that two other products lie between
+    constexpr int Lag = 2;
+    f32x4 v[Lag + 1];
+    auto multiply = [&](int j) {
+      const int i = j / C, t = j % C;
+      v[j % (Lag + 1)] = dense_mfma<T>(av[i & 1][0], av[i & 1][1], bv[t][0], bv[t][1], f32x4{0.f, 0.f, 0.f, 0.f});
+    };
+    auto add = [&](int j) {
+      const int i = j / C, t = j % C;
+      const float f = fa[MATS == 2 ? i / (R / 2) : 0] * fb[t];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(v[j % (Lag + 1)][e], f, acc[i][t][e]);
+    };
+    // Products first .. end - 1 in this order and no other.
+    auto product = [&](int j, int first) {
+      multiply(j);
+      if (j >= first + Lag) add(j - Lag);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto finish = [&](auto from, auto to) {
+      constexpr int First = decltype(from)::value, End = decltype(to)::value;
+#pragma unroll
+      for (int j = End - Lag; j < End; ++j) add(j);
+      // the sums are formed here: moved behind the barrier, their products would have to
+      // be kept
+#pragma unroll
+      for (int j = First; j < End; ++j) asm volatile("" : "+v"(acc[j / C][j % C]));
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    using J0 = std::integral_constant<int, 0>;
+    using J1 = std::integral_constant<int, (R - 1) * C>;
+    using J2 = std::integral_constant<int, R * C>;
+    auto rows = [&](const uint8_t* __restrict__ from, int k) {
+      load_scales(k);
+#pragma unroll
+      for (int j = 0; j < J1::value; ++j) {
+        if (j % C == 0) load_a(from, j / C + 1);
+        product(j, 0);
+      }
+      finish(J0{}, J1{});
+    };
+    // the requests between the products
+    auto last_row = [&](uint8_t* __restrict__ to, const uint8_t* __restrict__ from) {
+      load_a(from, 0);
+      request_with(to, [&](int i) {
+#pragma unroll
+        for (int t = 0; t < C; ++t)
+          if (t * P::Requests / C == i) {
+            product(J1::value + t, J1::value);
+            load_b(from, t);
+          }
+      });
+      finish(J1{}, J2{});
+    };
+    static_assert(R % 2 == 0, "A's two places");
     request_scales(k_first / kScaleStages);
     request_scales(k_first / kScaleStages + 1);
 #pragma unroll
-    for (int i = 0; i < ST - 1; ++i) request(lds + i * P::Bytes);
+    for (int i = 0; i < ST; ++i) request(lds + i * P::Bytes);
+    wait_stage<P::Requests * (ST - 1)>();
+    load_a(lds, 0);
+#pragma unroll
+    for (int t = 0; t < C; ++t) load_b(lds, t);
     int cur = 0;
     for (int k = k_first; k < k_last; ++k) {
-      // stage k and its scales are in LDS (the scales' loads, between the stages', make
-      // the wait longer, never shorter), and every wave has left the part that stage
-      // k + ST - 1 goes to
+      const int nxt = cur == ST - 1 ? 0 : cur + 1;
+      rows(lds + cur * P::Bytes, k);
+      // stage k + 1 is in LDS (the scales' loads, between the stages', make the wait
+      // longer, never shorter), and every wave has read all of stage k
       wait_stage<P::Requests * (ST - 2)>();
-      if (k % kScaleStages == 0 && k > k_first) request_scales(k / kScaleStages + 1);
-      const int nxt = cur == 0 ? ST - 1 : cur - 1;
-      step(lds + nxt * P::Bytes, lds + cur * P::Bytes, k);
-      cur = cur == ST - 1 ? 0 : cur + 1;
+      if (k % kScaleStages == kScaleStages - 1) request_scales(k / kScaleStages + 2);
+      last_row(lds + cur * P::Bytes, lds + nxt * P::Bytes);
+      cur = nxt;
     }
     wait_all_requests();  // none may arrive in LDS that is no longer this block's
   } else if constexpr (T == kTypeF8) {
