@@ -421,7 +421,7 @@ _DTYPE = {torch.float16: _lib.SI_F16, torch.int16: _lib.SI_F16, torch.bfloat16: 
           torch.float32: _lib.SI_F32}
 _HALF = frozenset((torch.float16, torch.int16, torch.bfloat16))
 _ANY = _HALF | {torch.float32}
-_current_device = torch.cuda.current_device
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 # These calls take a few microseconds each, so what is checked on every call is
