@@ -570,8 +570,9 @@ si_status si_norm_residual(const void* h, int h_dtype, size_t ldh, const void* b
  *   y, h: [m][rows] of type y_dtype / h_dtype, written.
  *   g, u: both or neither: the two sums themselves, [m][rows] in float32, for the
  *         backward pass.  With w_up only.
- *   m 0 to 2^24 (0 does nothing), rows and n 1 to 2^20, m times rows or n below 2^35
- *         and few enough blocks for one launch (else SI_ERR_SHAPE).
+ *   m 0 to 2^24 (0 does nothing), rows and n 1 to 2^20; m times rows, m times n and
+ *         rows times n below 2^35, and few enough blocks for one launch (else
+ *         SI_ERR_SHAPE).
  *   workspace: the ..._workspace_bytes() of the call: scratch for split sums and for
  *         copies of operands that cannot be read in 16-byte pieces (rows of a multiple
  *         of 8 values that start on 16 bytes can).  Nothing is kept in it from one call
@@ -597,7 +598,8 @@ si_status si_gated_linear(const void* x, int dtype, size_t ldx, int m, int n, co
  *   dy  : m rows of type dtype or float32, lddy elements from row to row; dh of any
  *         type.  dy (as an operand of the products), dg and du are rounded to dtype.
  *   g, u: as si_gated_linear kept them (g_dtype SI_F32).  w_up NULL: u NULL, and g is its
- *         output h, [m][rows] of type g_dtype (si_mlp_backward: g NULL).
+ *         output h, [m][rows] of type g_dtype (si_mlp_backward: g NULL); where that was
+ *         rounded to 0 the gradient is 0.
  *   h   : [m][k] of type dtype, si_gated_linear's output.
  *   g, u and h on 16 bytes.
  *   dx, dw, dw_gate, dw_up, dw_down: [m][n] and the weights' shapes, of type dtype,

@@ -25,8 +25,9 @@ size_t stride(size_t ld, int rows, int n) { return rows > 1 ? ld : (size_t)n; }
 si_status check_sizes(int m, int rows, int n) {
   if (si_status s = check_rows_n("m", m, n, kMaxLen)) return s;
   if (rows < 1 || rows > kMaxLen) return fail(SI_ERR_SHAPE, "rows=%d outside [1, %d]", rows, kMaxLen);
-  // element-wise kernels: 8 values a thread
-  if ((double)m * (std::max(rows, n) + 8) >= 34359738368.0)
+  // copies and element-wise kernels: 8 values a thread, 2^32 threads a launch
+  const double most = 34359738368.0, longer = std::max(rows, n) + 8.0;
+  if (m * longer >= most || std::min(rows, n) * longer >= most)
     return fail(SI_ERR_SHAPE, "m=%d rows=%d n=%d: more than one launch can hold", m, rows, n);
   return SI_OK;
 }

@@ -147,6 +147,7 @@ def gated(x=A, dtype=F16, ldx=128, m=3, n=128, wg=B, wu=C, rows=64, h=D, h_dtype
     (_lib.SI_ERR_SHAPE, linear(n=(1 << 20) + 1)), (_lib.SI_ERR_SHAPE, linear(rows=0)),
     (_lib.SI_ERR_SHAPE, linear(rows=(1 << 20) + 1)), (_lib.SI_ERR_SHAPE, linear(ldx=127)),
     (_lib.SI_ERR_SHAPE, linear(ldx=(1 << 21) + 1)), (_lib.SI_ERR_SHAPE, linear(m=1 << 24, rows=1 << 20)),
+    (_lib.SI_ERR_SHAPE, linear(n=1 << 18, ldx=1 << 18, rows=1 << 17)), (_lib.SI_ERR_SHAPE, linear(n=1 << 17, ldx=1 << 17, rows=1 << 18, t=1)),
     (_lib.SI_ERR_NULL, linear(x=None)), (_lib.SI_ERR_NULL, linear(w=None)), (_lib.SI_ERR_NULL, linear(y=None)),
     (_lib.SI_ERR_ALIGN, linear(x=A + 1)), (_lib.SI_ERR_ALIGN, linear(w=B + 1)), (_lib.SI_ERR_ALIGN, linear(y=C + 8)),
     (_lib.SI_ERR_ARG, linear(y=A + 256)), (_lib.SI_ERR_ARG, linear(y=B + 64 * 128 * 2 - 16)),
