@@ -4,7 +4,9 @@
 // while one is multiplied; the tokens' values come from the caches.  Sums stay with the
 // lanes until the row ends.
 //
-// Bound by W's bytes: at one token 2 flops for each value read.
+// Bound by W's bytes: at one token 2 flops for each value read.  7B gate and up (180 MB):
+// 27.2 us, 6.6 TB/s; e4m3, 4096 x 11008 (45 MB): 10 us, 4.5 TB/s, a launch and two round
+// trips of memory.
 #include "dense.h"
 #include "layer_common.h"
 

@@ -16,6 +16,16 @@
 // Loads are buffer loads whose descriptor ends with the operand: what lies behind
 // its last row, or is addressed past it on purpose (the last pieces of k), arrives
 // as zeros, so sums need no tail.
+//
+// Large products are bound by the matrix cores, and these by power: alone, without
+// loads, 16 x 16 x 32 products of random bf16 values run at 1980 TFLOP/s (of zeros at
+// 2430).  A wave's 64 x 128 values (256 x 256 a block, 128 sums a lane) take 24 reads of
+// LDS for 64 products; its requests, 64 of 1 KiB a block and stage, cost the address unit
+// 16 cycles each and are the next limit.  Measured at 8192^3, random values: x W^T 1260,
+// dy W 1290, dy^T x 1320, gate and up without their sums 1405 TFLOP/s, no conflicts in
+// LDS; e4m3, 13824 x 5120 and 4096 tokens, 1900 (2150 of zeros, 3050 of zeros without the
+// loads).  Small tiles are for few tokens, where W's bytes bound: 13824 x 5120 gate and
+// up, 37 tokens, 56 us, 5.1 TB/s of W.
 #pragma once
 
 #include <type_traits>
@@ -313,6 +323,8 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
       for (int t = 0; t < C; ++t)
         fb[t] = *reinterpret_cast<const float*>(from + (wn * (BN / WN) + t * 16 + r) * (kScaleStages * 4));
     };
+    // Every product's sum is multiplied by its block's scales: 4 vector instructions to a
+    // product, which the waves of a SIMD hide behind each other's products.
     // A stage is one step of K = 128 of each product.  A's pieces are read a row ahead;
     // B's of the next stage while the last row's products let go of this one's, so that
     // a wave keeps one set of B alone.  One barrier a stage, before that last row: all

