@@ -637,7 +637,7 @@ size_t si_mlp_backward_workspace_bytes(const void* dy, int dy_dtype, size_t lddy
  * Diagnostic, host-only: which kernel a dense product of these sizes takes.  kind 0:
  * si_linear (1: with W^T) or si_gated_linear; 2: the gradient with respect to x (3: with
  * W^T); 4: with respect to W (5: with W^T); 6: the FP8 products.  gated nonzero: with
- * W_up.  100: the one for a few tokens; 0 and up: the place of its tile in the library's
+ * W_up.  (si_mlp_backward: dh 1 and dw_down 5, of rows k and n d, the rest 2 and 4.)  100: the one for a few tokens; 0 and up: the place of its tile in the library's
  * list, smallest first; -2: sizes that the product refuses, or m = 0.
  */
 int si_dense_tile(int kind, int m, int rows, int n, int gated);

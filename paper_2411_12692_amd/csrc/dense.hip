@@ -181,7 +181,7 @@ class Copies {
  public:
   Copies(int type, char*& ws) : ws_(ws) { jobs_.type = type; }
   void add(DenseMat& a, size_t rows, int n) {
-    if (!a.p || !needs_copy(a, jobs_.type, n)) return;
+    if (!a.p || rows == 0 || !needs_copy(a, jobs_.type, n)) return;
     const int np = pad8(n);
     jobs_.job[jobs_.count++] = PadJob{a, rows, n, np, reinterpret_cast<u32x4*>(ws_)};
     a = DenseMat{ws_, jobs_.type, (size_t)np};
@@ -320,7 +320,7 @@ hipError_t launch_dense_linear(const DenseLinear& c, hipStream_t s) {
 
 size_t dense_grad_workspace(const DenseGrad& c) {
   const size_t one = align256((size_t)c.m * pad8(c.rows) * 2) * (c.up.p ? 2 : 1);
-  const bool want_w = c.dw || c.dw_up, through = c.dx || want_w;  // dg and du are asked for
+  const bool want_w = c.dw || c.dw_up, through = (c.dx || want_w) && c.m > 0;  // dg and du are asked for
   size_t b = 0, part = 0;
   if (c.down.p) {
     b += copy_bytes(c.dy, c.type, c.m, c.n);
@@ -349,7 +349,7 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
   const int type = c.type == kBF16 ? 1 : 0;
   DenseMat d = c.dy, du = {};
   DenseMat x = c.x, w = c.w, up = c.w_up, down = c.down, h = c.h;
-  const bool want_w = c.dw || c.dw_up, through = c.dx || want_w;
+  const bool want_w = c.dw || c.dw_up, through = (c.dx || want_w) && c.m > 0;
   Copies copies(c.type, ws);
   const int rp = pad8(c.rows);
   const size_t bytes = align256((size_t)c.m * rp * 2);
@@ -382,7 +382,7 @@ hipError_t launch_dense_grad(const DenseGrad& c, hipStream_t s) {
     copies.add(up, wr, wc);
   }
   TRY(copies.launch(s));
-  if (c.down.p && through && c.m > 0) {
+  if (c.down.p && through) {
     const Plan p = dh_plan(c);
     DenseArgs a = {};
     a.a[0] = down.p;

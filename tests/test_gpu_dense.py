@@ -268,16 +268,21 @@ def test_leading_dimensions_and_single_rows():
     assert row.shape == (40,) and torch.equal(row, si.linear(x.detach()[0, 0], w.detach())[0])
 
 
-def test_no_tokens():
-    """Nothing is computed; the weights' gradients are zeros."""
-    w = torch.ones(40, 64, dtype=F16, device=DEV).requires_grad_()
-    for x in (torch.zeros(0, 64, dtype=F16, device=DEV), torch.zeros(2, 0, 64, dtype=F16, device=DEV)):
+@pytest.mark.parametrize("n,k", [(64, 40), (37, 29)])
+def test_no_tokens(n, k):
+    """Nothing is computed; the weights' gradients are zeros.  At odd lengths there is
+    nothing to copy either."""
+    w, wt, wd = (torch.ones(*s, dtype=F16, device=DEV).requires_grad_() for s in ((k, n), (n, k), (n, k)))
+    for x in (torch.zeros(0, n, dtype=F16, device=DEV), torch.zeros(2, 0, n, dtype=F16, device=DEV)):
         x.requires_grad_()
-        wd = torch.ones(64, 40, dtype=F16, device=DEV).requires_grad_()
-        for y in (si.linear(x, w), si.gated_linear(x, w, w), si.gated_linear(x, w), si.mlp(x, w, w, wd), si.mlp(x, w, None, wd)):
+        for f, leaves in ((lambda: si.linear(x, w), (w,)), (lambda: si.linear(x, wt, transposed=True), (wt,)),
+                          (lambda: si.linear(x, w, out_dtype=F32), (w,)), (lambda: si.gated_linear(x, w, w), (w,)),
+                          (lambda: si.gated_linear(x, w), (w,)), (lambda: si.mlp(x, w, w, wd), (w, wd)),
+                          (lambda: si.mlp(x, w, None, wd), (w, wd))):
+            y = f()
             assert y.shape[:-1] == x.shape[:-1]
-            dx, dw = torch.autograd.grad(y, (x, w), torch.zeros_like(y))
-            assert dx.shape == x.shape and torch.equal(dw, torch.zeros_like(dw))
+            dx, *dw = torch.autograd.grad(y, (x, *leaves), torch.zeros_like(y))
+            assert dx.shape == x.shape and all(torch.equal(d, torch.zeros_like(d)) for d in dw)
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -480,6 +485,24 @@ def test_run_to_run():
         h = si.gated_linear(x, w, w)
         runs.append([h.detach(), *torch.autograd.grad(h, (x, w), dh)])
     assert all(torch.equal(a, b) for r in runs[1:] for a, b in zip(r, runs[0]))
+
+
+def test_mlp_gradients_on_several_streams():
+    """Steps with scratch at once on several streams, odd lengths among the copies."""
+    g = gen(22)
+    leaves = [torch.randn(*s, generator=g).mul(0.1).half().to(DEV).requires_grad_() for s in ((70, 109), (203, 109), (203, 109), (109, 203))]
+    dy = torch.randn(70, 109, generator=g).half().to(DEV)
+
+    def step():
+        y = si.mlp(*leaves)
+        return [y.detach(), *torch.autograd.grad(y, leaves, dy)]
+    want, out = step(), []
+    torch.cuda.synchronize()
+    for s in [torch.cuda.Stream() for _ in range(3)]:
+        with torch.cuda.stream(s):
+            out.append(step())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for o in out for a, b in zip(o, want))
 
 
 def test_captured_training_step():
