@@ -847,18 +847,6 @@ def _flat(x, name: str, dtypes):
     return (x2, *_rows(x2, name, dtypes))
 
 
-def _grad_rows(dy):
-    """A gradient as rows of any stride; those that autograd hands on expanded or
-    transposed are copied.  Returns ``(dy2, stride)``."""
-    dy2 = dy if dy.dim() == 2 else dy.reshape(-1, dy.shape[-1])
-    m, n = dy2.shape
-    if dy2.is_contiguous():
-        return dy2, n
-    if (n > 1 and dy2.stride(1) != 1) or (m > 1 and not n <= dy2.stride(0) <= 1 << 21):
-        dy2 = dy2.contiguous()
-    return dy2, dy2.stride(0) if m > 1 else n
-
-
 def _weight(w, name: str, x, shape=None):
     """A contiguous matrix of ``x``'s type."""
     _dev(w, name, _HALF, 2)
@@ -890,41 +878,19 @@ def _linear_forward(x2, m, n, ld, w, rows, transposed, out_dtype):
     return y
 
 
-def _first_order(backward):
-    """The gradients have none of their own: where a graph of the backward pass is
-    asked for, its use raises (``once_differentiable``); else that wrapper's time is
-    saved."""
-    guarded = torch.autograd.function.once_differentiable(backward)
-
-    def run(ctx, dy):
-        return guarded(ctx, dy) if torch.is_grad_enabled() else backward(ctx, dy)
-    return run
+_nodes = None
 
 
-class _Linear(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x2, w, m, n, ld, rows, transposed, out_dtype):
-        ctx.save_for_backward(x2, w)
-        ctx.args = (m, n, ld, rows, transposed)
-        return _linear_forward(x2, m, n, ld, w, rows, transposed, out_dtype)
-
-    @staticmethod
-    @_first_order
-    def backward(ctx, dy):
-        x2, w = ctx.saved_tensors
-        m, n, ld, rows, transposed = ctx.args
-        if _DTYPE[dy.dtype] not in (_DTYPE[x2.dtype], _lib.SI_F32):
-            dy = dy.float()
-        dy, ldd = _grad_rows(dy)
-        want_x, want_w = ctx.needs_input_grad[:2]
-        dx = x2.new_empty((m, n)) if want_x else None
-        dw = torch.empty_like(w) if want_w else None
-        nbytes = _dense_workspace("si_linear_backward_workspace_bytes", _like(dy), _DTYPE[dy.dtype], ldd, _like(x2), ld, m, n,
-                                  _like(w), rows, transposed, want_x, want_w)
-        ws = _scratch(x2, nbytes)
-        _call_on(_same_device(x2, dy, w), "si_linear_backward", dy.data_ptr(), _DTYPE[dy.dtype], ldd, x2.data_ptr(),
-                 _DTYPE[x2.dtype], ld, m, n, w.data_ptr(), rows, transposed, _vp(dx), _vp(dw), _vp(ws), nbytes)
-        return dx, dw, None, None, None, None, None, None
+def _graph(x):
+    """The module that places a call in autograd's graph (``csrc/autograd.cpp``), and the
+    stream of the call."""
+    global _nodes
+    if _nodes is None:
+        _nodes = _lib.autograd()
+    index = x.get_device()
+    if _raw_stream is not None:
+        return _nodes, _raw_stream(index)
+    return _nodes, torch.cuda.current_stream(index).cuda_stream
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, transposed: bool = False, out_dtype=None) -> torch.Tensor:
@@ -937,10 +903,10 @@ def linear(x: torch.Tensor, w: torch.Tensor, transposed: bool = False, out_dtype
     if shape[0 if transposed else 1] != n:
         raise ValueError(f"w {tuple(shape)} does not take rows of {n} values")
     out_dtype = _out_type(out_dtype, x)
+    y = _linear_forward(x2, m, n, ld, w, rows, bool(transposed), out_dtype)
     if _wants_grad(x, w):
-        y = _Linear.apply(x2, w, m, n, ld, rows, bool(transposed), out_dtype)
-    else:
-        y = _linear_forward(x2, m, n, ld, w, rows, bool(transposed), out_dtype)
+        graph, stream = _graph(x2)
+        graph.linear(y, x2, w, m, n, ld, rows, bool(transposed), stream)
     return y if x.dim() == 2 else y.view(*x.shape[:-1], rows)
 
 
@@ -958,33 +924,6 @@ def _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, keep):
     return h, g, u
 
 
-class _GatedLinear(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x2, w_gate, w_up, m, n, ld, rows, out_dtype):
-        h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, True)
-        ctx.save_for_backward(x2, w_gate, w_up, h if w_up is None else g, u)
-        ctx.args = (m, n, ld, rows)
-        return h
-
-    @staticmethod
-    @_first_order
-    def backward(ctx, dh):
-        x2, w_gate, w_up, g, u = ctx.saved_tensors
-        m, n, ld, rows = ctx.args
-        dh, ldd = _grad_rows(dh)
-        want_x, want_g, want_u = ctx.needs_input_grad[:3]
-        dx = x2.new_empty((m, n)) if want_x else None
-        dg = torch.empty_like(w_gate) if want_g else None
-        du = torch.empty_like(w_up) if want_u else None
-        nbytes = _dense_workspace("si_gated_linear_backward_workspace_bytes", _like(x2), ld, m, n, _like(w_gate), _like(w_up),
-                                  rows, want_x, want_g or want_u)
-        ws = _scratch(x2, nbytes)
-        _call_on(_same_device(x2, dh, w_gate, w_up), "si_gated_linear_backward", dh.data_ptr(), _DTYPE[dh.dtype], ldd,
-                 g.data_ptr(), _DTYPE[g.dtype], _vp(u), x2.data_ptr(), _DTYPE[x2.dtype], ld, m, n, w_gate.data_ptr(),
-                 _vp(w_up), rows, _vp(dx), _vp(dg), _vp(du), _vp(ws), nbytes)
-        return dx, dg, du, None, None, None, None, None
-
-
 def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor = None, out_dtype=None) -> torch.Tensor:
     """``ReLU(x W_gate^T) * (x W_up^T)`` over every row, Eq. (1) steps 1-3, in one
     launch (``si_gated_linear``); ``w_up=None``: ``ReLU(x W_fc1^T)``.  ``x [..., n]``
@@ -999,41 +938,12 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor = Non
     if w_up is not None:
         _weight(w_up, "w_up", x, (rows, n))
     out_dtype = _out_type(out_dtype, x)
-    if _wants_grad(x, w_gate, w_up):
-        h = _GatedLinear.apply(x2, w_gate, w_up, m, n, ld, rows, out_dtype)
-    else:
-        h = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, False)[0]
+    keep = _wants_grad(x, w_gate, w_up)
+    h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, keep)
+    if keep:
+        graph, stream = _graph(x2)
+        graph.gated_linear(h, x2, w_gate, w_up, g, u, m, n, ld, rows, stream)
     return h if x.dim() == 2 else h.view(*x.shape[:-1], rows)
-
-
-class _MLP(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x2, w_gate, w_up, w_down, m, n, ld, rows, out_dtype):
-        h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, x2.dtype, True)
-        ctx.save_for_backward(x2, w_gate, w_up, w_down, h, g, u)
-        ctx.args = (m, n, ld, rows)
-        return _linear_forward(h, m, rows, rows, w_down, n, False, out_dtype)
-
-    @staticmethod
-    @_first_order
-    def backward(ctx, dy):
-        x2, w_gate, w_up, w_down, h, g, u = ctx.saved_tensors
-        m, n, ld, rows = ctx.args
-        if _DTYPE[dy.dtype] not in (_DTYPE[x2.dtype], _lib.SI_F32):
-            dy = dy.float()
-        dy, ldd = _grad_rows(dy)
-        want_x, want_g, want_u, want_d = ctx.needs_input_grad[:4]
-        dx = x2.new_empty((m, n)) if want_x else None
-        dg = torch.empty_like(w_gate) if want_g else None
-        du = torch.empty_like(w_up) if want_u else None
-        dd = torch.empty_like(w_down) if want_d else None
-        nbytes = _dense_workspace("si_mlp_backward_workspace_bytes", _like(dy), _DTYPE[dy.dtype], ldd, _like(x2), ld, m, n,
-                                  _like(w_gate), _like(w_up), _like(w_down), rows, want_x, want_g or want_u, want_d)
-        ws = _scratch(x2, nbytes)
-        _call_on(_same_device(x2, dy, w_gate, w_up, w_down), "si_mlp_backward", dy.data_ptr(), _DTYPE[dy.dtype], ldd,
-                 x2.data_ptr(), _DTYPE[x2.dtype], ld, m, n, w_gate.data_ptr(), _vp(w_up), w_down.data_ptr(), rows,
-                 h.data_ptr(), _vp(g), _vp(u), _vp(dx), _vp(dg), _vp(du), _vp(dd), _vp(ws), nbytes)
-        return dx, dg, du, dd, None, None, None, None, None
 
 
 def mlp(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, out_dtype=None) -> torch.Tensor:
@@ -1050,11 +960,12 @@ def mlp(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch
         _weight(w_up, "w_up", x, (rows, n))
     _weight(w_down, "w_down", x, (n, rows))
     out_dtype = _out_type(out_dtype, x)
-    if _wants_grad(x, w_gate, w_up, w_down):
-        y = _MLP.apply(x2, w_gate, w_up, w_down, m, n, ld, rows, out_dtype)
-    else:
-        h = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, x2.dtype, False)[0]
-        y = _linear_forward(h, m, rows, rows, w_down, n, False, out_dtype)
+    keep = _wants_grad(x, w_gate, w_up, w_down)
+    h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, x2.dtype, keep)
+    y = _linear_forward(h, m, rows, rows, w_down, n, False, out_dtype)
+    if keep:
+        graph, stream = _graph(x2)
+        graph.mlp(y, x2, w_gate, w_up, w_down, h, g, u, m, n, ld, rows, stream)
     return y if x.dim() == 2 else y.view(x.shape)
 
 
@@ -1071,34 +982,6 @@ def _norm_forward(x2, tokens, d, ld, w, b, center, eps, keep):
     return y, mean, rstd
 
 
-class _Norm(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x2, w, b, tokens, d, ld, center, eps):
-        y, mean, rstd = _norm_forward(x2, tokens, d, ld, w, b, center, eps, True)
-        ctx.save_for_backward(x2, w, mean, rstd)
-        ctx.args = (tokens, d, ld, center)
-        return y
-
-    @staticmethod
-    @_first_order
-    def backward(ctx, dy):
-        x2, w, mean, rstd = ctx.saved_tensors
-        tokens, d, ld, center = ctx.args
-        dy, ldd = _grad_rows(dy)
-        want_x, want_w, want_b = ctx.needs_input_grad[:3]
-        dx = x2.new_empty((tokens, d)) if want_x else None
-        dw = torch.empty_like(w) if want_w else None
-        db = torch.empty_like(w) if want_b else None
-        nbytes = 0
-        if want_w or want_b:
-            nbytes = _dense_workspace("si_layer_norm_backward_workspace_bytes", tokens, d)
-        ws = _scratch(x2, nbytes)
-        _call_on(_same_device(x2, dy, w), "si_layer_norm_backward", dy.data_ptr(), ldd, x2.data_ptr(), _DTYPE[x2.dtype], ld,
-                 w.data_ptr(), _DTYPE[w.dtype], center, _vp(mean), _vp(rstd), _vp(dx), _vp(dw), _vp(db), tokens, d, _vp(ws),
-                 nbytes)
-        return dx, dw, db, None, None, None, None, None
-
-
 _FLOATS = frozenset((torch.float16, torch.bfloat16, torch.float32))
 
 
@@ -1112,10 +995,11 @@ def _norm(x, w, b, eps, center):
             raise ValueError(f"{name} must be [{d}], got {list(t.shape)}")
     if b is not None and b.dtype != w.dtype:
         raise TypeError(f"b has dtype {b.dtype}, w {w.dtype}")
-    if _wants_grad(x, w, b):
-        y = _Norm.apply(x2, w, b, tokens, d, ld, center, float(eps))
-    else:
-        y = _norm_forward(x2, tokens, d, ld, w, b, center, float(eps), False)[0]
+    keep = _wants_grad(x, w, b)
+    y, mean, rstd = _norm_forward(x2, tokens, d, ld, w, b, center, float(eps), keep)
+    if keep:
+        graph, stream = _graph(x2)
+        graph.norm(y, x2, w, b, mean, rstd, tokens, d, ld, center, stream)
     return y if x.dim() == 2 else y.view(x.shape)
 
 

@@ -132,6 +132,16 @@ def load() -> ctypes.CDLL:
     return _lib
 
 
+def autograd():
+    """The nodes of PyTorch's graph (``csrc/autograd.cpp``).  Raises if they have not
+    been built."""
+    load()
+    if not os.path.exists(os.path.join(_HERE, "_autograd.so")):
+        raise RuntimeError(f"{_HERE}/_autograd.so is missing: build it with `python -m paper_2411_12692_amd.build`")
+    from . import _autograd
+    return _autograd
+
+
 def call(name: str, *args) -> None:
     """Call an entry point that returns si_status; raise on failure."""
     st = getattr(_lib or load(), name)(*args)

@@ -1,4 +1,4 @@
-"""Build libsparseinfer.so (HIP, gfx950) in-tree with hipcc.
+"""Build libsparseinfer.so (HIP, gfx950) and _autograd.so (host code) in-tree.
 
 Usage: ``python -m paper_2411_12692_amd.build`` (or ``__graft_entry__.build()``).
 ``python -m paper_2411_12692_amd.build --trace`` builds the phase-trace
@@ -13,6 +13,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -20,6 +21,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libsparseinfer.so")
 TRACE_LIB = os.path.join(PKG, "libsparseinfer_trace.so")
+AUTOGRAD_LIB = os.path.join(PKG, "_autograd.so")
 TRACED = "owned.hip"  # the source compiled with -DSI_TRACE in the trace variant
 SOURCES = ["api.hip", "pack.hip", "predict.hip", "mlp.hip", "owned.hip", "diag.hip",
            "mx_quant.hip", "mx_linear.hip", "mx_sparse.hip", "mx_api.hip", "norm.hip",
@@ -28,6 +30,8 @@ SOURCES = ["api.hip", "pack.hip", "predict.hip", "mlp.hip", "owned.hip", "diag.h
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc" if os.path.exists("/opt/rocm/bin/hipcc") else "hipcc")
+
+CXX = os.environ.get("CXX", "g++")
 
 # Packed-FP32 instructions are disabled: compile plain scalar float code only.
 COMMON = [
@@ -46,9 +50,27 @@ def _run(cmd):
     return out
 
 
+def build_autograd() -> str:
+    """Compile and link the nodes of PyTorch's graph (``csrc/autograd.cpp``, host code
+    beside the library, which it finds in its own folder)."""
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    os.makedirs(BUILD, exist_ok=True)
+    obj = os.path.join(BUILD, "autograd.o")
+    include = [f"-I{p}" for p in (*include_paths(), sysconfig.get_paths()["include"])]
+    _run([CXX, "-O2", "-std=c++17", "-fPIC", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+          *include, "-c", os.path.join(CSRC, "autograd.cpp"), "-o", obj])
+    tmp = AUTOGRAD_LIB + ".tmp"
+    _run([CXX, "-shared", obj, "-o", tmp, f"-L{PKG}", "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN",
+          *[f"-L{p}" for p in library_paths()], "-lc10", "-ltorch_cpu", "-ltorch", "-ltorch_python"])
+    shutil.move(tmp, AUTOGRAD_LIB)
+    return AUTOGRAD_LIB
+
+
 def build(verbose: bool = False, trace: bool = False) -> str:
     """Compile every HIP source and link the shared library (``trace``: the
-    phase-trace variant); returns its path."""
+    phase-trace variant), then the nodes of PyTorch's graph; returns the library's
+    path."""
     out_dir = os.path.join(BUILD, "trace") if trace else BUILD
     lib = TRACE_LIB if trace else LIB
     os.makedirs(out_dir, exist_ok=True)
@@ -68,6 +90,8 @@ def build(verbose: bool = False, trace: bool = False) -> str:
     tmp = lib + ".tmp"
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp])
     shutil.move(tmp, lib)
+    if not trace:
+        build_autograd()
     return lib
 
 

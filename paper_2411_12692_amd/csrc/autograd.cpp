@@ -1,0 +1,216 @@
+// The gradients' place in PyTorch's graph of calls: nodes whose backward pass is one call
+// of the library (include/sparseinfer.h), on the stream of the forward call.  Host code:
+// a node written in Python took 40 us more of a training step's host time (LayerNorm of
+// 16 tokens, forward and backward: 114 us), which is more than the kernels of a small one.
+#include <ATen/ops/empty.h>
+#include <ATen/ops/empty_like.h>
+#include <c10/core/DeviceGuard.h>
+#include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
+#include <torch/csrc/autograd/saved_variable.h>
+#include <torch/csrc/utils/pybind.h>
+
+#include <optional>
+
+#include "../../include/sparseinfer.h"
+
+namespace {
+
+using at::Tensor;
+using torch::autograd::Node;
+using torch::autograd::SavedVariable;
+using torch::autograd::variable_list;
+
+int type_of(const Tensor& t) {
+  return t.scalar_type() == at::kFloat ? SI_F32 : t.scalar_type() == at::kBFloat16 ? SI_BF16 : SI_F16;
+}
+void* ptr(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+float* floats(const Tensor& t) { return static_cast<float*>(ptr(t)); }
+
+void check(si_status s) { TORCH_CHECK(s == SI_OK, "status ", (int)s, ": ", si_last_error()); }
+
+Tensor scratch(const Tensor& like, size_t bytes) {
+  return bytes ? at::empty({(int64_t)bytes}, like.options().dtype(at::kByte)) : Tensor();
+}
+
+// A gradient as rows of n values; those that are handed on expanded or transposed are
+// copied.
+struct Rows {
+  Tensor t;
+  size_t ld;
+};
+Rows rows_of(const Tensor& grad, int64_t n) {
+  Tensor t = grad.dim() == 2 ? grad : grad.reshape({-1, n});
+  const bool many = t.size(0) > 1;
+  if (!t.is_contiguous() && ((n > 1 && t.stride(1) != 1) || (many && (t.stride(0) < n || t.stride(0) > 1 << 21))))
+    t = t.contiguous();
+  return {t, (size_t)(many && !t.is_contiguous() ? t.stride(0) : n)};
+}
+
+// One call of a differentiable operator: its saved tensors and sizes, m rows of n (of
+// stride ld) to m rows of `rows`.
+struct Call : Node {
+  SavedVariable x, w, w_up, w_down, g, u, h;  // (norms: w, and the rows' mean and r as g, u)
+  int m = 0, n = 0, rows = 0;
+  size_t ld = 0;
+  bool flag = false;  // W^T in memory, or LayerNorm
+  void* stream = nullptr;
+
+  void release_variables() override {
+    for (SavedVariable* v : {&x, &w, &w_up, &w_down, &g, &u, &h}) v->reset_data();
+  }
+
+  // the gradients that are asked for
+  virtual void run(const Tensor& grad, const Tensor& x, const Tensor& w, variable_list& out) = 0;
+
+  variable_list apply(variable_list&& in) override {
+    std::lock_guard<std::mutex> lock(mutex_);
+    const bool graph = at::GradMode::is_enabled();
+    variable_list out(num_outputs());
+    if (!in[0].defined()) return out;
+    {
+      at::NoGradGuard none;
+      const Tensor xt = x.unpack(), wt = w.unpack();
+      const c10::DeviceGuard guard(xt.device());
+      run(in[0], xt, wt, out);
+    }
+    if (!graph) return out;
+    // the gradients have none of their own: a graph of them is refused where it is used
+    const auto refuse = std::make_shared<torch::autograd::DelayedError>(
+        "the gradients of this operator are first order: they cannot be differentiated again", (int64_t)out.size());
+    for (Tensor& t : out)
+      if (t.defined()) t.requires_grad_();
+    return (*refuse)(std::move(out));
+  }
+
+  bool wants(size_t i) const { return task_should_compute_output(i); }
+  Tensor like(bool want, const Tensor& t) const { return want ? at::empty_like(t) : Tensor(); }
+  Tensor dx_of(const Tensor& xt) const { return wants(0) ? at::empty({m, n}, xt.options()) : Tensor(); }
+};
+
+// of the products' type or float32
+Tensor operand(const Tensor& grad, const Tensor& xt) {
+  return grad.scalar_type() == xt.scalar_type() || grad.scalar_type() == at::kFloat ? grad : grad.to(at::kFloat);
+}
+
+struct LinearGrad : Call {
+  std::string name() const override { return "SparseInferLinearGrad"; }
+  void run(const Tensor& grad, const Tensor& xt, const Tensor& wt, variable_list& out) override {
+    const Rows dy = rows_of(operand(grad, xt), rows);
+    out = {dx_of(xt), like(wants(1), wt)};
+    const size_t bytes = si_linear_backward_workspace_bytes(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), ld, m, n, ptr(wt), rows,
+                                                            flag, out[0].defined(), out[1].defined());
+    const Tensor ws = scratch(xt, bytes);
+    check(si_linear_backward(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), type_of(xt), ld, m, n, ptr(wt), rows, flag, ptr(out[0]),
+                             ptr(out[1]), ptr(ws), bytes, stream));
+  }
+};
+
+struct GatedGrad : Call {
+  std::string name() const override { return "SparseInferGatedLinearGrad"; }
+  void run(const Tensor& grad, const Tensor& xt, const Tensor& wt, variable_list& out) override {
+    const Tensor up = w_up.unpack(), ut = u.unpack(), gt = up.defined() ? g.unpack() : h.unpack(shared_from_this());
+    const Rows dh = rows_of(grad, rows);
+    out = {dx_of(xt), like(wants(1), wt), like(wants(2), up)};
+    const size_t bytes = si_gated_linear_backward_workspace_bytes(ptr(xt), ld, m, n, ptr(wt), ptr(up), rows, out[0].defined(),
+                                                                  out[1].defined() || out[2].defined());
+    const Tensor ws = scratch(xt, bytes);
+    check(si_gated_linear_backward(ptr(dh.t), type_of(dh.t), dh.ld, ptr(gt), type_of(gt), floats(ut), ptr(xt), type_of(xt), ld,
+                                   m, n, ptr(wt), ptr(up), rows, ptr(out[0]), ptr(out[1]), ptr(out[2]), ptr(ws), bytes,
+                                   stream));
+  }
+};
+
+struct MlpGrad : Call {
+  std::string name() const override { return "SparseInferMlpGrad"; }
+  void run(const Tensor& grad, const Tensor& xt, const Tensor& wt, variable_list& out) override {
+    const Tensor up = w_up.unpack(), down = w_down.unpack(), gt = g.unpack(), ut = u.unpack(), ht = h.unpack();
+    const Rows dy = rows_of(operand(grad, xt), n);
+    out = {dx_of(xt), like(wants(1), wt), like(wants(2), up), like(wants(3), down)};
+    const size_t bytes = si_mlp_backward_workspace_bytes(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), ld, m, n, ptr(wt), ptr(up),
+                                                         ptr(down), rows, out[0].defined(),
+                                                         out[1].defined() || out[2].defined(), out[3].defined());
+    const Tensor ws = scratch(xt, bytes);
+    check(si_mlp_backward(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), type_of(xt), ld, m, n, ptr(wt), ptr(up), ptr(down), rows,
+                          ptr(ht), floats(gt), floats(ut), ptr(out[0]), ptr(out[1]), ptr(out[2]), ptr(out[3]), ptr(ws), bytes,
+                          stream));
+  }
+};
+
+struct NormGrad : Call {
+  std::string name() const override { return flag ? "SparseInferLayerNormGrad" : "SparseInferRmsNormGrad"; }
+  void run(const Tensor& grad, const Tensor& xt, const Tensor& wt, variable_list& out) override {
+    const Tensor mean = g.unpack(), r = u.unpack();
+    const Rows dy = rows_of(grad, n);
+    out = {dx_of(xt), like(wants(1), wt), like(wants(2), wt)};
+    const size_t bytes = out[1].defined() || out[2].defined() ? si_layer_norm_backward_workspace_bytes(m, n) : 0;
+    const Tensor ws = scratch(xt, bytes);
+    check(si_layer_norm_backward(ptr(dy.t), dy.ld, ptr(xt), type_of(xt), ld, ptr(wt), type_of(wt), flag, floats(mean), floats(r),
+                                 ptr(out[0]), ptr(out[1]), ptr(out[2]), m, n, ptr(ws), bytes, stream));
+  }
+};
+
+using Maybe = std::optional<Tensor>;
+Tensor given(const Maybe& t) { return t.value_or(Tensor()); }
+SavedVariable saved(const Maybe& t, bool output = false) {
+  return t.has_value() ? SavedVariable(*t, output) : SavedVariable();
+}
+
+// The node of a call that has been made, and y as its output.
+template <class T, class... Inputs>
+std::shared_ptr<T> attach(Tensor y, int m, int n, size_t ld, int rows, bool flag, uintptr_t stream, const Tensor& x,
+                          const Tensor& w, const Inputs&... more) {
+  auto call = std::shared_ptr<T>(new T(), torch::autograd::deleteNode);
+  call->set_next_edges(torch::autograd::collect_next_edges(x, w, more...));
+  call->x = SavedVariable(x, false);
+  call->w = SavedVariable(w, false);
+  call->m = m;
+  call->n = n;
+  call->rows = rows;
+  call->ld = ld;
+  call->flag = flag;
+  call->stream = reinterpret_cast<void*>(stream);
+  torch::autograd::set_history(y, call);
+  return call;
+}
+
+void linear(const Tensor& y, const Tensor& x, const Tensor& w, int m, int n, size_t ld, int rows, bool transposed,
+            uintptr_t stream) {
+  attach<LinearGrad>(y, m, n, ld, rows, transposed, stream, x, w);
+}
+
+void gated_linear(const Tensor& h, const Tensor& x, const Tensor& w_gate, const Maybe& w_up, const Maybe& g, const Maybe& u,
+                  int m, int n, size_t ld, int rows, uintptr_t stream) {
+  const auto c = attach<GatedGrad>(h, m, n, ld, rows, false, stream, x, w_gate, given(w_up));
+  c->w_up = saved(w_up);
+  c->g = saved(g);
+  c->u = saved(u);
+  if (!w_up.has_value()) c->h = SavedVariable(h, true);
+}
+
+void mlp(const Tensor& y, const Tensor& x, const Tensor& w_gate, const Maybe& w_up, const Tensor& w_down, const Tensor& h,
+         const Maybe& g, const Maybe& u, int m, int n, size_t ld, int rows, uintptr_t stream) {
+  const auto c = attach<MlpGrad>(y, m, n, ld, rows, false, stream, x, w_gate, given(w_up), w_down);
+  c->w_up = saved(w_up);
+  c->w_down = SavedVariable(w_down, false);
+  c->h = SavedVariable(h, false);
+  c->g = saved(g);
+  c->u = saved(u);
+}
+
+void norm(const Tensor& y, const Tensor& x, const Tensor& w, const Maybe& b, const Maybe& mean, const Tensor& r, int tokens,
+          int d, size_t ld, bool center, uintptr_t stream) {
+  const auto c = attach<NormGrad>(y, tokens, d, ld, d, center, stream, x, w, given(b));
+  c->g = saved(mean);
+  c->u = SavedVariable(r, false);
+}
+
+}  // namespace
+
+PYBIND11_MODULE(_autograd, module) {
+  module.def("linear", &linear);
+  module.def("gated_linear", &gated_linear);
+  module.def("mlp", &mlp);
+  module.def("norm", &norm);
+}

@@ -560,3 +560,76 @@ def test_prompt_of_the_fp16_layer(m, up):
     # decode keeps h in float32: half a step of fp16 and the two sums' additions
     assert ((y[:4].double() - dense).abs() <= (2.0 ** -11 * 1.01 + (k + d + 128) * 2.0 ** -22) * (size[:4] + 2.0 ** -14 * k)).all()
     assert torch.equal(layer.prompt(x), y.half()) and layer.prompt(x.view(1, m, d)).shape == (1, m, d)
+
+
+# ---- the place in autograd's graph ------------------------------------------------------
+
+def layer_of(g, m=40, d=96, k=130):
+    vals = [torch.randn(*s, generator=g).mul(0.1).half().to(DEV).requires_grad_() for s in ((m, d), (d,), (k, d), (k, d), (d, k))]
+    return vals, torch.randn(m, d, generator=g).half().to(DEV)
+
+
+def block(x, nw, wg, wu, wd):
+    return x + si.mlp(si.rms_norm(x, nw), wg, wu, wd) + si.linear(si.gated_linear(si.layer_norm(x, nw, nw), wg), wd)
+
+
+def test_backward_accumulates_and_frees():
+    leaves, dy = layer_of(gen(30))
+    want = torch.autograd.grad(block(*leaves), leaves, dy)
+    y = block(*leaves)
+    y.backward(dy, retain_graph=True)
+    assert all(torch.equal(t.grad, w) for t, w in zip(leaves, want))
+    y.backward(dy)
+    assert all(torch.equal(t.grad, w + w) for t, w in zip(leaves, want))
+    with pytest.raises(RuntimeError, match="second time"):
+        y.backward(dy)
+
+
+@pytest.mark.parametrize("up", [True, False])
+def test_a_saved_tensor_changed_in_place_is_refused(up):
+    (x, _, wg, wu, wd), dy = layer_of(gen(31))
+    for f in (lambda x: si.linear(x, wd, transposed=True), lambda x: si.gated_linear(x, wg, wu if up else None),
+              lambda x: si.mlp(x, wg, wu if up else None, wd), lambda x: si.rms_norm(x, x.detach()[0].float())):
+        own = x.detach().clone()
+        y = f(own.requires_grad_())
+        with torch.no_grad():
+            own.add_(1)
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.float().sum().backward()
+
+
+def test_hooks_of_saved_tensors():
+    """Checkpointing and saving to the host go through the same values."""
+    from torch.utils.checkpoint import checkpoint
+    leaves, dy = layer_of(gen(32))
+    want = torch.autograd.grad(block(*leaves), leaves, dy)
+    got = torch.autograd.grad(checkpoint(block, *leaves, use_reentrant=False), leaves, dy)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    with torch.autograd.graph.save_on_cpu():
+        y = block(*leaves)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(y, leaves, dy), want))
+
+
+def test_gradients_on_this_thread_and_of_some_leaves():
+    leaves, dy = layer_of(gen(33))
+    want = torch.autograd.grad(block(*leaves), leaves, dy)
+    with torch.autograd.set_multithreading_enabled(False):
+        got = torch.autograd.grad(block(*leaves), leaves, dy)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    y = block(*leaves)
+    for i in range(len(leaves)):  # only what is asked for is computed
+        assert torch.equal(torch.autograd.grad(y, leaves[i], dy, retain_graph=True)[0], want[i])
+    out = si.linear(leaves[0], leaves[2])
+    unused = torch.autograd.grad(out[:0].sum() * 0 + leaves[1].sum(), (leaves[0], leaves[1]), allow_unused=True)
+    assert unused[0] is None or not unused[0].any()
+
+
+def test_a_graph_of_the_gradients_is_refused_where_it_is_used():
+    leaves, dy = layer_of(gen(34))
+    for f, of in ((lambda x, nw, wg, wu, wd: si.mlp(x, wg, wu, wd), (0, 2, 3, 4)), (lambda x, nw, *_: si.layer_norm(x, nw), (0, 1)),
+                  (lambda x, nw, wg, wu, wd: si.gated_linear(x, wg, wu), (0, 2, 3))):
+        y = f(*leaves)
+        grads = torch.autograd.grad(y, [leaves[i] for i in of], torch.ones_like(y), create_graph=True)
+        assert all(t.requires_grad for t in grads)
+        with pytest.raises(RuntimeError, match="first order"):
+            sum(t.float().sum() for t in grads).backward()
