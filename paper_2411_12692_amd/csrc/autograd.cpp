@@ -5,6 +5,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/functions/utils.h>
@@ -157,10 +158,24 @@ SavedVariable saved(const Maybe& t, bool output = false) {
   return t.has_value() ? SavedVariable(*t, output) : SavedVariable();
 }
 
+// While an eager graph of a leaf lives, the leaf's place for gradients belongs to that
+// graph's stream, and a backward pass captured on another one would end the capture, and
+// the process, where autograd lets the two streams wait for each other.
+void refuse_foreign_leaf(const Tensor& t) {
+  if (!t.defined() || !t.requires_grad() || !t.is_leaf()) return;
+  const auto place = torch::autograd::impl::try_get_grad_accumulator(t);
+  if (!place || !place->stream().has_value()) return;
+  if (*place->stream() == c10::impl::VirtualGuardImpl(t.device().type()).getStream(t.device())) return;
+  TORCH_CHECK(!py::module_::import("torch.cuda").attr("is_current_stream_capturing")().cast<bool>(),
+              "a call under capture with a leaf of an eager graph that still lives: release that graph first, or capture "
+              "with leaves of the graph's own");
+}
+
 // The node of a call that has been made, and y as its output.
-template <class T, class... Inputs>
+template <class T, class... Inputs>  // (Inputs: tensors)
 std::shared_ptr<T> attach(Tensor y, int m, int n, size_t ld, int rows, bool flag, uintptr_t stream, const Tensor& x,
                           const Tensor& w, const Inputs&... more) {
+  for (const Tensor* t : {&x, &w, &more...}) refuse_foreign_leaf(*t);
   auto call = std::shared_ptr<T>(new T(), torch::autograd::deleteNode);
   call->set_next_edges(torch::autograd::collect_next_edges(x, w, more...));
   call->x = SavedVariable(x, false);

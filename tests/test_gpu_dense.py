@@ -633,3 +633,29 @@ def test_a_graph_of_the_gradients_is_refused_where_it_is_used():
         assert all(t.requires_grad for t in grads)
         with pytest.raises(RuntimeError, match="first order"):
             sum(t.float().sum() for t in grads).backward()
+
+
+def test_capture_with_leaves_of_a_live_graph_is_refused():
+    """Autograd would end the process in the backward pass; once the eager graph is gone
+    the same capture goes through."""
+    (x, nw, wg, wu, wd), dy = layer_of(gen(35))
+    for f in (lambda: si.mlp(x, wg, wu, wd), lambda: si.rms_norm(x, nw), lambda: si.linear(x, wg), lambda: si.gated_linear(x, wg, wu)):
+        alive = f()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with pytest.raises(RuntimeError, match="eager graph"):
+            with torch.cuda.graph(graph):
+                f()
+        torch.cuda.synchronize()
+        want = torch.autograd.grad(alive, x, torch.ones_like(alive))[0]
+        del alive, graph
+        graph = torch.cuda.CUDAGraph()
+        ones = torch.ones_like(f())
+        with torch.cuda.graph(graph):
+            y = f()
+            got = torch.autograd.grad(y, x, ones)[0]
+        del y
+        for _ in range(3):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
