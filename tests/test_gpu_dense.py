@@ -659,3 +659,24 @@ def test_capture_with_leaves_of_a_live_graph_is_refused():
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(got, want)
+
+
+def test_fp16_bits_and_graphs_of_one_gradient():
+    """x as int16 (fp16 bits) has no gradient, W has; a graph of the gradients where only
+    one is asked for."""
+    (x, nw, wg, wu, wd), dy = layer_of(gen(36))
+    bits = x.detach().view(torch.int16)
+    with pytest.raises(TypeError, match="int16"):
+        si.linear(bits, wg)
+    with torch.no_grad():
+        assert torch.equal(si.linear(bits, wg).view(F16), si.linear(x, wg))
+    dh = torch.ones(40, 130, dtype=F16, device=DEV)
+    for f in (lambda a: si.linear(a, wg, out_dtype=F16), lambda a: si.gated_linear(a, wg, wu, out_dtype=F16)):
+        assert torch.equal(torch.autograd.grad(f(bits), wg, dh)[0], torch.autograd.grad(f(x), wg, dh)[0])
+    assert torch.equal(torch.autograd.grad(si.mlp(bits, wg, wu, wd, out_dtype=F16), wd, dy)[0],
+                       torch.autograd.grad(si.mlp(x, wg, wu, wd), wd, dy)[0])
+    for f in (lambda: si.linear(x, wg.detach()), lambda: si.rms_norm(x, nw.detach()), lambda: si.mlp(x, wg.detach(), None, wd.detach())):
+        y = f()
+        (dx,) = torch.autograd.grad(y, x, torch.ones_like(y), create_graph=True)
+        with pytest.raises(RuntimeError, match="first order"):
+            dx.float().sum().backward()
