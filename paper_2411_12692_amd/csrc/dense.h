@@ -97,10 +97,8 @@ __device__ inline GatedPiece gated_piece(const DenseArgs& a, int n, int m) {
   return p;
 }
 
-// dg and du in their place, zeros behind the M-th.
-template <bool UP>
-__device__ inline void put_gated_grad(const DenseArgs& a, int n, int m, f32x4 dh, const GatedPiece& p) {
-  const size_t at = (size_t)n * a.ldc + m;
+// dg (x, y) and du (z, w) of four values from m on, rounded; zeros behind the M-th.
+__device__ inline u32x4 gated_grads(const DenseArgs& a, int m, f32x4 dh, const GatedPiece& p) {
   float x[4], y[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -108,9 +106,16 @@ __device__ inline void put_gated_grad(const DenseArgs& a, int n, int m, f32x4 dh
     if (m + e >= a.M) x[e] = y[e] = 0.f;
   }
   auto pack = [&](float v, float w) { return a.c_dtype == kBF16 ? pack_bf2(v, w) : pack_f2(v, w); };
-  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.c[0]) + at) = u32x2{pack(x[0], x[1]), pack(x[2], x[3])};
-  if constexpr (UP)
-    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.du) + at) = u32x2{pack(y[0], y[1]), pack(y[2], y[3])};
+  return u32x4{pack(x[0], x[1]), pack(x[2], x[3]), pack(y[0], y[1]), pack(y[2], y[3])};
+}
+
+// They in their place.
+template <bool UP>
+__device__ inline void put_gated_grad(const DenseArgs& a, int n, int m, f32x4 dh, const GatedPiece& p) {
+  const size_t at = (size_t)n * a.ldc + m;
+  const u32x4 v = gated_grads(a, m, dh, p);
+  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.c[0]) + at) = u32x2{v.x, v.y};
+  if constexpr (UP) *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.du) + at) = u32x2{v.z, v.w};
 }
 
 // ---- calls (dense.hip), arguments validated by the caller ----------------------

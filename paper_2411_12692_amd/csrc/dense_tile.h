@@ -551,6 +551,94 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
         for (int t = 0; t < C; ++t) acc[i][t] += sums[(((q - 1) * R + i) * C + t) * (WM * WN * kWave)];
   }
 
+  // Whole rows of 16-byte pieces are written by way of LDS (WK = 1: its stages are done
+  // with): a lane holds 8 or 16 bytes of each of many rows, and stores of it would be
+  // pieces of 32 or 64 bytes, each a write of the L2 of its own.  Turned, 16 bytes a lane,
+  // they are as much of a row as the wave has.  value(i, t): 4 values from m = 4 g on of
+  // piece i for n = r of piece t, as they are stored.
+  constexpr int RM = R / MATS;
+  auto turned = [&](auto bytes, void* y, size_t row_len, int m_end, auto value) {
+    constexpr int Size = decltype(bytes)::value, Row = RM * 16 * Size, Pieces = Row / 16, Room = ST * P::Bytes / NW;
+    constexpr int Fit = Room / (16 * Row), TP = Fit < C ? Fit : C;
+    static_assert(WK > 1 || (TP >= 1 && C % TP == 0 && Pieces >= 2), "a wave's part of LDS");
+    uint8_t* const own = lds + wv * Room;
+    const int m_first = m0 + piece_row(0) % (BM / MATS), n_first = n0 + wn * (BN / WN);
+#pragma unroll
+    for (int t0 = 0; t0 < C; t0 += TP) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the reads before
+#pragma unroll
+      for (int t = t0; t < t0 + TP; ++t)
+#pragma unroll
+        for (int i = 0; i < RM; ++i) {
+          const int row = (t - t0) * 16 + r;
+          const auto v = value(i, t);
+          static_assert(sizeof(v) == 4 * Size);
+          const int p = Size == 4 ? 4 * i + g : 2 * i + (g >> 1);
+          uint8_t* to = own + row * Row + ((p ^ (row & (Pieces - 1))) * 16) + (Size == 4 ? 0 : (g & 1) * 8);
+          *reinterpret_cast<std::remove_const_t<decltype(v)>*>(to) = v;
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int q = 0; q < TP * 16 * Pieces / kWave; ++q) {
+        const int at = q * kWave + lane, row = at / Pieces, p = at % Pieces;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(own + row * Row + ((p ^ (row & (Pieces - 1))) * 16));
+        const int n = n_first + t0 * 16 + row, m = m_first + p * (16 / Size);
+        if (n < a.N && m < m_end) *reinterpret_cast<u32x4*>(static_cast<uint8_t*>(y) + ((size_t)n * row_len + m) * Size) = v;
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
+  using Two = std::integral_constant<int, 2>;
+  using Four = std::integral_constant<int, 4>;
+  // values of float32 as dt
+  auto write = [&](void* y, int dt, auto value) {
+    if (dt == kF32)
+      turned(Four{}, y, a.M, a.M, value);
+    else if (dt == kBF16)
+      turned(Two{}, y, a.M, a.M, [&](int i, int t) {
+        const f32x4 v = value(i, t);
+        return u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
+      });
+    else
+      turned(Two{}, y, a.M, a.M, [&](int i, int t) {
+        const f32x4 v = value(i, t);
+        return u32x2{pack_f2(v[0], v[1]), pack_f2(v[2], v[3])};
+      });
+  };
+  // what is written of piece (i, t) of a product
+  auto output = [&](int i, int t) {
+    f32x4 v = acc[i][t];
+    if constexpr (MATS == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = relu(v[e]) * acc[i + R / 2][t][e];
+    } else if (a.relu) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = relu(v[e]);
+    }
+    return v;
+  };
+  if constexpr (WK == 1 && GRAD == 0) {
+    if (a.M % 8 == 0) {
+      __syncthreads();
+      if (a.part) {
+        const size_t size = (size_t)a.M * a.N;
+        float* const to = a.part + (size_t)(part * a.parts_of + batch) * size;
+        write(to, kF32, [&](int i, int t) { return acc[i][t]; });
+        if constexpr (MATS == 2) write(to + size, kF32, [&](int i, int t) { return acc[i + R / 2][t]; });
+        return;
+      }
+      if constexpr (MATS == 2) {
+        if (a.g) {
+          write(a.g, kF32, [&](int i, int t) { return acc[i][t]; });
+          write(a.u, kF32, [&](int i, int t) { return acc[i + R / 2][t]; });
+        }
+      }
+      write(a.c[batch], a.c_dtype, output);
+      return;
+    }
+  }
+
   // a lane holds m = 4 g .. 4 g + 3 of each piece for n = r of each
   auto put = [&](void* y, int dt, int i, int t, f32x4 v) {
     const int m = m0 + piece_row(i) % (BM / MATS) + 4 * g;
@@ -594,9 +682,10 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
     // dh: what is written is dg and du.  What they ask for is read B pieces ahead of the
     // stores.
     auto grads = [&](auto whole) {
-      constexpr bool UP = GRAD == 2, WHOLE = decltype(whole)::value;
-      constexpr int P = R * C, B = WHOLE && P >= 4 ? 4 : 1;
-      static_assert(P % B == 0);
+      // (whole rows: dg and du take the sums' place, and are written as above)
+      constexpr bool UP = GRAD == 2, WHOLE = decltype(whole)::value, Turn = WHOLE && WK == 1;
+      constexpr int Count = R * C, B = WHOLE && Count >= 4 ? 4 : 1;
+      static_assert(Count % B == 0);
       const auto m_of = [&](int p) { return m0 + piece_row(p % R) + 4 * g; };
       const auto n_of = [&](int p) { return n0 + wn * (BN / WN) + p / R * 16 + r; };
       GatedPiece now[B], next[B];
@@ -607,14 +696,27 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
       };
       read(0, now);
 #pragma unroll
-      for (int p = 0; p < P; p += B) {
-        if (p + B < P) read(p + B, next);
+      for (int p = 0; p < Count; p += B) {
+        if (p + B < Count) read(p + B, next);
 #pragma unroll
         for (int j = 0; j < B; ++j) {
           const int n = n_of(p + j), m = m_of(p + j);
-          if (n < a.N && m < a.ldc) put_gated_grad<UP>(a, n, m, acc[(p + j) % R][(p + j) / R], now[j]);
+          f32x4& dh = acc[(p + j) % R][(p + j) / R];
+          if constexpr (Turn)
+            dh = __builtin_bit_cast(f32x4, gated_grads(a, m, dh, now[j]));
+          else if (n < a.N && m < a.ldc)
+            put_gated_grad<UP>(a, n, m, dh, now[j]);
           now[j] = next[j];
         }
+      }
+      if constexpr (Turn) {
+        __syncthreads();
+        auto half = [&](int i, int t, int of) {
+          const u32x4 v = __builtin_bit_cast(u32x4, acc[i][t]);
+          return of ? u32x2{v.z, v.w} : u32x2{v.x, v.y};
+        };
+        turned(Two{}, a.c[0], a.ldc, a.ldc, [&](int i, int t) { return half(i, t, 0); });
+        if constexpr (UP) turned(Two{}, a.du, a.ldc, a.ldc, [&](int i, int t) { return half(i, t, 1); });
       }
     };
     if ((a.M & 3) == 0)
@@ -626,21 +728,14 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
 #pragma unroll
   for (int t = 0; t < C; ++t)
 #pragma unroll
-    for (int i = 0; i < R / MATS; ++i) {  // i inside: a row's pieces lie side by side
-      f32x4 v = acc[i][t];
+    for (int i = 0; i < RM; ++i) {
       if constexpr (MATS == 2) {
-        const f32x4 u = acc[i + R / 2][t];
         if (a.g) {
-          put(a.g, kF32, i, t, v);
-          put(a.u, kF32, i, t, u);
+          put(a.g, kF32, i, t, acc[i][t]);
+          put(a.u, kF32, i, t, acc[i + R / 2][t]);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = relu(v[e]) * u[e];
-      } else if (a.relu) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = relu(v[e]);
       }
-      put(a.c[batch], a.c_dtype, i, t, v);
+      put(a.c[batch], a.c_dtype, i, t, output(i, t));
     }
 #endif
 }
