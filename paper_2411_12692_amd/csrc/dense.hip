@@ -211,7 +211,8 @@ struct Plan {
 // before and behind them, and the second launch that joins parts.  The times are
 // kDenseTiles' and those of the join, fitted to 438 products of random sizes (5 to 6000
 // tokens, 64 to 16384 rows, sums of 64 to 8192, every tile and split timed): the tile
-// taken is 2% slower than the best one on average.  Up to 4 tokens W's rows go
+// taken is 2 to 3% slower than the best one on average (over 419 others 3.0%, with times
+// fitted to those 2.3%).  Up to 4 tokens W's rows go
 // through dense_few.hip (gate and up of 11008 x 4096, one token: 35.1 us in tiles, 27.7).
 Plan plan_of(int M, int N, long K, int mats, int batches, int es, bool b_rows, bool few) {
   if (few && N <= kFewTokens) return {kDenseFew, 1, 0};

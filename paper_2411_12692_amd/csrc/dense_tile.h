@@ -21,10 +21,10 @@
 // loads, 16 x 16 x 32 products of random bf16 values run at 1980 TFLOP/s (of zeros at
 // 2430).  A wave's 64 x 128 values (256 x 256 a block, 128 sums a lane) take 24 reads of
 // LDS for 64 products; its requests, 64 of 1 KiB a block and stage, cost the address unit
-// 16 cycles each and are the next limit.  Measured at 8192^3, random values: x W^T 1260,
-// dy W 1290, dy^T x 1320, gate and up without their sums 1405 TFLOP/s, no conflicts in
-// LDS; e4m3, 13824 x 5120 and 4096 tokens, 1900 (2150 of zeros, 3050 of zeros without the
-// loads).  Small tiles are for few tokens, where W's bytes bound: 13824 x 5120 gate and
+// 16 cycles each and are the next limit.  Measured at 8192^3, random values, after short
+// and long load of the card: x W^T 1310-1150, dy W 1390-1150, dy^T x 1410-1330, gate and
+// up without their sums 1430-1360 TFLOP/s, no conflicts in LDS; e4m3 2350-2250, and 2000
+// at 13824 x 5120 and 4096 tokens (2270 of zeros).  Small tiles are for few tokens, where W's bytes bound: 13824 x 5120 gate and
 // up, 37 tokens, 56 us, 5.1 TB/s of W.
 #pragma once
 
@@ -554,7 +554,8 @@ __global__ __launch_bounds__(WM* WN* WK* kWave) void k_dense(DenseArgs a) {
   // Whole rows of 16-byte pieces are written by way of LDS (WK = 1: its stages are done
   // with): a lane holds 8 or 16 bytes of each of many rows, and stores of it would be
   // pieces of 32 or 64 bytes, each a write of the L2 of its own.  Turned, 16 bytes a lane,
-  // they are as much of a row as the wave has.  value(i, t): 4 values from m = 4 g on of
+  // they are as much of a row as the wave has (weight gradient of 4096 x 16384, 777
+  // tokens: 151 -> 108 us; e4m3, 16384 x 8192, 4096 tokens: 576 -> 510).  value(i, t): 4 values from m = 4 g on of
   // piece i for n = r of piece t, as they are stored.
   constexpr int RM = R / MATS;
   auto turned = [&](auto bytes, void* y, size_t row_len, int m_end, auto value) {
