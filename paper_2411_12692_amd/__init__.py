@@ -908,7 +908,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, transposed: bool = False, out_dtype
     y = _linear_forward(x2, m, n, ld, w, rows, bool(transposed), out_dtype)
     if _wants_grad(x, w):
         graph, stream = _graph(y)
-        graph.linear(y, x2, w, m, n, ld, rows, bool(transposed), stream)
+        graph.linear(y, x2, w, m, n, rows, bool(transposed), stream)
     return y if x.dim() == 2 else y.view(*x.shape[:-1], rows)
 
 
@@ -944,7 +944,7 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor = Non
     h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, keep)
     if keep:
         graph, stream = _graph(h)
-        graph.gated_linear(h, x2, w_gate, w_up, g, u, m, n, ld, rows, stream)
+        graph.gated_linear(h, x2, w_gate, w_up, g, u, m, n, rows, stream)
     return h if x.dim() == 2 else h.view(*x.shape[:-1], rows)
 
 
@@ -967,7 +967,7 @@ def mlp(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch
     y = _linear_forward(h, m, rows, rows, w_down, n, False, out_dtype)
     if keep:
         graph, stream = _graph(y)
-        graph.mlp(y, x2, w_gate, w_up, w_down, h, g, u, m, n, ld, rows, stream)
+        graph.mlp(y, x2, w_gate, w_up, w_down, h, g, u, m, n, rows, stream)
     return y if x.dim() == 2 else y.view(x.shape)
 
 
@@ -1001,7 +1001,7 @@ def _norm(x, w, b, eps, center):
     y, mean, rstd = _norm_forward(x2, tokens, d, ld, w, b, center, float(eps), keep)
     if keep:
         graph, stream = _graph(y)
-        graph.norm(y, x2, w, b, mean, rstd, tokens, d, ld, center, stream)
+        graph.norm(y, x2, w, b, mean, rstd, tokens, d, center, stream)
     return y if x.dim() == 2 else y.view(x.shape)
 
 

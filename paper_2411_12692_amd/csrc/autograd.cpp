@@ -23,8 +23,15 @@ using torch::autograd::Node;
 using torch::autograd::SavedVariable;
 using torch::autograd::variable_list;
 
+// fp16 also as the bit patterns of int16
 int type_of(const Tensor& t) {
-  return t.scalar_type() == at::kFloat ? SI_F32 : t.scalar_type() == at::kBFloat16 ? SI_BF16 : SI_F16;
+  switch (t.scalar_type()) {
+    case at::kFloat: return SI_F32;
+    case at::kBFloat16: return SI_BF16;
+    case at::kHalf:
+    case at::kShort: return SI_F16;
+    default: TORCH_CHECK(false, "a tensor of ", t.scalar_type(), " in the backward pass");
+  }
 }
 void* ptr(const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 float* floats(const Tensor& t) { return static_cast<float*>(ptr(t)); }
@@ -35,26 +42,27 @@ Tensor scratch(const Tensor& like, size_t bytes) {
   return bytes ? at::empty({(int64_t)bytes}, like.options().dtype(at::kByte)) : Tensor();
 }
 
-// A gradient as rows of n values; those that are handed on expanded or transposed are
-// copied.
+// Rows of n values, `ld` elements from row to row.
 struct Rows {
   Tensor t;
   size_t ld;
 };
-Rows rows_of(const Tensor& grad, int64_t n) {
-  Tensor t = grad.dim() == 2 ? grad : grad.reshape({-1, n});
+constexpr int64_t kMaxLd = (int64_t)1 << 21, kMaxNormLd = (int64_t)1 << 32;  // the library's longest strides
+// t [rows][n] as it lies in memory; expanded, transposed or overlapping rows are copied.
+Rows rows_of(Tensor t, int64_t n, int64_t max_ld) {
   const bool many = t.size(0) > 1;
-  if (!t.is_contiguous() && ((n > 1 && t.stride(1) != 1) || (many && (t.stride(0) < n || t.stride(0) > 1 << 21))))
+  if (!t.is_contiguous() && ((n > 1 && t.stride(1) != 1) || (many && (t.stride(0) < n || t.stride(0) > max_ld))))
     t = t.contiguous();
   return {t, (size_t)(many && !t.is_contiguous() ? t.stride(0) : n)};
 }
 
-// One call of a differentiable operator: its saved tensors and sizes, m rows of n (of
-// stride ld) to m rows of `rows`.
+// One call of a differentiable operator: its saved tensors and sizes, m rows of n to m
+// rows of `rows`.
 struct Call : Node {
   SavedVariable x, w, w_up, w_down, g, u, h;  // (norms: w, and the rows' mean and r as g, u)
-  int m = 0, n = 0, rows = 0;
-  size_t ld = 0;
+  int64_t m = 0, n = 0, rows = 0;
+  int x_type = 0, w_type = 0, y_type = 0;
+  c10::Device device{at::kCPU};
   bool flag = false;  // W^T in memory, or LayerNorm
   void* stream = nullptr;
 
@@ -62,8 +70,27 @@ struct Call : Node {
     for (SavedVariable* v : {&x, &w, &w_up, &w_down, &g, &u, &h}) v->reset_data();
   }
 
+  // A saved tensor as it is handed back.  Hooks of saved tensors choose its place and
+  // strides (save_on_cpu makes a slice contiguous), so both are taken from this tensor,
+  // never from the forward call; another type, size or device is refused.
+  Tensor kept(const Tensor& t, const char* name, int type, at::IntArrayRef sizes) const {
+    TORCH_CHECK(t.defined(), "the saved tensor ", name, " was handed back undefined");
+    TORCH_CHECK(t.device() == device, "the saved tensor ", name, " was handed back on ", t.device(), ", not ", device);
+    TORCH_CHECK(t.sizes() == sizes, "the saved tensor ", name, " was handed back as ", t.sizes(), ", not ", sizes);
+    TORCH_CHECK(t.layout() == at::kStrided && type_of(t) == type, "the saved tensor ", name, " was handed back as ",
+                t.scalar_type(), ", another type than it had");
+    return t;
+  }
+  Rows x_rows(int64_t max_ld = kMaxLd) const { return rows_of(kept(x.unpack(), "x", x_type, {m, n}), n, max_ld); }
+  Tensor whole(const Tensor& t, const char* name, int type, at::IntArrayRef sizes) const {
+    return kept(t, name, type, sizes).contiguous();
+  }
+  Tensor whole_if(const Tensor& t, const char* name, int type, at::IntArrayRef sizes) const {
+    return t.defined() ? whole(t, name, type, sizes) : t;
+  }
+
   // the gradients that are asked for
-  virtual void run(const Tensor& grad, const Tensor& x, const Tensor& w, variable_list& out) = 0;
+  virtual void run(const Tensor& grad, variable_list& out) = 0;
 
   variable_list apply(variable_list&& in) override {
     std::lock_guard<std::mutex> lock(mutex_);
@@ -72,9 +99,8 @@ struct Call : Node {
     if (!in[0].defined()) return out;
     {
       at::NoGradGuard none;
-      const Tensor xt = x.unpack(), wt = w.unpack();
-      const c10::DeviceGuard guard(xt.device());
-      run(in[0], xt, wt, out);
+      const c10::DeviceGuard guard(device);
+      run(in[0], out);
     }
     if (!graph) return out;
     // the gradients have none of their own: a graph of them is refused where it is used
@@ -97,27 +123,34 @@ Tensor operand(const Tensor& grad, const Tensor& xt) {
 
 struct LinearGrad : Call {
   std::string name() const override { return "SparseInferLinearGrad"; }
-  void run(const Tensor& grad, const Tensor& xt, const Tensor& wt, variable_list& out) override {
-    const Rows dy = rows_of(operand(grad, xt), rows);
+  void run(const Tensor& grad, variable_list& out) override {
+    const Rows xr = x_rows();
+    const Tensor &xt = xr.t, wt = flag ? whole(w.unpack(), "w", w_type, {n, rows}) : whole(w.unpack(), "w", w_type, {rows, n});
+    const Rows dy = rows_of(operand(grad, xt), rows, kMaxLd);
     out = {dx_of(xt), like(wants(1), wt)};
-    const size_t bytes = si_linear_backward_workspace_bytes(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), ld, m, n, ptr(wt), rows,
-                                                            flag, out[0].defined(), out[1].defined());
+    const size_t bytes = si_linear_backward_workspace_bytes(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), xr.ld, m, n, ptr(wt),
+                                                            rows, flag, out[0].defined(), out[1].defined());
     const Tensor ws = scratch(xt, bytes);
-    check(si_linear_backward(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), type_of(xt), ld, m, n, ptr(wt), rows, flag, ptr(out[0]),
+    check(si_linear_backward(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), x_type, xr.ld, m, n, ptr(wt), rows, flag, ptr(out[0]),
                              ptr(out[1]), ptr(ws), bytes, stream));
   }
 };
 
 struct GatedGrad : Call {
   std::string name() const override { return "SparseInferGatedLinearGrad"; }
-  void run(const Tensor& grad, const Tensor& xt, const Tensor& wt, variable_list& out) override {
-    const Tensor up = w_up.unpack(), ut = u.unpack(), gt = up.defined() ? g.unpack() : h.unpack(shared_from_this());
-    const Rows dh = rows_of(grad, rows);
+  void run(const Tensor& grad, variable_list& out) override {
+    const Rows xr = x_rows();
+    const Tensor &xt = xr.t, wt = whole(w.unpack(), "w_gate", w_type, {rows, n}),
+                 up = whole_if(w_up.unpack(), "w_up", w_type, {rows, n});
+    const Tensor ut = up.defined() ? whole(u.unpack(), "u", SI_F32, {m, rows}) : Tensor();
+    const Tensor gt = up.defined() ? whole(g.unpack(), "g", SI_F32, {m, rows})
+                                   : whole(h.unpack(shared_from_this()), "h", y_type, {m, rows});
+    const Rows dh = rows_of(grad, rows, kMaxLd);
     out = {dx_of(xt), like(wants(1), wt), like(wants(2), up)};
-    const size_t bytes = si_gated_linear_backward_workspace_bytes(ptr(xt), ld, m, n, ptr(wt), ptr(up), rows, out[0].defined(),
-                                                                  out[1].defined() || out[2].defined());
+    const size_t bytes = si_gated_linear_backward_workspace_bytes(ptr(xt), xr.ld, m, n, ptr(wt), ptr(up), rows,
+                                                                  out[0].defined(), out[1].defined() || out[2].defined());
     const Tensor ws = scratch(xt, bytes);
-    check(si_gated_linear_backward(ptr(dh.t), type_of(dh.t), dh.ld, ptr(gt), type_of(gt), floats(ut), ptr(xt), type_of(xt), ld,
+    check(si_gated_linear_backward(ptr(dh.t), type_of(dh.t), dh.ld, ptr(gt), type_of(gt), floats(ut), ptr(xt), x_type, xr.ld,
                                    m, n, ptr(wt), ptr(up), rows, ptr(out[0]), ptr(out[1]), ptr(out[2]), ptr(ws), bytes,
                                    stream));
   }
@@ -125,15 +158,20 @@ struct GatedGrad : Call {
 
 struct MlpGrad : Call {
   std::string name() const override { return "SparseInferMlpGrad"; }
-  void run(const Tensor& grad, const Tensor& xt, const Tensor& wt, variable_list& out) override {
-    const Tensor up = w_up.unpack(), down = w_down.unpack(), gt = g.unpack(), ut = u.unpack(), ht = h.unpack();
-    const Rows dy = rows_of(operand(grad, xt), n);
+  void run(const Tensor& grad, variable_list& out) override {
+    const Rows xr = x_rows();
+    const Tensor &xt = xr.t, wt = whole(w.unpack(), "w_gate", w_type, {rows, n}),
+                 up = whole_if(w_up.unpack(), "w_up", w_type, {rows, n}),
+                 down = whole(w_down.unpack(), "w_down", w_type, {n, rows}), ht = whole(h.unpack(), "h", x_type, {m, rows});
+    const Tensor gt = up.defined() ? whole(g.unpack(), "g", SI_F32, {m, rows}) : Tensor(),
+                 ut = up.defined() ? whole(u.unpack(), "u", SI_F32, {m, rows}) : Tensor();
+    const Rows dy = rows_of(operand(grad, xt), n, kMaxLd);
     out = {dx_of(xt), like(wants(1), wt), like(wants(2), up), like(wants(3), down)};
-    const size_t bytes = si_mlp_backward_workspace_bytes(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), ld, m, n, ptr(wt), ptr(up),
-                                                         ptr(down), rows, out[0].defined(),
+    const size_t bytes = si_mlp_backward_workspace_bytes(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), xr.ld, m, n, ptr(wt),
+                                                         ptr(up), ptr(down), rows, out[0].defined(),
                                                          out[1].defined() || out[2].defined(), out[3].defined());
     const Tensor ws = scratch(xt, bytes);
-    check(si_mlp_backward(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), type_of(xt), ld, m, n, ptr(wt), ptr(up), ptr(down), rows,
+    check(si_mlp_backward(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), x_type, xr.ld, m, n, ptr(wt), ptr(up), ptr(down), rows,
                           ptr(ht), floats(gt), floats(ut), ptr(out[0]), ptr(out[1]), ptr(out[2]), ptr(out[3]), ptr(ws), bytes,
                           stream));
   }
@@ -141,13 +179,15 @@ struct MlpGrad : Call {
 
 struct NormGrad : Call {
   std::string name() const override { return flag ? "SparseInferLayerNormGrad" : "SparseInferRmsNormGrad"; }
-  void run(const Tensor& grad, const Tensor& xt, const Tensor& wt, variable_list& out) override {
-    const Tensor mean = g.unpack(), r = u.unpack();
-    const Rows dy = rows_of(grad, n);
+  void run(const Tensor& grad, variable_list& out) override {
+    const Rows xr = x_rows(kMaxNormLd);
+    const Tensor &xt = xr.t, wt = whole(w.unpack(), "w", w_type, {n}), r = whole(u.unpack(), "r", SI_F32, {m});
+    const Tensor mean = flag ? whole(g.unpack(), "mean", SI_F32, {m}) : Tensor();
+    const Rows dy = rows_of(grad, n, kMaxNormLd);
     out = {dx_of(xt), like(wants(1), wt), like(wants(2), wt)};
     const size_t bytes = out[1].defined() || out[2].defined() ? si_layer_norm_backward_workspace_bytes(m, n) : 0;
     const Tensor ws = scratch(xt, bytes);
-    check(si_layer_norm_backward(ptr(dy.t), dy.ld, ptr(xt), type_of(xt), ld, ptr(wt), type_of(wt), flag, floats(mean), floats(r),
+    check(si_layer_norm_backward(ptr(dy.t), dy.ld, ptr(xt), x_type, xr.ld, ptr(wt), w_type, flag, floats(mean), floats(r),
                                  ptr(out[0]), ptr(out[1]), ptr(out[2]), m, n, ptr(ws), bytes, stream));
   }
 };
@@ -173,7 +213,7 @@ void refuse_foreign_leaf(const Tensor& t) {
 
 // The node of a call that has been made, and y as its output.
 template <class T, class... Inputs>  // (Inputs: tensors)
-std::shared_ptr<T> attach(Tensor y, int m, int n, size_t ld, int rows, bool flag, uintptr_t stream, const Tensor& x,
+std::shared_ptr<T> attach(Tensor y, int m, int n, int rows, bool flag, uintptr_t stream, const Tensor& x,
                           const Tensor& w, const Inputs&... more) {
   for (const Tensor* t : {&x, &w, &more...}) refuse_foreign_leaf(*t);
   auto call = std::shared_ptr<T>(new T(), torch::autograd::deleteNode);
@@ -183,21 +223,24 @@ std::shared_ptr<T> attach(Tensor y, int m, int n, size_t ld, int rows, bool flag
   call->m = m;
   call->n = n;
   call->rows = rows;
-  call->ld = ld;
+  call->x_type = type_of(x);
+  call->w_type = type_of(w);
+  call->y_type = type_of(y);
+  call->device = x.device();
   call->flag = flag;
   call->stream = reinterpret_cast<void*>(stream);
   torch::autograd::set_history(y, call);
   return call;
 }
 
-void linear(const Tensor& y, const Tensor& x, const Tensor& w, int m, int n, size_t ld, int rows, bool transposed,
+void linear(const Tensor& y, const Tensor& x, const Tensor& w, int m, int n, int rows, bool transposed,
             uintptr_t stream) {
-  attach<LinearGrad>(y, m, n, ld, rows, transposed, stream, x, w);
+  attach<LinearGrad>(y, m, n, rows, transposed, stream, x, w);
 }
 
 void gated_linear(const Tensor& h, const Tensor& x, const Tensor& w_gate, const Maybe& w_up, const Maybe& g, const Maybe& u,
-                  int m, int n, size_t ld, int rows, uintptr_t stream) {
-  const auto c = attach<GatedGrad>(h, m, n, ld, rows, false, stream, x, w_gate, given(w_up));
+                  int m, int n, int rows, uintptr_t stream) {
+  const auto c = attach<GatedGrad>(h, m, n, rows, false, stream, x, w_gate, given(w_up));
   c->w_up = saved(w_up);
   c->g = saved(g);
   c->u = saved(u);
@@ -205,8 +248,8 @@ void gated_linear(const Tensor& h, const Tensor& x, const Tensor& w_gate, const 
 }
 
 void mlp(const Tensor& y, const Tensor& x, const Tensor& w_gate, const Maybe& w_up, const Tensor& w_down, const Tensor& h,
-         const Maybe& g, const Maybe& u, int m, int n, size_t ld, int rows, uintptr_t stream) {
-  const auto c = attach<MlpGrad>(y, m, n, ld, rows, false, stream, x, w_gate, given(w_up), w_down);
+         const Maybe& g, const Maybe& u, int m, int n, int rows, uintptr_t stream) {
+  const auto c = attach<MlpGrad>(y, m, n, rows, false, stream, x, w_gate, given(w_up), w_down);
   c->w_up = saved(w_up);
   c->w_down = SavedVariable(w_down, false);
   c->h = SavedVariable(h, false);
@@ -215,8 +258,8 @@ void mlp(const Tensor& y, const Tensor& x, const Tensor& w_gate, const Maybe& w_
 }
 
 void norm(const Tensor& y, const Tensor& x, const Tensor& w, const Maybe& b, const Maybe& mean, const Tensor& r, int tokens,
-          int d, size_t ld, bool center, uintptr_t stream) {
-  const auto c = attach<NormGrad>(y, tokens, d, ld, d, center, stream, x, w, given(b));
+          int d, bool center, uintptr_t stream) {
+  const auto c = attach<NormGrad>(y, tokens, d, d, center, stream, x, w, given(b));
   c->g = saved(mean);
   c->u = SavedVariable(r, false);
 }

@@ -1,0 +1,73 @@
+"""The differentiable operators as nodes of PyTorch's graph: what hooks, streams, empty
+batches and captures ask of them beyond the values of their gradients
+(``test_gpu_dense.py``, ``test_gpu_norm_train.py``)."""
+
+import pytest
+import torch
+
+import paper_2411_12692_amd as si
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F16, F32 = torch.float16, torch.float32
+M, N, K = 37, 96, 40
+
+
+def gen(*key):
+    g = torch.Generator()
+    g.manual_seed(hash(key) % (1 << 31))
+    return g
+
+
+def values(g, *shape, dtype=F16):
+    return torch.randn(*shape, generator=g).mul(0.3).to(dtype).to(DEV)
+
+
+def operators(g):
+    """Name, the call over x, its weights."""
+    w, wt, wg, wu, wd = (values(g, *s).requires_grad_() for s in ((K, N), (N, K), (K, N), (K, N), (N, K)))
+    nw, nb = values(g, N, dtype=F32).requires_grad_(), values(g, N, dtype=F32).requires_grad_()
+    return [("linear", lambda x: si.linear(x, w), (w,)),
+            ("linear, W^T", lambda x: si.linear(x, wt, transposed=True), (wt,)),
+            ("gated_linear", lambda x: si.gated_linear(x, wg, wu), (wg, wu)),
+            ("gated_linear, no W_up", lambda x: si.gated_linear(x, wg), (wg,)),
+            ("mlp", lambda x: si.mlp(x, wg, wu, wd), (wg, wu, wd)),
+            ("mlp, no W_up", lambda x: si.mlp(x, wg, None, wd), (wg, wd)),
+            ("layer_norm", lambda x: si.layer_norm(x, nw, nb), (nw, nb)),
+            ("rms_norm", lambda x: si.rms_norm(x, nw), (nw,))]
+
+
+NAMES = ["linear", "linear, W^T", "gated_linear", "gated_linear, no W_up", "mlp", "mlp, no W_up", "layer_norm", "rms_norm"]
+
+
+def pick(name, g):
+    return next((f, leaves) for n, f, leaves in operators(g) if n == name)
+
+
+class Wider(torch.autograd.graph.saved_tensors_hooks):
+    """Hands matrices back as column ranges of wider ones."""
+
+    def __init__(self):
+        def unpack(t):
+            return t if t.dim() != 2 else torch.nn.functional.pad(t, (16, 24))[:, 16:16 + t.shape[1]]
+        super().__init__(lambda t: t, unpack)
+
+
+@pytest.mark.parametrize("name", NAMES)
+@pytest.mark.parametrize("width", [304, 300])
+def test_slices_and_hooks_of_saved_tensors(name, width):
+    """x is a column range; hooks hand it back contiguous (``save_on_cpu``) or in rows of
+    yet another stride: the same gradients, bit for bit.  (A norm of rows that do not
+    start on 16 bytes adds in another order, and only those that do are compared.)"""
+    if "norm" in name and width % 8:
+        width += 8 - width % 8
+    f, leaves = pick(name, gen(1))
+    x = values(gen(2), M, width)[:, 8:8 + N].detach().requires_grad_()
+    assert x.stride(0) == width
+    dy = values(gen(3), *f(x).shape)
+    want = torch.autograd.grad(f(x), (x, *leaves), dy)
+    for hooks in (torch.autograd.graph.save_on_cpu, Wider):
+        with hooks():
+            y = f(x)
+        got = torch.autograd.grad(y, (x, *leaves), dy)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), hooks
