@@ -15,6 +15,7 @@ from __future__ import annotations
 import functools
 
 import torch
+import torch.autograd.forward_ad as _forward_ad
 
 from . import _lib
 from ._lib import SI_NO_AS, SI_NO_SPECULATION, SparseInferError
@@ -865,6 +866,13 @@ def _out_type(dtype, x):
 
 
 def _wants_grad(*tensors) -> bool:
+    """Whether a call has gradients to give.  A tangent (forward-mode
+    differentiation) would be lost in its output, and is refused."""
+    if getattr(_forward_ad, "_current_level", 0) >= 0:  # within a dual_level
+        for t in tensors:
+            if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+                raise NotImplementedError("this operator has gradients in reverse mode alone: a tensor with a tangent "
+                                          "(forward-mode differentiation) is not taken")
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
@@ -905,8 +913,9 @@ def linear(x: torch.Tensor, w: torch.Tensor, transposed: bool = False, out_dtype
     if shape[0 if transposed else 1] != n:
         raise ValueError(f"w {tuple(shape)} does not take rows of {n} values")
     out_dtype = _out_type(out_dtype, x)
+    keep = _wants_grad(x, w)
     y = _linear_forward(x2, m, n, ld, w, rows, bool(transposed), out_dtype)
-    if _wants_grad(x, w):
+    if keep:
         graph, stream = _graph(y)
         graph.linear(y, x2, w, m, n, rows, bool(transposed), stream)
     return y if x.dim() == 2 else y.view(*x.shape[:-1], rows)

@@ -10,7 +10,10 @@ import subprocess
 import sys
 
 import pytest
+import torch
+import torch.autograd.forward_ad as fwAD
 
+import paper_2411_12692_amd as si
 from paper_2411_12692_amd import build
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -231,3 +234,18 @@ def check(name):
     assert len(read) == len(back) and not {t.data_ptr() for t in back} & set(read.values()), c
     assert c["ldx"] == N
 ''')
+
+
+def test_tangents_are_refused():
+    """Forward-mode: outputs have no tangents, so inputs with one are not taken, with or
+    without reverse mode; inputs without one are, inside a ``dual_level`` too."""
+    x, w = torch.ones(2, 4), torch.ones(3, 4).requires_grad_()
+    with fwAD.dual_level():
+        dual = fwAD.make_dual(x, torch.ones_like(x))
+        for tensors in ((dual, None, w), (x, dual), (dual,)):
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                si._wants_grad(*tensors)
+            with torch.no_grad(), pytest.raises(NotImplementedError, match="forward-mode"):
+                si._wants_grad(*tensors)
+        assert si._wants_grad(x, None, w) and not si._wants_grad(x)
+    assert si._wants_grad(x, w) and not si._wants_grad(x)

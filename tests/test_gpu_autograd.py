@@ -4,6 +4,7 @@ batches and captures ask of them beyond the values of their gradients
 
 import pytest
 import torch
+import torch.autograd.forward_ad as fwAD
 
 import paper_2411_12692_amd as si
 
@@ -71,3 +72,33 @@ def test_slices_and_hooks_of_saved_tensors(name, width):
             y = f(x)
         got = torch.autograd.grad(y, (x, *leaves), dy)
         assert all(torch.equal(a, b) for a, b in zip(got, want)), hooks
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_tangents_are_refused(name):
+    """A tensor with a tangent: every operand is looked at, with and without reverse mode.
+    Inside a ``dual_level`` tensors without one are taken."""
+    f, leaves = pick(name, gen(4))
+    x = values(gen(5), M, N)
+    want = f(x)
+    with fwAD.dual_level():
+        assert torch.equal(f(x), want)
+        dual = fwAD.make_dual(x, torch.ones_like(x))
+        for call in (lambda: f(dual), lambda: f(dual.view(1, M, N))):
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                call()
+            with torch.no_grad(), pytest.raises(NotImplementedError, match="forward-mode"):
+                call()
+
+
+def test_tangents_of_weights_are_refused():
+    g = gen(6)
+    x, w, wt, nw = values(g, M, N), values(g, K, N), values(g, N, K), values(g, N, dtype=F32)
+    with fwAD.dual_level():
+        d, dt, dn = (fwAD.make_dual(t, torch.ones_like(t)) for t in (w, wt, nw))
+        for call in (lambda: si.linear(x, d), lambda: si.gated_linear(x, d, w), lambda: si.gated_linear(x, w, d),
+                     lambda: si.gated_linear(x, d), lambda: si.mlp(x, d, w, wt), lambda: si.mlp(x, w, d, wt),
+                     lambda: si.mlp(x, w, w, dt), lambda: si.mlp(x, w, None, dt), lambda: si.layer_norm(x, dn, nw),
+                     lambda: si.layer_norm(x, nw, dn), lambda: si.rms_norm(x, dn)):
+            with pytest.raises(NotImplementedError, match="forward-mode"):
+                call()
