@@ -603,7 +603,8 @@ si_status si_gated_linear(const void* x, int dtype, size_t ldx, int m, int n, co
  *   h   : [m][k] of type dtype, si_gated_linear's output.
  *   g, u and h on 16 bytes.
  *   dx, dw, dw_gate, dw_up, dw_down: [m][n] and the weights' shapes, of type dtype,
- *         written; each may be NULL.  With m = 0 the weights' gradients are zeros.
+ *         written; each may be NULL (all of them with m = 0 alone).  With m = 0 the
+ *         weights' gradients are zeros.
  *   workspace: ..._workspace_bytes() of the call; want_dx, want_dw (of either of w_gate
  *         and w_up) and want_dw_down say which of the gradients are not NULL.
  */
@@ -701,7 +702,8 @@ size_t si_linear_fp8_workspace_bytes(int m, int rows, int n, int gated);
  *   w, b    : [d] of type w_dtype, as dw and db; b may be NULL.
  *   mean, rstd : [tokens] float32, the means and r of the rows, written by the forward
  *             pass where given (mean with center alone), read by the backward pass.
- *   dx, dw, db : written; each may be NULL.  With tokens = 0 dw and db are zeros.
+ *   dx, dw, db : written; each may be NULL (all of them with tokens = 0 alone).  With
+ *             tokens = 0 dw and db are zeros.
  *   tokens 0 to 2^23 - 1, d 1 to 16384, addresses that fit an element.
  *   workspace: si_layer_norm_backward_workspace_bytes(), where dw or db is given.
  * The gradients' sums are taken in an order that depends on the sizes alone.

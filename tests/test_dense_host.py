@@ -289,6 +289,20 @@ def test_nothing_to_do():
         assert _lib.status(*call) == _lib.SI_OK, (call[0], _lib.last_error())
 
 
+def test_no_tokens_and_no_gradient_of_a_weight():
+    """The gradient with respect to x of no tokens has no address: with that alone asked
+    for there is nothing to do, where with tokens it is a call without a gradient."""
+    for call in (lambda m: backward(m=m, dx=None, dw=None), lambda m: backward(m=m, dx=None, dw=None, t=1),
+                 lambda m: gated_backward(m=m, dx=None, dwg=None, dwu=None),
+                 lambda m: mlp_backward(m=m, dx=None, dwg=None, dwu=None, dwd=None),
+                 lambda m: norm_backward(tokens=m, dx=None, dw=None, db=None),
+                 lambda m: norm_backward(tokens=m, dx=None, dw=None, db=None, center=0)):
+        assert _lib.status(*call(0)) == _lib.SI_OK, (call(0)[0], _lib.last_error())
+        refused(_lib.SI_ERR_NULL, *call(3))
+    refused(_lib.SI_ERR_SHAPE, *backward(m=-1, dx=None, dw=None))
+    refused(_lib.SI_ERR_ALIGN, *backward(m=0, dx=None, dw=None, w=C + 1))
+
+
 def test_python_refuses_before_a_device_is_needed():
     x, w = torch.zeros(2, 8, dtype=torch.float16), torch.zeros(4, 8, dtype=torch.float16)
     for f in (lambda: si.linear(x, w), lambda: si.gated_linear(x, w, w), lambda: si.mlp(x, w, w, w.t()),

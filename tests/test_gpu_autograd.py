@@ -102,3 +102,23 @@ def test_tangents_of_weights_are_refused():
                      lambda: si.layer_norm(x, nw, dn), lambda: si.rms_norm(x, dn)):
             with pytest.raises(NotImplementedError, match="forward-mode"):
                 call()
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_no_tokens_and_frozen_weights(name):
+    """The gradient with respect to x alone, of no tokens: asked for alone, or with
+    weights that have none."""
+    f, leaves = pick(name, gen(7))
+    for shape in ((0, N), (2, 0, N)):
+        x = torch.zeros(shape, dtype=F16, device=DEV).requires_grad_()
+        y = f(x)
+        (dx,) = torch.autograd.grad(y, x, torch.zeros_like(y))
+        assert dx.shape == x.shape and dx.dtype == F16
+        for t in leaves:
+            t.requires_grad_(False)
+        f(x).float().sum().backward()
+        assert x.grad.shape == x.shape
+        for t in leaves:
+            t.requires_grad_(True)
+        dw = torch.autograd.grad(f(x), leaves, torch.zeros_like(y))
+        assert all(torch.equal(d, torch.zeros_like(t)) for d, t in zip(dw, leaves))
