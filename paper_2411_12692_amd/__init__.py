@@ -889,14 +889,16 @@ def _linear_forward(x2, m, n, ld, w, rows, transposed, out_dtype):
 _nodes = None
 
 
-def _graph(y):
-    """The module that places a call with output ``y`` in autograd's graph
+def _graph(y, x):
+    """The module that places a call of ``x`` with output ``y`` in autograd's graph
     (``csrc/autograd.cpp``), and the stream of the call."""
     global _nodes
     if _nodes is None:
         _nodes = _lib.autograd()
     if y.dtype == torch.int16:
         raise TypeError("an output of int16 (fp16 bits) has no gradient: ask for another out_dtype")
+    if x.dim() != 2:  # its rows, which the node is given, may be a copy
+        _nodes.refuse_foreign_leaf(x)
     index = y.get_device()
     if _raw_stream is not None:
         return _nodes, _raw_stream(index)
@@ -916,7 +918,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, transposed: bool = False, out_dtype
     keep = _wants_grad(x, w)
     y = _linear_forward(x2, m, n, ld, w, rows, bool(transposed), out_dtype)
     if keep:
-        graph, stream = _graph(y)
+        graph, stream = _graph(y, x)
         graph.linear(y, x2, w, m, n, rows, bool(transposed), stream)
     return y if x.dim() == 2 else y.view(*x.shape[:-1], rows)
 
@@ -952,7 +954,7 @@ def gated_linear(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor = Non
     keep = _wants_grad(x, w_gate, w_up)
     h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, out_dtype, keep)
     if keep:
-        graph, stream = _graph(h)
+        graph, stream = _graph(h, x)
         graph.gated_linear(h, x2, w_gate, w_up, g, u, m, n, rows, stream)
     return h if x.dim() == 2 else h.view(*x.shape[:-1], rows)
 
@@ -975,7 +977,7 @@ def mlp(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch
     h, g, u = _gated_forward(x2, m, n, ld, w_gate, w_up, rows, x2.dtype, keep)
     y = _linear_forward(h, m, rows, rows, w_down, n, False, out_dtype)
     if keep:
-        graph, stream = _graph(y)
+        graph, stream = _graph(y, x)
         graph.mlp(y, x2, w_gate, w_up, w_down, h, g, u, m, n, rows, stream)
     return y if x.dim() == 2 else y.view(x.shape)
 
@@ -1009,7 +1011,7 @@ def _norm(x, w, b, eps, center):
     keep = _wants_grad(x, w, b)
     y, mean, rstd = _norm_forward(x2, tokens, d, ld, w, b, center, float(eps), keep)
     if keep:
-        graph, stream = _graph(y)
+        graph, stream = _graph(y, x)
         graph.norm(y, x2, w, b, mean, rstd, tokens, d, center, stream)
     return y if x.dim() == 2 else y.view(x.shape)
 

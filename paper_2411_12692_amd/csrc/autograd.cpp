@@ -200,10 +200,13 @@ SavedVariable saved(const Maybe& t, bool output = false) {
 
 // While an eager graph of a leaf lives, the leaf's place for gradients belongs to that
 // graph's stream, and a backward pass captured on another one would end the capture, and
-// the process, where autograd lets the two streams wait for each other.
+// the process, where autograd lets the two streams wait for each other.  A view (the rows
+// of a leaf of more dimensions, a slice of one) hands its gradients to its base.
 void refuse_foreign_leaf(const Tensor& t) {
-  if (!t.defined() || !t.requires_grad() || !t.is_leaf()) return;
-  const auto place = torch::autograd::impl::try_get_grad_accumulator(t);
+  if (!t.defined() || !t.requires_grad()) return;
+  const at::TensorBase& leaf = !t.is_leaf() && t.is_view() ? t._base() : t;
+  if (!leaf.requires_grad() || !leaf.is_leaf()) return;
+  const auto place = torch::autograd::impl::try_get_grad_accumulator(leaf);
   if (!place || !place->stream().has_value()) return;
   if (*place->stream() == c10::impl::VirtualGuardImpl(t.device().type()).getStream(t.device())) return;
   TORCH_CHECK(!py::module_::import("torch.cuda").attr("is_current_stream_capturing")().cast<bool>(),
@@ -267,6 +270,7 @@ void norm(const Tensor& y, const Tensor& x, const Tensor& w, const Maybe& b, con
 }  // namespace
 
 PYBIND11_MODULE(_autograd, module) {
+  module.def("refuse_foreign_leaf", &refuse_foreign_leaf);
   module.def("linear", &linear);
   module.def("gated_linear", &gated_linear);
   module.def("mlp", &mlp);

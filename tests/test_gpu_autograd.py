@@ -122,3 +122,61 @@ def test_no_tokens_and_frozen_weights(name):
             t.requires_grad_(True)
         dw = torch.autograd.grad(f(x), leaves, torch.zeros_like(y))
         assert all(torch.equal(d, torch.zeros_like(t)) for d, t in zip(dw, leaves))
+
+
+def leaf_cases():
+    """What of a leaf a call is given: the leaf itself is another test's."""
+    return [("3-D", (3, 13, N), lambda t: t), ("3-D, copied rows", (13, 3, N), lambda t: t.transpose(0, 1)),
+            ("slice", (M, 304), lambda t: t[:, 8:8 + N]), ("slice of 3-D", (4, 13, N), lambda t: t[1:]),
+            ("one row", (N,), lambda t: t)]
+
+
+@pytest.mark.parametrize("case", range(5))
+def test_capture_with_views_of_a_leaf_of_a_live_graph_is_refused(case):
+    """The refusal comes in the forward call, before any captured backward pass.  Once the
+    eager graph is gone the same capture goes through."""
+    kind, shape, part = leaf_cases()[case]
+    x = values(gen(8), *shape).requires_grad_()
+    for name in NAMES:
+        f, leaves = pick(name, gen(9))
+        for t in leaves:
+            t.requires_grad_(False)
+        alive = f(part(x))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with pytest.raises(RuntimeError, match="eager graph"):
+            with torch.cuda.graph(graph):
+                f(part(x))
+        torch.cuda.synchronize()
+        ones = torch.ones_like(alive)
+        want = torch.autograd.grad(alive, x, ones)[0]
+        del alive, graph
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            y = f(part(x))
+            got = torch.autograd.grad(y, x, ones)[0]
+        del y
+        for _ in range(3):
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(got, want), (kind, name)
+
+
+def test_capture_with_weights_that_are_views_of_a_leaf_of_a_live_graph_is_refused():
+    g = gen(10)
+    both = values(g, 2 * K, N).requires_grad_()  # W_gate over W_up
+    down, norm = values(g, N, 2 * K).requires_grad_(), values(g, 2, N, dtype=F32).requires_grad_()
+    x, w, wt = values(g, M, N), values(g, K, N), values(g, N, K)
+    for f, leaf in ((lambda: si.linear(x, both[K:]), both), (lambda: si.gated_linear(x, both[:K], w), both),
+                    (lambda: si.gated_linear(x, w, both[K:]), both), (lambda: si.mlp(x, w, both[:K], wt), both),
+                    (lambda: si.mlp(x, w, w, down.view(2, N, K)[1]), down), (lambda: si.layer_norm(x, norm[0], norm[1]), norm),
+                    (lambda: si.layer_norm(x, norm[0].detach(), norm[1]), norm), (lambda: si.rms_norm(x, norm[0]), norm)):
+        alive = f()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with pytest.raises(RuntimeError, match="eager graph"):
+            with torch.cuda.graph(graph):
+                f()
+        torch.cuda.synchronize()
+        assert torch.autograd.grad(alive, leaf, torch.ones_like(alive))[0].shape == leaf.shape
+        del alive, graph
