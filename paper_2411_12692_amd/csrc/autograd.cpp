@@ -64,6 +64,7 @@ struct Call : Node {
   int x_type = 0, w_type = 0, y_type = 0;
   c10::Device device{at::kCPU};
   bool flag = false;  // W^T in memory, or LayerNorm
+  at::ScalarType y_scalar = at::kFloat;
   void* stream = nullptr;
 
   void release_variables() override {
@@ -92,6 +93,17 @@ struct Call : Node {
   // the gradients that are asked for
   virtual void run(const Tensor& grad, variable_list& out) = 0;
 
+  // The gradient of y.  Autograd hands on one of y's size, type and device; the node's own
+  // call and its hooks are held to that here.
+  Tensor gradient(const Tensor& grad) const {
+    TORCH_CHECK(grad.device() == device && grad.layout() == at::kStrided, "a gradient on ", grad.device(), ", not ", device);
+    TORCH_CHECK(grad.dim() == 2 && grad.size(0) == m && grad.size(1) == y_n(), "a gradient of size ", grad.sizes(), ", not [", m,
+                ", ", y_n(), "]");
+    return grad.to(y_scalar);
+  }
+
+  virtual int64_t y_n() const { return rows; }  // values of a row of y
+
   variable_list apply(variable_list&& in) override {
     std::lock_guard<std::mutex> lock(mutex_);
     const bool graph = at::GradMode::is_enabled();
@@ -100,7 +112,7 @@ struct Call : Node {
     {
       at::NoGradGuard none;
       const c10::DeviceGuard guard(device);
-      run(in[0], out);
+      run(gradient(in[0]), out);
     }
     if (!graph) return out;
     // the gradients have none of their own: a graph of them is refused where it is used
@@ -157,6 +169,7 @@ struct GatedGrad : Call {
 };
 
 struct MlpGrad : Call {
+  int64_t y_n() const override { return n; }
   std::string name() const override { return "SparseInferMlpGrad"; }
   void run(const Tensor& grad, variable_list& out) override {
     const Rows xr = x_rows();
@@ -231,6 +244,7 @@ std::shared_ptr<T> attach(Tensor y, int m, int n, int rows, bool flag, uintptr_t
   call->y_type = type_of(y);
   call->device = x.device();
   call->flag = flag;
+  call->y_scalar = y.scalar_type();
   call->stream = reinterpret_cast<void*>(stream);
   torch::autograd::set_history(y, call);
   return call;

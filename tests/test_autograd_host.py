@@ -249,3 +249,32 @@ def test_tangents_are_refused():
                 si._wants_grad(*tensors)
         assert si._wants_grad(x, None, w) and not si._wants_grad(x)
     assert si._wants_grad(x, w) and not si._wants_grad(x)
+
+
+def test_gradients_of_another_size_type_or_device(calls):
+    """A node's own call and hooks in front of it are not looked at by autograd: another
+    type is y's first, as autograd makes it; another size or device is refused."""
+    run(calls, r'''
+def check(name):
+    x = tensor(M, N).requires_grad_()
+    y, leaves = make(name, x)
+    good = of(capture(lambda: y.grad_fn(torch.ones_like(y))))
+    for other in (torch.ones(y.shape).double(), torch.ones(y.shape).bfloat16(), torch.ones(y.shape)):
+        c = of(capture(lambda: y.grad_fn(other)))
+        assert c["dy"] != other.data_ptr() and c.get("dy_dtype") == good.get("dy_dtype") and c["lddy"] == good["lddy"], c
+    bad = (tensor(M - 1, y.shape[1]), tensor(M, y.shape[1] - 1), tensor(y.shape[1]), tensor(1, *y.shape), tensor(0, y.shape[1]),
+           torch.empty(y.shape, dtype=F16, device="meta"))
+    for other in bad:
+        text = []
+
+        def refused(f):
+            try:
+                f()
+            except RuntimeError as e:
+                text.append(str(e))
+        assert not capture(lambda: refused(lambda: y.grad_fn(other))) and "a gradient" in text[-1], (other.shape, text)
+        hook = y.grad_fn.register_prehook(lambda grads: (other,))
+        lines = capture(lambda: refused(lambda: torch.autograd.grad(y, x, torch.ones_like(y), retain_graph=True)))
+        assert not lines and len(text) == 2, (other.shape, lines, text)
+        hook.remove()
+''')
