@@ -99,7 +99,7 @@ struct Call : Node {
     TORCH_CHECK(grad.device() == device && grad.layout() == at::kStrided, "a gradient on ", grad.device(), ", not ", device);
     TORCH_CHECK(grad.dim() == 2 && grad.size(0) == m && grad.size(1) == y_n(), "a gradient of size ", grad.sizes(), ", not [", m,
                 ", ", y_n(), "]");
-    return grad.to(y_scalar);
+    return grad.to(y_scalar).resolve_neg();
   }
 
   virtual int64_t y_n() const { return rows; }  // values of a row of y

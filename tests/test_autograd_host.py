@@ -278,3 +278,17 @@ def check(name):
         assert not lines and len(text) == 2, (other.shape, lines, text)
         hook.remove()
 ''')
+
+
+def test_lazily_negated_gradients(calls):
+    """The sign of an imaginary part of a conjugate is a bit of the tensor, not of its
+    values: the library is given values."""
+    run(calls, r'''
+def check(name):
+    x = tensor(M, N).requires_grad_()
+    y, leaves = make(name, x)
+    dy = torch._neg_view(torch.ones_like(y))
+    assert dy.is_neg()
+    c = of(capture(lambda: torch.autograd.grad(y, x, dy)))
+    assert c["dy"] != dy.data_ptr(), c
+''')
