@@ -65,7 +65,7 @@ struct Call : Node {
   c10::Device device{at::kCPU};
   bool flag = false;  // W^T in memory, or LayerNorm
   at::ScalarType y_scalar = at::kFloat;
-  void* stream = nullptr;
+  void* raw_stream = nullptr;
 
   void release_variables() override {
     for (SavedVariable* v : {&x, &w, &w_up, &w_down, &g, &u, &h}) v->reset_data();
@@ -93,12 +93,15 @@ struct Call : Node {
   // the gradients that are asked for
   virtual void run(const Tensor& grad, variable_list& out) = 0;
 
-  // The gradient of y.  Autograd hands on one of y's size, type and device; the node's own
-  // call and its hooks are held to that here.
-  Tensor gradient(const Tensor& grad) const {
+  // The gradient of y.  Autograd hands on one of y's size, type and device on the stream of
+  // the forward call; the node's own call and its hooks are held to that here.
+  Tensor gradient(const Tensor& grad) {
     TORCH_CHECK(grad.device() == device && grad.layout() == at::kStrided, "a gradient on ", grad.device(), ", not ", device);
     TORCH_CHECK(grad.dim() == 2 && grad.size(0) == m && grad.size(1) == y_n(), "a gradient of size ", grad.sizes(), ", not [", m,
                 ", ", y_n(), "]");
+    const auto forward = stream();
+    TORCH_CHECK(!forward.has_value() || *forward == c10::impl::VirtualGuardImpl(device.type()).getStream(device),
+                "the backward pass was called on another stream than the forward call's");
     return grad.to(y_scalar).resolve_neg();
   }
 
@@ -144,7 +147,7 @@ struct LinearGrad : Call {
                                                             rows, flag, out[0].defined(), out[1].defined());
     const Tensor ws = scratch(xt, bytes);
     check(si_linear_backward(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), x_type, xr.ld, m, n, ptr(wt), rows, flag, ptr(out[0]),
-                             ptr(out[1]), ptr(ws), bytes, stream));
+                             ptr(out[1]), ptr(ws), bytes, raw_stream));
   }
 };
 
@@ -164,7 +167,7 @@ struct GatedGrad : Call {
     const Tensor ws = scratch(xt, bytes);
     check(si_gated_linear_backward(ptr(dh.t), type_of(dh.t), dh.ld, ptr(gt), type_of(gt), floats(ut), ptr(xt), x_type, xr.ld,
                                    m, n, ptr(wt), ptr(up), rows, ptr(out[0]), ptr(out[1]), ptr(out[2]), ptr(ws), bytes,
-                                   stream));
+                                   raw_stream));
   }
 };
 
@@ -186,7 +189,7 @@ struct MlpGrad : Call {
     const Tensor ws = scratch(xt, bytes);
     check(si_mlp_backward(ptr(dy.t), type_of(dy.t), dy.ld, ptr(xt), x_type, xr.ld, m, n, ptr(wt), ptr(up), ptr(down), rows,
                           ptr(ht), floats(gt), floats(ut), ptr(out[0]), ptr(out[1]), ptr(out[2]), ptr(out[3]), ptr(ws), bytes,
-                          stream));
+                          raw_stream));
   }
 };
 
@@ -201,7 +204,7 @@ struct NormGrad : Call {
     const size_t bytes = out[1].defined() || out[2].defined() ? si_layer_norm_backward_workspace_bytes(m, n) : 0;
     const Tensor ws = scratch(xt, bytes);
     check(si_layer_norm_backward(ptr(dy.t), dy.ld, ptr(xt), x_type, xr.ld, ptr(wt), w_type, flag, floats(mean), floats(r),
-                                 ptr(out[0]), ptr(out[1]), ptr(out[2]), m, n, ptr(ws), bytes, stream));
+                                 ptr(out[0]), ptr(out[1]), ptr(out[2]), m, n, ptr(ws), bytes, raw_stream));
   }
 };
 
@@ -245,7 +248,7 @@ std::shared_ptr<T> attach(Tensor y, int m, int n, int rows, bool flag, uintptr_t
   call->device = x.device();
   call->flag = flag;
   call->y_scalar = y.scalar_type();
-  call->stream = reinterpret_cast<void*>(stream);
+  call->raw_stream = reinterpret_cast<void*>(stream);
   torch::autograd::set_history(y, call);
   return call;
 }

@@ -180,3 +180,24 @@ def test_capture_with_weights_that_are_views_of_a_leaf_of_a_live_graph_is_refuse
         torch.cuda.synchronize()
         assert torch.autograd.grad(alive, leaf, torch.ones_like(alive))[0].shape == leaf.shape
         del alive, graph
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_a_node_called_by_itself(name):
+    """On the stream of the forward call: as in a backward pass.  On another one, where
+    its memory and launches would not be in order: refused before any launch."""
+    f, leaves = pick(name, gen(11))
+    x = values(gen(12), M, N).requires_grad_()
+    y = f(x)
+    dy = values(gen(13), *y.shape)
+    want = torch.autograd.grad(y, (x, *leaves), dy, retain_graph=True)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        with pytest.raises(RuntimeError, match="another stream"):
+            y.grad_fn(dy)
+        # autograd changes to the forward call's stream
+        other = torch.autograd.grad(y, (x, *leaves), dy, retain_graph=True)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(other, want))
+    got = [t for t in y.grad_fn(dy) if t is not None]
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and len(got) == len(want)
