@@ -1155,7 +1155,9 @@ class FP8MLPLayer:
     def prompt(self, x, out_dtype=None):
         """The MLP of any number of tokens, ``x [m][d]`` fp16, bf16 or float32: tokens
         to FP8, ``ReLU(x W_gate^T) * (x W_up^T)`` in ``x``'s type, that to FP8, the
-        product with ``W_down^T``; ``[m][d]`` in ``out_dtype`` (``x``'s type)."""
+        product with ``W_down^T``; ``[m][d]`` in ``out_dtype`` (``x``'s type).  With fp16
+        tokens a hidden value above 65504 becomes infinite, its block's scale NaN and
+        that token's output NaN; with bf16 or float32 tokens it does not."""
         if x.shape[-1] != self.d:
             raise ValueError(f"x has rows of {x.shape[-1]} values, the layer takes {self.d}")
         h = gated_linear_fp8(*quantize_rows_fp8(x), self.q_gate, self.s_gate, self.q_up, self.s_up, out_dtype=x.dtype)
