@@ -50,6 +50,19 @@ def _run(cmd):
     return out
 
 
+def autograd_lacks() -> str:
+    """What building the nodes of PyTorch's graph asks for beyond hipcc and is not here
+    ("" where nothing is missing)."""
+    if shutil.which(CXX) is None:
+        return f"a C++ compiler ({CXX})"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python's headers"
+    from torch.utils.cpp_extension import include_paths
+    if not any(os.path.exists(os.path.join(p, "torch", "csrc", "autograd", "function.h")) for p in include_paths()):
+        return "PyTorch's headers"
+    return ""
+
+
 def build_autograd() -> str:
     """Compile and link the nodes of PyTorch's graph (``csrc/autograd.cpp``, host code
     beside the library, which it finds in its own folder)."""
@@ -70,7 +83,9 @@ def build_autograd() -> str:
 def build(verbose: bool = False, trace: bool = False) -> str:
     """Compile every HIP source and link the shared library (``trace``: the
     phase-trace variant), then the nodes of PyTorch's graph; returns the library's
-    path."""
+    path.  The library asks for hipcc alone: where the nodes cannot be built it is
+    complete without them (the C ABI, and every call without gradients), which is said
+    on stderr, and calls that need them raise."""
     out_dir = os.path.join(BUILD, "trace") if trace else BUILD
     lib = TRACE_LIB if trace else LIB
     os.makedirs(out_dir, exist_ok=True)
@@ -91,7 +106,14 @@ def build(verbose: bool = False, trace: bool = False) -> str:
     _run([HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp])
     shutil.move(tmp, lib)
     if not trace:
-        build_autograd()
+        lacks = autograd_lacks()
+        if lacks:
+            if os.path.exists(AUTOGRAD_LIB):  # of other sources
+                os.remove(AUTOGRAD_LIB)
+            print(f"{os.path.basename(AUTOGRAD_LIB)} is not built, gradients are not available: {lacks} missing",
+                  file=sys.stderr)
+        else:
+            build_autograd()
     return lib
 
 
