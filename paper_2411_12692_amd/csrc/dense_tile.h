@@ -24,7 +24,8 @@
 // 16 cycles each and are the next limit.  Measured at 8192^3, random values, after short
 // and long load of the card: x W^T 1310-1150, dy W 1390-1150, dy^T x 1410-1330, gate and
 // up without their sums 1430-1360 TFLOP/s, no LDS conflicts but the outputs' (3% of its
-// cycles); e4m3 2350-2250, and 2000 at 13824 x 5120 and 4096 tokens (2270 of zeros).
+// cycles); e4m3 2350-2250, and 1860-1890 at 13824 x 5120 and 4096 tokens (2000 the quickest
+// call, 2270 of zeros), where 864 tiles are 3.4 rounds of the compute units taken as 4.
 // Small tiles are for few tokens, where W's bytes bound: 13824 x 5120 gate and up, 37
 // tokens, 56 us, 5.1 TB/s of W.
 #pragma once

@@ -11,7 +11,7 @@
 // same columns of every row of its block, so the columns' sums stay in registers
 // over the block's rows and are written once a block; k_norm_columns adds the
 // blocks' sums in their order, so that the gradients are the same bits in every run.
-// Measured at 4096 x 5120, bf16: forward 18.4 us (4.6 TB/s), backward 38 to 40 (3.7 TB/s,
+// Measured at 4096 x 5120, bf16: forward 19.6 us (4.3 TB/s), backward 38 to 40 (3.7 TB/s,
 // 21 MB of blocks' sums among its bytes; 256, 768 and 1024 blocks: 37.5, 42, 44 us, and
 // 15.2, 14, 15.4 where 512 take 13.4, at 1999 x 4096 without a bias) and 4.3 for the
 // columns; a token of 4096 2.7.
